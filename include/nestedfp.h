@@ -287,6 +287,98 @@ int nestedfp_linear(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_la
                     void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * What stands around the linears of a decoder layer: the norm in front of qkv and gate/up, and between qkv and o the
+ * rotary positions, the key/value cache and the attention that reads it.
+ *
+ * add_rms_norm: for every row of K values (K a positive multiple of 16, at most 2^21; row strides as for X above, 16-byte
+ * aligned pointers)
+ *   h = fp16(X + residual)                  (h = X where residual is NULL)
+ *   y = h / sqrt(mean(h^2) + eps) * weight  (in binary32; weight is FP16 [K])
+ * and writes whichever of these is not NULL (one of Y and Xq at least):
+ *   sum    h, the residual stream that the next layer adds to; may be `residual` or X itself,
+ *   Y      fp16(y),
+ *   Xq     E4M3_RNE_saturating(y / scale), dense [M,K] bytes, and scales [M], scale = amax|y| / 448 (1 if the row is all
+ *          zero): the operands of nestedfp_gemm_fp8_prequantized.  The codes come from y in binary32, not from its FP16
+ *          rounding (nestedfp_quantize_act of Y rounds once more).
+ * eps must be finite and not negative.  Inputs must be finite where Xq is wanted; an Inf or a NaN otherwise stays in its row.
+ */
+int nestedfp_add_rms_norm(const uint16_t *X, int64_t M, int64_t K, int64_t ldx,
+                          const uint16_t *residual, int64_t ldr, const uint16_t *weight, float eps,
+                          uint16_t *sum, int64_t lds, uint16_t *Y, int64_t ldy,
+                          uint8_t *Xq, float *scales, void *stream);
+
+/*
+ * A paged cache of keys and values: `pages` pages of `page_tokens` tokens (16, 32, 64, 128 or 256) for `kv_heads` heads of
+ * `head_dim` dims (64, 96, 128 or 256), in FP16 or in E4M3 with one scale per head (value = code * scale; NULL: 1).  The
+ * struct lives in HOST memory, its pointers are device pointers owned by the caller, k and v 16-byte aligned and
+ * nestedfp_kv_cache_bytes long each.  pages * page_tokens is at most 2^31 - 1, pages * page_tokens * kv_heads below 2^35.
+ *   Storage: [pages][kv_heads][page_tokens / 16] blocks of 16 tokens.  With E elements in 16 bytes (8 in FP16, 16 in E4M3) a
+ *   key block is [head_dim / E][16 tokens][E dims] and a value block [16 / E][head_dim][E tokens]: the order in which
+ *   lanes hold matrix operands, so that the kernels load both with whole lines and use them as they come.
+ * A SLOT is the place of a token in the cache: page * page_tokens + place in the page.  A sequence's token t lies in page
+ * table[t / page_tokens] of its row of the page table.
+ */
+typedef enum {
+    NESTEDFP_CACHE_FP16 = 0,
+    NESTEDFP_CACHE_E4M3 = 1
+} nestedfp_cache_type;
+
+typedef struct {
+    int64_t pages;
+    int32_t page_tokens, kv_heads, head_dim;
+    int32_t type;               /* nestedfp_cache_type */
+    void *k, *v;
+    const float *k_scale, *v_scale;     /* [kv_heads], E4M3 only */
+} nestedfp_kv_cache;
+
+size_t nestedfp_kv_cache_bytes(const nestedfp_kv_cache *cache_host);      /* of k, and of v; 0 for an invalid description */
+
+/*
+ * rope_append: rotary positions on the queries and keys of M new tokens, and the write of their keys and values into the cache.
+ * Q [M, heads * head_dim] (row stride ldq), K and V [M, kv_heads * head_dim] (ldk, ldv) are the rows that the qkv linear
+ * wrote; strides are multiples of 8, pointers 16-byte aligned, heads is a multiple of kv_heads.  The first `rotary_dim` dims of a head
+ * (a multiple of 16, at most head_dim; 0: none) are pairs (i, i + rotary_dim / 2):
+ *   out_i = x_i cos - x_j sin,  out_j = x_j cos + x_i sin,   j = i + rotary_dim / 2
+ * with cos and sin from [max_positions, rotary_dim / 2] float tables at the token's position, in binary32; the rotated
+ * queries go to Qout (FP16; may be Q itself), keys and values to slots[m], rounded once (E4M3: saturating at +-448 scale).
+ * A token whose slot is negative or beyond the cache is not written to it (padding of a captured batch); a position
+ * outside the tables gives NaN.  Slots of one call must differ from each other.
+ */
+int nestedfp_rope_append(const uint16_t *Q, int64_t ldq, const uint16_t *K, int64_t ldk, const uint16_t *V, int64_t ldv,
+                         int64_t M, int64_t heads, const float *cos_table, const float *sin_table, int64_t max_positions,
+                         int64_t rotary_dim, const int32_t *positions, const int32_t *slots,
+                         uint16_t *Qout, int64_t ldqo, const nestedfp_kv_cache *cache_host, void *stream);
+
+/*
+ * paged_attention: for the new tokens of `batch` sequences, whose keys and values are in the cache already,
+ *   o = softmax over visible t of (scale * q . k_t), times v_t
+ * for every query head; query head h reads key/value head h / (heads / kv_heads).
+ *   lens [batch]       tokens of every sequence in the cache, the new ones among them (they are its last ones)
+ *   table [batch][table_columns] (row stride ld_table): the sequences' pages
+ *   starts [batch + 1] rows of Q at which the sequences' new tokens begin (starts[batch] = tokens); NULL: every sequence
+ *                      has tokens / batch of them (one for a plain decode step, a few where tokens were drafted)
+ *   max_new, max_len   no sequence has more new tokens, or more tokens, than this.  They size the launch: a new token past max_new
+ *                      gets no output; a sequence longer than max_len costs time, its result is the same
+ *   window, sinks      a new token at position pos sees t <= pos and, with window > 0, of these only t > pos - window and t < sinks
+ * A new token that sees nothing (its sequence's length is smaller than its new tokens) gets zeros.  Pages that no new token sees are
+ * not read, nor are their entries in the table; values that no new token sees may hold anything.  An entry outside the
+ * cache where a token is seen gives NaN; lengths and starts outside their arrays are cut off.
+ * Scores, sums and accumulators are binary32, O is FP16 [tokens, heads * head_dim] (row stride ldo); strides are multiples of 8,
+ * Q 16-byte and O 8-byte aligned.
+ * The workspace follows the rules above (WORKSPACE); where a sequence is split over workgroups they leave their sums in it.
+ * The results do not depend on timing: the parts are joined in order.
+ */
+size_t nestedfp_paged_attention_workspace_size(int64_t tokens, int64_t batch, int64_t heads,
+                                               const nestedfp_kv_cache *cache_host, int64_t max_new, int64_t max_len,
+                                               int64_t window, int64_t sinks);
+int nestedfp_paged_attention(const uint16_t *Q, int64_t tokens, int64_t ldq, int64_t heads,
+                             const nestedfp_kv_cache *cache_host,
+                             const int32_t *table, int64_t ld_table, int64_t table_columns,
+                             const int32_t *lens, int64_t batch, const int32_t *starts,
+                             int64_t max_new, int64_t max_len, float scale, int64_t window, int64_t sinks,
+                             uint16_t *O, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Load-aware mode selection (Sec. 5.4): an iteration runs in FP8 mode when the number of
  * tokens it has to process exceeds `threshold` (1024 in the paper's experiment), otherwise in
  * FP16 mode.  Pure host function; returns a nestedfp_mode.

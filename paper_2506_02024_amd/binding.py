@@ -97,6 +97,17 @@ def lib():
     L.nestedfp_linear_workspace_size.argtypes = [i64, vp, ci]
     L.nestedfp_linear.restype = ci
     L.nestedfp_linear.argtypes = [vp, i64, i64, vp, ci, vp, vp, i64, vp, sz, vp]
+    L.nestedfp_add_rms_norm.restype = ci
+    L.nestedfp_add_rms_norm.argtypes = [vp, i64, i64, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp, vp]
+    L.nestedfp_kv_cache_bytes.restype = sz
+    L.nestedfp_kv_cache_bytes.argtypes = [vp]
+    L.nestedfp_rope_append.restype = ci
+    L.nestedfp_rope_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, vp, vp, i64, i64, vp, vp, vp, i64, vp, vp]
+    L.nestedfp_paged_attention_workspace_size.restype = sz
+    L.nestedfp_paged_attention_workspace_size.argtypes = [i64, i64, i64, vp, i64, i64, i64, i64]
+    L.nestedfp_paged_attention.restype = ci
+    L.nestedfp_paged_attention.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, vp, i64, vp, i64, i64, f32, i64, i64, vp, i64,
+                                           vp, sz, vp]
     L.nestedfp_tune.restype = ci
     L.nestedfp_tune.argtypes = [c.c_char_p, i64]
     L.nestedfp_tune_name.restype = c.c_char_p
@@ -464,6 +475,184 @@ def linear(X, layer, mode, act_scale=None, out=None, workspace=None):
     st = lib().nestedfp_linear(_ptr(X), M, ldx, layer._ref, int(mode), _ptr(act_scale),
                                _ptr(out), ldy, _ptr(workspace), workspace.numel(), _stream())
     _check(st, "nestedfp_linear")
+    return out
+
+
+def _dtype(t, dtype, name):
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s" % (name, dtype))
+
+
+def add_rms_norm(X, weight, eps=1e-5, residual=None, sum_out=None, out=None, Xq=None, scales=None):
+    """h = fp16(X + residual), y = h / sqrt(mean(h^2) + eps) * weight over the rows of X (fp16 [M,K]).
+
+    Writes those of sum_out (h; may be residual or X), out (fp16 y), Xq (uint8 [M,K], E4M3 codes of y) with scales (float32
+    [M]) that are given, and returns (out, Xq, scales, sum_out).  With neither out nor Xq, out is made."""
+    M, K, ldx = _rowmajor(X, "X")
+    _dtype(X, torch.float16, "X")
+    if weight.dtype != torch.float16 or weight.shape != (K,) or not weight.is_contiguous():
+        raise ValueError("weight must be a contiguous float16 [K] tensor")
+    if out is None and Xq is None:
+        out = torch.empty((M, K), dtype=torch.float16, device=X.device)
+    lds = []
+    for t, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")):
+        if t is None:
+            lds.append(0)
+            continue
+        rows, cols, ld = _rowmajor(t, name)
+        if rows != M or cols != K or t.dtype != torch.float16:
+            raise ValueError("%s must be float16 [M,K]" % name)
+        lds.append(ld)
+    if Xq is not None:
+        if Xq.dtype != torch.uint8 or Xq.shape != (M, K) or not Xq.is_contiguous():
+            raise ValueError("Xq must be a contiguous uint8 [M,K] tensor")
+        if scales is None or scales.dtype != torch.float32 or scales.shape != (M,) or not scales.is_contiguous():
+            raise ValueError("scales must be a contiguous float32 [M] tensor")
+    st = lib().nestedfp_add_rms_norm(_ptr(X), M, K, ldx, _ptr(residual), lds[0], _ptr(weight), eps, _ptr(sum_out), lds[1],
+                                     _ptr(out), lds[2], _ptr(Xq), _ptr(scales), _stream())
+    _check(st, "nestedfp_add_rms_norm")
+    return out, Xq, scales, sum_out
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+CACHE_FP16, CACHE_E4M3 = 0, 1
+
+
+class KVCache:
+    """A paged cache of keys and values as the library describes it (include/nestedfp.h has the storage).
+
+    KVCache(pages, page_tokens, kv_heads, head_dim, dtype=torch.float16 or torch.uint8 (E4M3 codes), device=...) makes the
+    storage; KVCache(k=..., v=...) describes one that is there: contiguous [pages, kv_heads, page_tokens / 16, head_dim / E,
+    16, E] keys and [pages, kv_heads, page_tokens / 16, 16 / E, head_dim, E] values, E = 8 (float16) or 16 (uint8).
+    k_scale, v_scale: float32 [kv_heads], of E4M3 caches (None: 1).  Keeps the device buffers alive."""
+
+    def __init__(self, pages=0, page_tokens=0, kv_heads=0, head_dim=0, dtype=torch.float16, device=None, k=None, v=None,
+                 k_scale=None, v_scale=None):
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        if k is None:
+            if dtype not in (torch.float16, torch.uint8):
+                raise ValueError("dtype must be float16 or uint8 (E4M3 codes)")
+            e = 8 if dtype == torch.float16 else 16
+            head = (pages, kv_heads, page_tokens // 16)
+            k = torch.zeros(head + (head_dim // e, 16, e), dtype=dtype, device=device)
+            v = torch.zeros(head + (16 // e, head_dim, e), dtype=dtype, device=device)
+        else:
+            e = {torch.float16: 8, torch.uint8: 16}.get(k.dtype, 0)
+            shape = tuple(k.shape)
+            if not e or v.dtype != k.dtype or len(shape) != 6 or shape[4:] != (16, e):
+                raise ValueError("k must be float16 [pages, kv_heads, blocks, head_dim / 8, 16, 8] or uint8 [.., head_dim / 16, 16, 16]")
+            head, head_dim = shape[:3], shape[3] * e
+            if tuple(v.shape) != head + (16 // e, head_dim, e) or not (k.is_contiguous() and v.is_contiguous()):
+                raise ValueError("v must be contiguous [pages, kv_heads, blocks, 16 / E, head_dim, E]")
+            pages, kv_heads, page_tokens = head[0], head[1], head[2] * 16
+        for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if s is not None and (s.dtype != torch.float32 or s.shape != (kv_heads,) or not s.is_contiguous()):
+                raise ValueError("%s must be a contiguous float32 [kv_heads] tensor" % name)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim = int(pages), int(page_tokens), int(kv_heads), int(head_dim)
+        self._c = _CacheStruct(self.pages, self.page_tokens, self.kv_heads, self.head_dim,
+                               CACHE_FP16 if k.dtype == torch.float16 else CACHE_E4M3, k.data_ptr(), v.data_ptr(),
+                               _ptr(k_scale), _ptr(v_scale))
+        self._ref = ctypes.byref(self._c)
+        if pages and not lib().nestedfp_kv_cache_bytes(self._ref):
+            raise ValueError("a cache has pages of 16, 32, 64, 128 or 256 tokens and heads of 64, 96, 128 or 256 dims")
+
+    def keys(self):
+        """The keys as a strided view [pages, blocks of a page, 16 tokens, kv_heads, head_dim / E, E]."""
+        return self.k.permute(0, 2, 4, 1, 3, 5)
+
+    def values(self):
+        """The values as a strided view [pages, blocks of a page, 16 / E, E tokens, kv_heads, head_dim]."""
+        return self.v.permute(0, 2, 3, 5, 1, 4)
+
+
+def _heads(t, dim, name):
+    rows, cols, ld = _rowmajor(t, name)
+    if t.dtype != torch.float16 or cols == 0 or cols % dim:
+        raise ValueError("%s must be float16 [tokens, heads * head_dim]" % name)
+    return rows, cols // dim, ld
+
+
+def _indices(t, n, name):
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of %d" % (name, n))
+    return t.data_ptr()
+
+
+def rope_append(q, k, v, positions, slots, cache, cos=None, sin=None, out=None):
+    """Rotates the heads of q (fp16 [M, heads * head_dim]) and k by the rows of cos and sin (float32 [positions, rotary_dim / 2];
+    None: no rotation) at `positions` (int32 [M]), and writes k and v ([M, kv_heads * head_dim]) to `slots` (int32 [M]) of the
+    cache.  Returns the rotated q (out, which may be q; made if None)."""
+    dim = cache.head_dim
+    M, heads, ldq = _heads(q, dim, "q")
+    rows_k, kv_k, ldk = _heads(k, dim, "k")
+    rows_v, kv_v, ldv = _heads(v, dim, "v")
+    if rows_k != M or rows_v != M or kv_k != cache.kv_heads or kv_v != cache.kv_heads:
+        raise ValueError("k and v must be [tokens, kv_heads * head_dim] of the cache")
+    known = rotary = 0
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    if cos is not None:
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()):
+            raise ValueError("cos and sin must be contiguous float32 [positions, rotary_dim / 2] tensors")
+        known, rotary = cos.shape[0], 2 * cos.shape[1]
+    if out is None:
+        out = torch.empty((M, heads * dim), dtype=torch.float16, device=q.device)
+    rows_o, heads_o, ldo = _heads(out, dim, "out")
+    if rows_o != M or heads_o != heads:
+        raise ValueError("out must have the shape of q")
+    st = lib().nestedfp_rope_append(_ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, M, heads, _ptr(cos), _ptr(sin), known, rotary,
+                                    _indices(positions, M, "positions") if rotary else None, _indices(slots, M, "slots"),
+                                    _ptr(out), ldo, cache._ref, _stream())
+    _check(st, "nestedfp_rope_append")
+    return out
+
+
+def paged_attention_workspace_size(tokens, heads, cache, batch, max_new=None, max_len=0, window=0, sinks=0):
+    return int(lib().nestedfp_paged_attention_workspace_size(tokens, batch, heads, cache._ref, tokens if max_new is None else max_new,
+                                                             max_len, window, sinks))
+
+
+def paged_attention(q, cache, table, lens, starts=None, max_new=None, max_len=None, scale=None, window=0, sinks=0, out=None,
+                    workspace=None):
+    """Attention of new tokens (q: fp16 [tokens, heads * head_dim]) over the paged cache.
+
+    table: int32 [batch, columns], the sequences' pages; lens: int32 [batch], their tokens with the new ones, which are
+    the last; starts: int32 [batch + 1], rows of q at which the sequences begin (None: as many for each).  max_new and max_len bound
+    the sequences' new tokens and lengths (None: what the shapes of q and table allow; a tight max_len makes a better launch).
+    scale: head_dim ** -0.5 if None.  window, sinks: see include/nestedfp.h."""
+    dim = cache.head_dim
+    tokens, heads, ldq = _heads(q, dim, "q")
+    batch = lens.shape[0]
+    if table.dtype != torch.int32:
+        raise ValueError("table must be int32")
+    rows, columns, ld_table = _rowmajor(table, "table")
+    if rows != batch:
+        raise ValueError("table must be [batch, columns]")
+    if max_new is None:
+        max_new = tokens if starts is not None else tokens // max(batch, 1)
+    if max_len is None:
+        max_len = columns * cache.page_tokens
+    if out is None:
+        out = torch.empty((tokens, heads * dim), dtype=torch.float16, device=q.device)
+    rows_o, heads_o, ldo = _heads(out, dim, "out")
+    if rows_o != tokens or heads_o != heads:
+        raise ValueError("out must have the shape of q")
+    L = lib()
+    if workspace is None:
+        workspace = _workspace(L.nestedfp_paged_attention_workspace_size(tokens, batch, heads, cache._ref, max_new, max_len, window, sinks),
+                               q.device)
+    st = L.nestedfp_paged_attention(q.data_ptr(), tokens, ldq, heads, cache._ref, table.data_ptr(), ld_table, columns,
+                                    _indices(lens, batch, "lens"), batch, None if starts is None else _indices(starts, batch + 1, "starts"),
+                                    max_new, max_len, dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ldo,
+                                    workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "nestedfp_paged_attention")
     return out
 
 

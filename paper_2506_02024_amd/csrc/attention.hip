@@ -1,0 +1,593 @@
+// Attention of new tokens over a paged cache:  o = sum_t p_t v_t / sum_t p_t,  p_t = exp(c q.k_t - m),  over the tokens t
+// of the sequence that a new token at position `pos` sees:  t <= pos and (no window, or t > pos - window, or t < sinks).
+//
+// Rows.  The new tokens of a sequence and the query heads that share a key/value head are the rows of one small matrix:
+// row r is new token r / group, head r % group.  A tile of rows reads every key and value once for all of them.
+// Both products are transposed: S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's scores, the statistics of a
+// row lie in one column of lanes, and P^T becomes the operand of the second product by exchanging registers between groups of 16 lanes.
+//
+// The visible tokens are walked in blocks of 16 (a block lies in one page): first the blocks of the sinks, then those of the
+// window; pages outside are never looked at.
+#include "nfp_device.h"
+#include "nfp_host.h"
+
+namespace nfp {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_inff();
+// Probabilities are at most 2^kShift instead of 1: FP16 has normal numbers down to 2^-14, so that what counts as subnormal
+// starts 2^-26 below the row's maximum.  Sums carry the same factor, which the division takes out.
+constexpr float kShift = 12.0f;
+
+// ---- exchanges between the four groups of 16 lanes ------------------------------------------------------------------------
+// swap32: upper half of a with lower half of b; swap16: odd groups of a with even groups of b.
+__device__ __forceinline__ void swap32(uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ float max_of_groups(float v) {
+    uint32_t a = __float_as_uint(v), b = a;
+    swap32(a, b);
+    v = fmaxf(__uint_as_float(a), __uint_as_float(b));
+    a = b = __float_as_uint(v);
+    swap16(a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float sum_of_groups(float v) {
+    uint32_t a = __float_as_uint(v), b = a;
+    swap32(a, b);
+    v = __uint_as_float(a) + __uint_as_float(b);
+    a = b = __float_as_uint(v);
+    swap16(a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+
+// 16 E4M3 codes -> 16 FP16 values (every code is one)
+__device__ __forceinline__ void widen(const u32x4 &v, half8 &lo, half8 &hi) {
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    half2v h[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
+        h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true);
+    }
+    lo = half8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+    hi = half8{h[4][0], h[4][1], h[5][0], h[5][1], h[6][0], h[6][1], h[7][0], h[7][1]};
+}
+
+// Values that are not finite.  Their products with a probability of zero are NaN, also where the probability is zero because
+// the row does not see the token, and so is the product with the rest of a probability.  The loops therefore run on
+// the values as they come; sums that are not finite at the end are made again without those values, and what they add
+// to the rows that do see them is found by itself: counts of +Inf, -Inf and NaN per row and column.
+enum { kPlusInf = 0, kMinusInf = 1, kNaN = 2 };
+template <bool FP8>
+__device__ __forceinline__ u32x4 only_finite(const u32x4 &v) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (FP8) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) w[i] = (w[i] >> j & 0x7fu) == 0x7fu ? w[i] & ~(0xffu << j) : w[i];
+        } else {
+            w[i] = (w[i] & 0x7c00u) == 0x7c00u ? w[i] & 0xffff0000u : w[i];
+            w[i] = (w[i] & 0x7c000000u) == 0x7c000000u ? w[i] & 0xffffu : w[i];
+        }
+    }
+    return u32x4{w[0], w[1], w[2], w[3]};
+}
+// 1 where an FP16 value is of a kind, 0 elsewhere: bits from `low` to `high` without the sign bits that `sign` clears
+__device__ __forceinline__ half8 of_kind(half8 v, int kind) {
+    const u32x4 b = __builtin_bit_cast(u32x4, v);
+    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+    const uint32_t sign = kind == kNaN ? 0x7fffu : 0xffffu, low = kind == kPlusInf ? 0x7c00u : kind == kMinusInf ? 0xfc00u : 0x7c01u;
+    const uint32_t span = kind == kNaN ? 0x3feu : 0u;
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[i] = (w[i] & sign) - low <= span ? 0x3c00u : 0u;
+        r[i] |= (w[i] >> 16 & sign) - low <= span ? 0x3c000000u : 0u;
+    }
+    return __builtin_bit_cast(half8, u32x4{r[0], r[1], r[2], r[3]});
+}
+__device__ __forceinline__ float of_kind_value(int kind) {
+    return kind == kPlusInf ? -kNegInf : kind == kMinusInf ? kNegInf : __builtin_nanf("");
+}
+__device__ __forceinline__ bool not_finite(const floatx4 &v) {
+    // (a difference with itself is zero for finite values alone)
+    const floatx4 z = v - v;
+    return !(z[0] == 0.0f && z[1] == 0.0f && z[2] == 0.0f && z[3] == 0.0f);
+}
+
+// What a sequence's place in the batch and in the cache comes down to; lengths and starts that do not fit the arrays
+// they index are cut off, so that nothing outside is read.
+struct Sequence { int first, fresh, length; };
+__device__ __forceinline__ Sequence sequence(const AttentionArgs &p, int b) {
+    Sequence s;
+    s.length = max(0, min(p.lens[b], (int)min((int64_t)0x7fffffff, (int64_t)p.columns << (p.page_shift + 4))));
+    if (p.starts) {
+        const int from = p.starts[b], to = p.starts[b + 1];
+        s.first = max(0, min(from, p.tokens));
+        s.fresh = max(0, min(min(to, p.tokens) - s.first, p.max_new));
+        if (from < 0) s.fresh = 0;
+    } else {
+        s.first = b * p.per;
+        s.fresh = p.per;
+    }
+    return s;
+}
+
+// The last token before the window of a row at `pos` (-1: there is none), and whether a row with these two sees a token.
+__device__ __forceinline__ int before(const AttentionArgs &p, int pos) {
+    return p.window > 0 && pos >= p.window ? pos - p.window : -1;
+}
+__device__ __forceinline__ bool sees(int t, int pos, int low, int sinks) { return t <= pos && (t > low || t < sinks); }
+
+// Blocks that the rows of new tokens i0 ... i1 see, in the order in which they are walked.
+struct Walk {
+    int sink_blocks, low_block, blocks;              // blocks in all: sink_blocks from 0, the rest from low_block
+    __device__ __forceinline__ int block(int v) const { return v < sink_blocks ? v : v - sink_blocks + low_block; }
+};
+__device__ __forceinline__ Walk walk(const AttentionArgs &p, int low_pos, int high_pos) {
+    Walk w;
+    const int high_block = high_pos < 0 ? 0 : (high_pos >> 4) + 1;
+    w.low_block = min((before(p, low_pos) + 1) >> 4, high_block);
+    w.sink_blocks = p.window > 0 ? min((int)(((int64_t)p.sinks + 15) >> 4), w.low_block) : 0;
+    w.blocks = w.sink_blocks + high_block - w.low_block;
+    return w;
+}
+// ---- streaming kernel -------------------------------------------------------------------------------------------------------
+// For few rows: bound by the bytes of the cache.  A workgroup of four waves takes 16 * RT rows and a stretch of the
+// sequence's blocks; a wave loads keys and values of 32 tokens (64 in E4M3) straight into registers, in operand order, every
+// load instruction whole lines.  The waves' sums meet in LDS; where a sequence takes more than one workgroup, each leaves its sums
+// in the workspace and the one that comes last joins them in order.
+// P is carried as two FP16 terms (its FP16 rounding and the rest): the second product costs nothing here, and the
+// result then has the precision of the 32-bit sums.
+template <int D, bool FP8, int RT>
+__global__ void __launch_bounds__(256)
+attention_stream_kernel(AttentionArgs p) {
+    constexpr int NT = FP8 ? 4 : 2;                    // blocks per step
+    constexpr int BLOCK = 16 * D * (FP8 ? 1 : 2);      // bytes of a block
+    constexpr int KL = (BLOCK + 1023) / 1024;          // 16-byte loads per lane for the keys of a block
+    constexpr int QS = FP8 ? 2 * KL : KL;              // operands of 32 dims
+    constexpr int DB = D / 16;
+    constexpr int LD = D + 4;
+    __shared__ float part[2][16 * RT][LD];
+    __shared__ float stat[4][2][16 * RT];
+    __shared__ int last;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, col = lane & 15;
+    const int tiles = p.batch * p.kv_heads * p.row_tiles;
+    const int chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
+    const int rt0 = tile % p.row_tiles, head = tile / p.row_tiles % p.kv_heads, b = tile / p.row_tiles / p.kv_heads;
+    const Sequence sq = sequence(p, b);
+    const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
+    if (row0 >= rows) return;
+    const int row1 = min(rows, row0 + 16 * RT) - 1;
+    const int past = sq.length - sq.fresh;
+    const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
+    const Walk w = walk(p, low_pos, high_pos);
+    // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
+    const int chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+    if (chunk >= chunks) return;
+    const int v0 = chunk * p.chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
+
+    // queries, as the second operand: column = row, dims in the order in which the keys' chunks come
+    int row[RT], pos[RT], low[RT];
+    half8 q[RT][QS];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        row[r] = row0 + 16 * r + col;
+        const int i = min(row[r], row1) / p.group, g = min(row[r], row1) - i * p.group;
+        pos[r] = past + i;
+        low[r] = before(p, pos[r]);
+        const uint16_t *src = p.Q + (int64_t)(sq.first + i) * p.ldq + (int64_t)(head * p.group + g) * D;
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            const int dim = FP8 ? 16 * (4 * (s >> 1) + group) + 8 * (s & 1) : 8 * (4 * s + group);
+            q[r][s] = dim < D ? *reinterpret_cast<const half8 *>(src + dim) : half8{};
+        }
+    }
+    floatx4 acc[RT][DB];
+    float top[RT], total[RT];
+    const float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
+    const int in_page = (1 << p.page_shift) - 1;
+
+    // this wave's blocks of the 256 from `base`: step j takes blocks base + NT (4 j + wave) ...; lane NT j + k has the page of the k-th of step j
+    const auto pages_from = [&](int base) {
+        const int v = base + NT * (4 * (lane / NT) + wave) + lane % NT;
+        return v < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v) >> p.page_shift)] : 0;
+    };
+    const auto offset = [&](int block, int pg, bool valid) {
+        return ((((int64_t)(valid ? pg : 0) * p.kv_heads + head) << p.page_shift) + (valid ? block & in_page : 0)) * BLOCK;
+    };
+    // this lane's values: of its group's block, 8 (16 in E4M3) tokens of dims 16 d + col
+    const int mine_in_block = (FP8 ? 0 : (group & 1) * D * 16) + col * 16, mine_first = FP8 ? 0 : 8 * (group & 1);
+    const int first_low = before(p, low_pos), last_low = before(p, high_pos);
+
+    bool clean = false;
+    for (;;) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            top[r] = kNegInf;
+            total[r] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[r][d] = floatx4{0, 0, 0, 0};
+        }
+        for (int base = v0; base < v1; base += 64 * 4) {
+            const int page = pages_from(base);
+            for (int j = 0; j < 64 / NT; ++j) {
+                const int v = base + NT * (4 * j + wave);
+                if (v >= v1) break;
+                u32x4 kk[NT][KL], vv[DB];
+                int t0[NT];
+                bool plain = true;
+                uint32_t missing = 0;                      // blocks of this step that are not there
+                const uint8_t *mine = nullptr;             // of this lane's block of values
+#pragma unroll
+                for (int k = 0; k < NT; ++k) {
+                    const int block = w.block(min(v + k, v1 - 1)), pg = __builtin_amdgcn_readlane(page, NT * j + k);
+                    const bool there = v + k < v1;
+                    const bool valid = (uint32_t)pg < (uint32_t)p.pages;
+                    t0[k] = there ? block * 16 : 0x7ffffff0;          // (nothing sees those)
+                    if (there && !valid) missing |= 1u << k;
+                    plain &= there && valid && t0[k] + 15 <= low_pos && (t0[k] > last_low || t0[k] + 15 < p.sinks);
+                    const int64_t at = offset(block, pg, valid && there);
+                    const uint8_t *kb = p.k + at, *vb = p.v + at;
+#pragma unroll
+                    for (int s = 0; s < KL; ++s) {
+                        int off = s * 1024 + lane * 16;
+                        if (BLOCK % 1024 != 0 && off >= BLOCK) off -= 512;           // (those dims are multiplied by zero)
+                        kk[k][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kb + off));
+                    }
+                    if ((FP8 ? group : group >> 1) == k) mine = vb;
+                }
+                mine += mine_in_block;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) vv[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(mine + d * 256));
+                // scores, in units of log 2
+                floatx4 s4[RT][NT];
+#pragma unroll
+                for (int k = 0; k < NT; ++k)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        floatx4 s = floatx4{0, 0, 0, 0};
+#pragma unroll
+                        for (int i = 0; i < KL; ++i) {
+                            if constexpr (FP8) {
+                                half8 lo, hi;
+                                widen(kk[k][i], lo, hi);
+                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[r][2 * i], s, 0, 0, 0);
+                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[r][2 * i + 1], s, 0, 0, 0);
+                            } else {
+                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kk[k][i]), q[r][i], s, 0, 0, 0);
+                            }
+                        }
+                        s4[r][k] = s * scale;
+                    }
+                if (!plain) {
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (missing >> k & 1) s4[r][k][i] = __builtin_nanf("");
+                                if (!sees(t0[k] + 4 * group + i, pos[r], low[r], p.sinks)) s4[r][k][i] = kNegInf;
+                                // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
+                            }
+                    // values that no row sees may be anything: memory that was never written, another sequence's
+                    int t = mine_first;
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+                        if ((FP8 ? group : group >> 1) == k) t += t0[k];
+                    uint32_t keep[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < (FP8 ? 16 : 8); ++i)
+                        if (sees(t + i, high_pos, first_low, p.sinks)) keep[FP8 ? i >> 2 : i >> 1] |= FP8 ? 0xffu << (8 * (i & 3)) : 0xffffu << (16 * (i & 1));
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) vv[d] &= u32x4{keep[0], keep[1], keep[2], keep[3]};
+                }
+                if (clean)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) vv[d] = only_finite<FP8>(vv[d]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    float m = top[r];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) m = fmaxf(fmaxf(fmaxf(m, s4[r][k][0]), fmaxf(s4[r][k][1], s4[r][k][2])), s4[r][k][3]);
+                    m = max_of_groups(m);
+                    const float from = fmaxf(m, -1e30f) - kShift;        // (a row that has seen nothing yet)
+                    const float shrink = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
+                    top[r] = m;
+                    uint32_t hi[NT][2], lo[NT][2];
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) {
+                        float e[4], rest[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            e[i] = __builtin_amdgcn_exp2f(s4[r][k][i] - from);
+                            sum += e[i];
+                            rest[i] = e[i] - (float)(_Float16)e[i];
+                        }
+                        hi[k][0] = float2_to_half2_bits(e[0], e[1]);
+                        hi[k][1] = float2_to_half2_bits(e[2], e[3]);
+                        lo[k][0] = float2_to_half2_bits(rest[0], rest[1]);
+                        lo[k][1] = float2_to_half2_bits(rest[2], rest[3]);
+                    }
+                    total[r] = total[r] * shrink + sum;
+                    if (__builtin_amdgcn_ballot_w64(shrink != 1.0f)) {
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) acc[r][d] *= shrink;
+                    }
+                    // from (block, tokens 4 group ...) to (group, the tokens that this group's values are of)
+                    half8 ph[NT / 2], pl[NT / 2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if constexpr (FP8) {
+                            swap32(hi[0][i], hi[2][i]);  swap32(hi[1][i], hi[3][i]);
+                            swap16(hi[0][i], hi[1][i]);  swap16(hi[2][i], hi[3][i]);
+                            swap32(lo[0][i], lo[2][i]);  swap32(lo[1][i], lo[3][i]);
+                            swap16(lo[0][i], lo[1][i]);  swap16(lo[2][i], lo[3][i]);
+                        } else {
+                            swap32(hi[0][i], hi[1][i]);  swap16(hi[0][i], hi[1][i]);
+                            swap32(lo[0][i], lo[1][i]);  swap16(lo[0][i], lo[1][i]);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < NT / 2; ++k) {
+                        ph[k] = __builtin_bit_cast(half8, u32x4{hi[2 * k][0], hi[2 * k][1], hi[2 * k + 1][0], hi[2 * k + 1][1]});
+                        pl[k] = __builtin_bit_cast(half8, u32x4{lo[2 * k][0], lo[2 * k][1], lo[2 * k + 1][0], lo[2 * k + 1][1]});
+                    }
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        if constexpr (FP8) {
+                            half8 va, vb;
+                            widen(vv[d], va, vb);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, ph[1], acc[r][d], 0, 0, 0);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, pl[1], acc[r][d], 0, 0, 0);
+                        } else {
+                            const half8 va = __builtin_bit_cast(half8, vv[d]);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+        bool bad = false;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) bad |= not_finite(acc[r][d]);
+        if (clean || !__builtin_amdgcn_ballot_w64(bad)) break;
+        clean = true;
+    }
+    if (clean) {
+        for (int kind = kPlusInf; kind <= kNaN; ++kind) {
+            floatx4 count[RT][DB];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) count[r][d] = floatx4{0, 0, 0, 0};
+            for (int base = v0; base < v1; base += 64 * 4) {
+                const int page = pages_from(base);
+                for (int j = 0; j < 64 / NT; ++j) {
+                    const int v = base + NT * (4 * j + wave);
+                    if (v >= v1) break;
+                    const int k = FP8 ? group : group >> 1;
+                    const bool there = v + k < v1;
+                    const int block = w.block(min(v + k, v1 - 1)), pg = __shfl(page, NT * j + k);
+                    const bool valid = there && (uint32_t)pg < (uint32_t)p.pages;
+                    const int t = valid ? block * 16 + mine_first : 0x7ffffff0;
+                    const uint8_t *mine = p.v + offset(block, pg, valid) + mine_in_block;
+                    half8 seen[RT][NT / 2];
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4 * NT; ++i) seen[r][i >> 3][i & 7] = sees(t + i, pos[r], low[r], p.sinks) ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const u32x4 vv = *reinterpret_cast<const u32x4 *>(mine + d * 256);
+                        half8 part_of[NT / 2];
+                        if constexpr (FP8) widen(vv, part_of[0], part_of[1]);
+                        else part_of[0] = __builtin_bit_cast(half8, vv);
+#pragma unroll
+                        for (int i = 0; i < NT / 2; ++i)
+#pragma unroll
+                            for (int r = 0; r < RT; ++r)
+                                count[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(of_kind(part_of[i], kind), seen[r][i], count[r][d], 0, 0, 0);
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (count[r][d][i] > 0.0f) acc[r][d][i] += of_kind_value(kind);
+        }
+    }
+
+    // the four waves' sums: waves 2 and 3 hand theirs to 0 and 1, then 1 to 0
+    float mine_top[RT], all_top[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        total[r] = sum_of_groups(total[r]);
+        mine_top[r] = top[r];
+        if (group == 0) {
+            stat[wave][0][16 * r + col] = top[r];
+            stat[wave][1][16 * r + col] = total[r];
+        }
+    }
+    __syncthreads();
+    float sum[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        float m = kNegInf;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][16 * r + col]);
+        all_top[r] = m;
+        const float ref = fmaxf(m, -1e30f);
+        sum[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[r] += stat[i][1][16 * r + col] * __builtin_amdgcn_exp2f(fmaxf(stat[i][0][16 * r + col], -1e30f) - ref);
+        const float f = __builtin_amdgcn_exp2f(fmaxf(mine_top[r], -1e30f) - ref);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[r][d] *= f;
+    }
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) *reinterpret_cast<floatx4 *>(&part[wave - half][16 * r + col][16 * d + 4 * group]) = acc[r][d];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[r][d] += *reinterpret_cast<const floatx4 *>(&part[wave][16 * r + col][16 * d + 4 * group]);
+        __syncthreads();
+    }
+    const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
+    if (chunks == 1) {
+        if (wave == 0)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (row[r] > row1) continue;
+                const int i = row[r] / p.group, g = row[r] - i * p.group;
+                uint16_t *dst = p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + 4 * group;
+                const float f = pos[r] < 0 ? 0.0f : v_scale / sum[r];       // a row that sees nothing is zero
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    *reinterpret_cast<u32x2 *>(dst + 16 * d) = pos[r] < 0 ? u32x2{0u, 0u} :
+                        u32x2{float2_to_half2_bits(acc[r][d][0] * f, acc[r][d][1] * f), float2_to_half2_bits(acc[r][d][2] * f, acc[r][d][3] * f)};
+            }
+        return;
+    }
+    // [tile][chunk][row]: D sums, then the maximum and the sum of the row's probabilities
+    const int stride = D + 2;
+    const int64_t slot = ((int64_t)tile * p.chunks + chunk) * p.part_rows;
+    if (wave == 0) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if (row[r] > row1) continue;
+            float *dst = p.partials + (slot + 16 * r + col) * stride;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2)
+                    __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + 16 * d + 4 * group + i),
+                                       (unsigned long long)__float_as_uint(acc[r][d][i]) | (unsigned long long)__float_as_uint(acc[r][d][i + 1]) << 32,
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (group == 0)
+                __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + D),
+                                   (unsigned long long)__float_as_uint(all_top[r]) | (unsigned long long)__float_as_uint(sum[r]) << 32,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        // the partials are past the caches before the ticket is drawn
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (lane == 0) {
+            const uint32_t ticket = __hip_atomic_fetch_add(p.counters + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = ticket == (uint32_t)chunks - 1;
+            if (last) __hip_atomic_store(p.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    // the last workgroup: the chunks in order, two columns per lane
+    const int count = row1 - row0 + 1;
+    for (int item = threadIdx.x; item < count * (D / 2); item += 256) {
+        const int r = item / (D / 2), d = 2 * (item - r * (D / 2));
+        float m = kNegInf, l = 0.0f, a0 = 0.0f, a1 = 0.0f;
+        for (int c = 0; c < chunks; ++c) {
+            const float *src = p.partials + (((int64_t)tile * p.chunks + c) * p.part_rows + r) * stride;
+            const unsigned long long ml = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + D), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const unsigned long long o = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + d), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const float mc = __uint_as_float((uint32_t)ml), lc = __uint_as_float((uint32_t)(ml >> 32));
+            const float next = fmaxf(m, mc), ref = fmaxf(next, -1e30f);
+            const float f = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(mc, -1e30f) - ref);
+            l = l * f + lc * g;
+            a0 = a0 * f + __uint_as_float((uint32_t)o) * g;
+            a1 = a1 * f + __uint_as_float((uint32_t)(o >> 32)) * g;
+            m = next;
+        }
+        const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
+        const float f = v_scale / l;
+        *reinterpret_cast<uint32_t *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) =
+            past + i < 0 ? 0u : float2_to_half2_bits(a0 * f, a1 * f);
+    }
+}
+
+// ---- launch shapes ----------------------------------------------------------------------------------------------------------
+
+AttentionPlan attention_plan(const AttentionShape &s) {
+    AttentionPlan a;
+    const int64_t rows = (int64_t)s.max_new * s.group;
+    a.rt = rows <= 16 || s.D > 128 ? 1 : 2;            // (two tiles of 256 dims do not fit the registers)
+    a.row_tiles = (rows + 16 * a.rt - 1) / (16 * a.rt);
+    a.part_rows = rows < 16 * a.rt ? rows : 16 * a.rt;
+    const int64_t tiles = s.batch * s.kv_heads * a.row_tiles;
+    // blocks that a tile of rows sees at most
+    int64_t blocks = (s.max_len + 15) / 16;
+    if (s.window > 0) {
+        const int64_t near = (s.window + 16 * a.rt / s.group + 17) / 16 + 1 + (s.sinks + 15) / 16;
+        if (near < blocks) blocks = near;
+    }
+    if (blocks < 1) blocks = 1;
+    const int64_t least = s.fp8 ? 16 : 8;              // one step of each wave
+    int64_t chunk = (blocks * tiles + 1535) / 1536;
+    if (tuning().attn_chunk > 0) chunk = tuning().attn_chunk / 16;
+    if (chunk < least) chunk = least;
+    chunk = (chunk + least - 1) / least * least;
+    if (tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
+    a.chunk_blocks = chunk;
+    a.chunks = (blocks + chunk - 1) / chunk;
+    a.tiles = tiles;
+    a.partial_bytes = a.chunks > 1 ? (size_t)tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
+    return a;
+}
+
+template <int D, bool FP8>
+static void launch_stream(int64_t rt, const AttentionArgs &a, dim3 grid, hipStream_t stream) {
+    if constexpr (D <= 128) {
+        if (rt == 2) {
+            attention_stream_kernel<D, FP8, 2><<<grid, 256, 0, stream>>>(a);
+            return;
+        }
+    }
+    attention_stream_kernel<D, FP8, 1><<<grid, 256, 0, stream>>>(a);
+}
+
+int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream) {
+    a.row_tiles = (int)plan.row_tiles;
+    a.part_rows = (int)plan.part_rows;
+    a.chunk_blocks = (int)plan.chunk_blocks;
+    a.chunks = (int)plan.chunks;
+    const int64_t groups = plan.tiles * plan.chunks;
+    if (groups > 0x7fffffff) return kErrShape;
+    const dim3 grid((unsigned)groups);
+#define NFP_STREAM(D) (s.fp8 ? launch_stream<D, true>(plan.rt, a, grid, stream) : launch_stream<D, false>(plan.rt, a, grid, stream))
+    switch (s.D) {
+        case 64: NFP_STREAM(64); break;
+        case 96: NFP_STREAM(96); break;
+        case 128: NFP_STREAM(128); break;
+        default: NFP_STREAM(256); break;
+    }
+#undef NFP_STREAM
+    return hip_ok(hipGetLastError());
+}
+
+}  // namespace nfp

@@ -87,6 +87,7 @@ struct Tuning {
     int64_t large_rows;      // 1 / 0: row-major planes reach tiles above 64 tokens through LDS / straight into registers
     int64_t tuned_table;     // 0: the tiled kernels' launch shape always comes from the cost model, never from the table of timed shapes
     int64_t quant_onepass;   // 1 / 0: force / forbid the single-pass activation quantisation (rows kept in registers) where it fits
+    int64_t attn_chunk;      // tokens of the cache per workgroup of the attention kernels, rounded up to what their waves take in a step
 };
 Tuning &tuning();
 uint32_t tuning_epoch();                               // counts the changes of the knobs
@@ -196,6 +197,52 @@ int launch_probe_stream_read(const void *src, size_t bytes, uint32_t *sink, hipS
 int launch_probe_stream_read_sparse(const void *src, size_t bytes, uint32_t *sink, hipStream_t stream);
 int launch_probe_mfma(const void *operands, int fp8, int iters, uint32_t *sink, double *flops_host,
                       hipStream_t stream);
+
+// what stands around the linears of a layer
+struct NormArgs {
+    const uint16_t *X, *R, *weight;
+    uint16_t *sum, *Y;
+    uint8_t *Xq;
+    float *scales;
+    int64_t K, ldx, ldr, lds, ldy;
+    float eps;
+};
+int launch_add_rms_norm(const NormArgs &a, int64_t M, hipStream_t stream);
+
+struct AppendArgs {
+    const uint16_t *q, *new_k, *new_v;
+    int64_t ldq, ldk, ldv, M;
+    const float *cos, *sin;
+    const int32_t *positions, *slots;
+    uint16_t *out;
+    int64_t ldo;
+    uint8_t *k, *v;
+    const float *k_scale, *v_scale;
+    int32_t heads, kv_heads, D, rotary, positions_known, slot_count;
+    int32_t page_shift;                                // a page has 16 << page_shift tokens
+    int32_t group;                                     // tokens per workgroup
+    bool fp8;
+};
+int launch_rope_append(AppendArgs a, hipStream_t stream);
+
+struct AttentionArgs {
+    const uint16_t *Q;
+    int64_t ldq, ldo, ld_table;
+    uint16_t *O;
+    const uint8_t *k, *v;
+    const float *k_scale, *v_scale;
+    const int32_t *table, *lens, *starts;
+    float *partials;
+    uint32_t *counters;
+    float scale;
+    int32_t tokens, batch, per, max_new, columns;      // per: new tokens of every sequence where there are no starts
+    int32_t kv_heads, group, pages, page_shift, window, sinks;
+    int32_t row_tiles, part_rows, chunk_blocks, chunks;
+};
+struct AttentionShape { int64_t batch, kv_heads, group, D, max_new, max_len, window, sinks;  bool fp8; };
+struct AttentionPlan { int64_t rt, row_tiles, part_rows, chunk_blocks, chunks, tiles;  size_t partial_bytes; };
+AttentionPlan attention_plan(const AttentionShape &s);
+int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream);
 
 bool use_small_gemm(int64_t M);
 bool route_small(int kind, int64_t M, int64_t N, int64_t K, int64_t ldw);     // which of the two families a problem runs on
