@@ -142,6 +142,44 @@ __device__ __forceinline__ Walk walk(const AttentionArgs &p, int low_pos, int hi
     w.blocks = w.sink_blocks + high_block - w.low_block;
     return w;
 }
+// ---- sequences split over workgroups -----------------------------------------------------------------------------------------
+// A workgroup's sums lie in the workspace as [tile][chunk][row]: D sums, then the maximum and the sum of the row's
+// probabilities.  They are stored past the caches (every XCD has an L2 of its own) before the tile's ticket is drawn;
+// the workgroup with the last ticket joins the chunks in their order and leaves the counter cleared.  Nobody waits for anybody.
+__device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunks, const Sequence &sq, int row0, int row1, int past, int head,
+                                     int D, int threads, float v_scale, int *last) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t ticket = __hip_atomic_fetch_add(p.counters + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *last = ticket == (uint32_t)chunks - 1;
+        if (*last) __hip_atomic_store(p.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!*last) return;
+    const int count = row1 - row0 + 1, stride = D + 2;
+    for (int item = threadIdx.x; item < count * (D / 2); item += threads) {
+        const int r = item / (D / 2), d = 2 * (item - r * (D / 2));
+        float m = kNegInf, l = 0.0f, a0 = 0.0f, a1 = 0.0f;
+        for (int c = 0; c < chunks; ++c) {
+            const float *src = p.partials + (((int64_t)tile * p.chunks + c) * p.part_rows + r) * stride;
+            const unsigned long long ml = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + D), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const unsigned long long o = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + d), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const float mc = __uint_as_float((uint32_t)ml), lc = __uint_as_float((uint32_t)(ml >> 32));
+            const float next = fmaxf(m, mc), ref = fmaxf(next, -1e30f);
+            const float f = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(mc, -1e30f) - ref);
+            l = l * f + lc * g;
+            a0 = a0 * f + __uint_as_float((uint32_t)o) * g;
+            a1 = a1 * f + __uint_as_float((uint32_t)(o >> 32)) * g;
+            m = next;
+        }
+        const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
+        const float f = v_scale / l;
+        *reinterpret_cast<uint32_t *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) =
+            past + i < 0 ? 0u : float2_to_half2_bits(a0 * f, a1 * f);
+    }
+}
+
 // ---- streaming kernel -------------------------------------------------------------------------------------------------------
 // For few rows: bound by the bytes of the cache.  A workgroup of four waves takes 16 * RT rows and a stretch of the
 // sequence's blocks; a wave loads keys and values of 32 tokens (64 in E4M3) straight into registers, in operand order, every
@@ -168,7 +206,7 @@ attention_stream_kernel(AttentionArgs p) {
     const int rt0 = tile % p.row_tiles, head = tile / p.row_tiles % p.kv_heads, b = tile / p.row_tiles / p.kv_heads;
     const Sequence sq = sequence(p, b);
     const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
-    if (row0 >= rows) return;
+    if (row0 >= rows || (p.few > 0 && rows > p.few)) return;     // (the tile kernel's)
     const int row1 = min(rows, row0 + 16 * RT) - 1;
     const int past = sq.length - sq.fresh;
     const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
@@ -477,7 +515,6 @@ attention_stream_kernel(AttentionArgs p) {
             }
         return;
     }
-    // [tile][chunk][row]: D sums, then the maximum and the sum of the row's probabilities
     const int stride = D + 2;
     const int64_t slot = ((int64_t)tile * p.chunks + chunk) * p.part_rows;
     if (wave == 0) {
@@ -497,67 +534,448 @@ attention_stream_kernel(AttentionArgs p) {
                                    (unsigned long long)__float_as_uint(all_top[r]) | (unsigned long long)__float_as_uint(sum[r]) << 32,
                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        // the partials are past the caches before the ticket is drawn
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (lane == 0) {
-            const uint32_t ticket = __hip_atomic_fetch_add(p.counters + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last = ticket == (uint32_t)chunks - 1;
-            if (last) __hip_atomic_store(p.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    join(p, tile, chunks, sq, row0, row1, past, head, D, 256, v_scale, &last);
+}
+
+// ---- tile kernel --------------------------------------------------------------------------------------------------------------
+// For many rows: bound by the matrix pipe and the exponentials.  A workgroup of NW waves takes 32 * NW rows, a wave 32 of them; keys and
+// values of TK tokens at a time go through two buffers of LDS, which all waves read, in the storage's own order: a wave's operand reads
+// are contiguous, nothing is transposed.  E4M3 codes become FP16 on their way into LDS, once for all rows.
+// A row's probabilities are taken relative to a maximum that follows the true one only when that is 2^kLag larger, so that
+// the sums are rarely rescaled; P is rounded to FP16 and its sum is that of the rounded values.
+constexpr float kLag = 8.0f;
+constexpr float kTileShift = 4.0f;                     // probabilities up to 2^(kLag + kTileShift)
+
+template <int D, bool FP8, int NW, int TK>
+__global__ void __launch_bounds__(64 * NW)
+attention_tile_kernel(AttentionArgs p) {
+    constexpr int T = 64 * NW, NB = TK / 16, HB = TK / 32;       // threads, blocks and halves (of 32 tokens) of a tile of tokens
+    constexpr int CB = FP8 ? D : 2 * D;                          // 16-byte chunks of a block in memory
+    constexpr int CHUNKS = NB * CB, PER = (CHUNKS + T - 1) / T;  // of a tile, and per lane
+    constexpr int KS = D / 16, DB = D / 32;
+    extern __shared__ u32x4 lds[];                               // [2][keys, values][NB][2 D] chunks of FP16
+    constexpr int HALF = NB * 2 * D, BUFFER = 2 * HALF;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    // rows of late tokens, which see most, first; the heads of a sequence on different XCDs
+    const int tiles = p.batch * p.kv_heads * p.row_tiles;
+    const int chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
+    const int head = tile % p.kv_heads, b = tile / p.kv_heads % p.batch, from_last = tile / p.kv_heads / p.batch;
+    const Sequence sq = sequence(p, b);
+    const int rows = sq.fresh * p.group;
+    if (rows <= p.few) return;                                   // (the streaming kernel's)
+    const int row_tiles = (rows + 32 * NW - 1) / (32 * NW);
+    if (from_last >= row_tiles) return;
+    const int row0 = (row_tiles - 1 - from_last) * 32 * NW, row1 = min(rows, row0 + 32 * NW) - 1;
+    const int past = sq.length - sq.fresh;
+    const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
+    const Walk w = walk(p, low_pos, high_pos);
+    const int chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+    if (chunk >= chunks) return;
+    const int v0 = chunk * p.chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
+    const int steps = (v1 - v0 + NB - 1) / NB;
+    const int first_low = before(p, low_pos);
+
+    // this wave's rows
+    const int wave_row0 = row0 + 32 * wave, row = wave_row0 + col;
+    const bool idle = wave_row0 > row1;
+    const int clamped = min(row, row1), token = clamped / p.group, g = clamped - token * p.group;
+    const int pos = past + token, low = before(p, pos);
+    const int wave_low = past + min(wave_row0, row1) / p.group, wave_high = past + min(wave_row0 + 31, row1) / p.group;
+    const int wave_first_low = before(p, wave_low), wave_last_low = before(p, wave_high);
+    half8 q[KS];
+    {
+        const uint16_t *src = p.Q + (int64_t)(sq.first + token) * p.ldq + (int64_t)(head * p.group + g) * D + 8 * h;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const half8 *>(src + 16 * s);
+    }
+    const float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
+    const int in_page = (1 << p.page_shift) - 1;
+    // the row of S^T that this lane's operand of K holds is one of these tokens of a half: with it the lane's scores are those of the 8
+    // tokens that its operand of V holds (8 h ... of each block)
+    const int k_token = 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+    const int k_chunk = (col >> 4) * 2 * D + h * 16 + k_token, v_chunk = h * D + col;
+
+    int page = 0, page_base = v0 - 64;                           // pages of the 64 blocks from page_base, a lane each
+    u32x4 kreg[PER], vreg[PER];
+
+    // where a block of the walk lies: -1 if it is not in the cache (blocks behind the last one: some block's place)
+    const auto offset_of = [&](int v) -> int64_t {
+        v = min(v, v1 - 1);
+        const int pg = __builtin_amdgcn_readlane(page, v - page_base);
+        const int64_t at = ((((int64_t)pg * p.kv_heads + head) << p.page_shift) + (w.block(v) & in_page)) * (CB * 16);
+        return (uint32_t)pg < (uint32_t)p.pages ? at : -1;
+    };
+    uint32_t gone = 0;                                           // blocks of the tile last loaded that are not in the cache
+    const auto load = [&](int step) {
+        const int v = v0 + step * NB;
+        if (v >= page_base + 64) {
+            page_base = v;
+            page = v + lane < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v + lane) >> p.page_shift)] : 0;
         }
+        int64_t at[NB];
+        gone = 0;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+            at[k] = offset_of(v + k);
+            gone |= at[k] < 0 ? 1u << k : 0u;
+            at[k] = max(at[k], (int64_t)0);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int id = threadIdx.x + i * T;
+            if (CHUNKS % T != 0 && id >= CHUNKS) break;
+            const int block = id / CB;
+            int64_t from = at[0];
+#pragma unroll
+            for (int k = 1; k < NB; ++k) from = block == k ? at[k] : from;
+            from += (id - block * CB) * 16;
+            kreg[i] = *reinterpret_cast<const u32x4 *>(p.k + from);
+            vreg[i] = *reinterpret_cast<const u32x4 *>(p.v + from);
+        }
+    };
+    const auto first_token = [&](int v) { return v < v1 ? w.block(v) * 16 : 0x7ffffff0; };     // (nothing sees those)
+    const auto store = [&](int step, int buffer) {
+        const int v = v0 + step * NB;
+        bool plain = true;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+            const int t = first_token(v + k);
+            plain &= t + 15 <= high_pos && (t > first_low || t + 15 < p.sinks);
+        }
+        u32x4 *keys = lds + buffer * BUFFER, *values = keys + HALF;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int id = threadIdx.x + i * T;
+            if (CHUNKS % T != 0 && id >= CHUNKS) break;
+            const int block = id / CB, place = id - block * CB;
+            u32x4 vv = vreg[i];
+            if (!plain) {
+                // values that no row sees may be anything: memory that was never written, another sequence's
+                const int t = first_token(v + block) + (FP8 ? 0 : 8 * (place / D));
+                uint32_t keep[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < (FP8 ? 16 : 8); ++j)
+                    if (sees(t + j, high_pos, first_low, p.sinks)) keep[FP8 ? j >> 2 : j >> 1] |= FP8 ? 0xffu << (8 * (j & 3)) : 0xffffu << (16 * (j & 1));
+                vv &= u32x4{keep[0], keep[1], keep[2], keep[3]};
+            }
+            if constexpr (FP8) {
+                half8 lo, hi;
+                widen(kreg[i], lo, hi);
+                const int k_at = block * 2 * D + (place >> 4) * 32 + (place & 15), v_at = block * 2 * D + place;
+                keys[k_at] = __builtin_bit_cast(u32x4, lo);
+                keys[k_at + 16] = __builtin_bit_cast(u32x4, hi);
+                widen(vv, lo, hi);
+                values[v_at] = __builtin_bit_cast(u32x4, lo);
+                values[v_at + D] = __builtin_bit_cast(u32x4, hi);
+            } else {
+                keys[id] = kreg[i];
+                values[id] = vv;
+            }
+        }
+    };
+
+    floatx16 acc[DB];
+    float top, total;
+    top = kNegInf;
+    total = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+    uint32_t gone_now = 0, gone_next = 0;
+    if (steps > 0) {
+        load(0);
+        gone_now = gone;
+        store(0, 0);
+        if (steps > 1) load(1);
+        gone_next = gone;
     }
     __syncthreads();
-    if (!last) return;
-    // the last workgroup: the chunks in order, two columns per lane
-    const int count = row1 - row0 + 1;
-    for (int item = threadIdx.x; item < count * (D / 2); item += 256) {
-        const int r = item / (D / 2), d = 2 * (item - r * (D / 2));
-        float m = kNegInf, l = 0.0f, a0 = 0.0f, a1 = 0.0f;
-        for (int c = 0; c < chunks; ++c) {
-            const float *src = p.partials + (((int64_t)tile * p.chunks + c) * p.part_rows + r) * stride;
-            const unsigned long long ml = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + D), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const unsigned long long o = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + d), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const float mc = __uint_as_float((uint32_t)ml), lc = __uint_as_float((uint32_t)(ml >> 32));
-            const float next = fmaxf(m, mc), ref = fmaxf(next, -1e30f);
-            const float f = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(mc, -1e30f) - ref);
-            l = l * f + lc * g;
-            a0 = a0 * f + __uint_as_float((uint32_t)o) * g;
-            a1 = a1 * f + __uint_as_float((uint32_t)(o >> 32)) * g;
-            m = next;
+    for (int step = 0; step < steps; ++step) {
+        const u32x4 *keys = lds + (step & 1) * BUFFER, *values = keys + HALF;
+        const int v = v0 + step * NB;
+        int t0[NB];
+        bool plain = gone_now == 0, any = false;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+            t0[k] = first_token(v + k);
+            plain &= t0[k] + 15 <= wave_low && (t0[k] > wave_last_low || t0[k] + 15 < p.sinks);
+            any |= t0[k] <= wave_high && (t0[k] + 15 > wave_first_low || t0[k] < p.sinks);
         }
-        const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
-        const float f = v_scale / l;
-        *reinterpret_cast<uint32_t *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) =
-            past + i < 0 ? 0u : float2_to_half2_bits(a0 * f, a1 * f);
+        const bool work = any && !idle;
+        floatx16 s[HB];
+        if (work) {
+#pragma unroll
+            for (int t = 0; t < HB; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, keys[t * 4 * D + k * 32 + k_chunk]), q[k], s[t], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < steps) store(step + 1, (step + 1) & 1);
+        if (step + 2 < steps) load(step + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (work) {
+            if (!plain) {
+#pragma unroll
+                for (int t = 0; t < HB; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
+                        if (gone_now >> (2 * t + (i >> 3)) & 1) s[t][i] = __builtin_nanf("");
+                        // (before the scale: its sign must not matter)
+                        s[t][i] *= scale;
+                        if (!sees(t0[2 * t + (i >> 3)] + 8 * h + (i & 7), pos, low, p.sinks)) s[t][i] = kNegInf;
+                    }
+            } else {
+#pragma unroll
+                for (int t = 0; t < HB; ++t) s[t] *= scale;
+            }
+            float m = kNegInf;
+#pragma unroll
+            for (int t = 0; t < HB; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) m = fmaxf(fmaxf(m, s[t][i]), s[t][i + 1]);
+            {
+                uint32_t x = __float_as_uint(m), y = x;
+                swap32(x, y);
+                m = fmaxf(__uint_as_float(x), __uint_as_float(y));
+            }
+            // (also where the first score is seen: top is -Inf until then)
+            if (__builtin_amdgcn_ballot_w64(m > top + kLag)) {
+                const float next = fmaxf(top, m);
+                const float shrink = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - fmaxf(next, -1e30f));
+                top = next;
+                total *= shrink;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[d] *= shrink;
+            }
+            const float from = fmaxf(top, -1e30f) - kTileShift;
+            half8 pr[2 * HB];
+#pragma unroll
+            for (int t = 0; t < HB; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pr[2 * t + (i >> 3)][i & 7] = (_Float16)__builtin_amdgcn_exp2f(s[t][i] - from);
+            typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+            const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+            for (int k = 0; k < 2 * HB; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) total = __builtin_amdgcn_fdot2(half2v{pr[k][i], pr[k][i + 1]}, ones, total, false);
+#pragma unroll
+            for (int k = 0; k < 2 * HB; ++k) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, values[k * 2 * D + d * 32 + v_chunk]), pr[k], acc[d], 0, 0, 0);
+            }
+        }
+        gone_now = gone_next;
+        gone_next = gone;
+        __syncthreads();
     }
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) bad |= not_finite(floatx4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]});
+    if (__builtin_amdgcn_ballot_w64(bad && !idle)) {
+        // this wave's rows again, straight from memory and by itself: first without the values that are not finite ...
+        const auto refresh = [&](int v) {
+            if (((v - v0) & 63) == 0) {
+                page_base = v;
+                page = v + lane < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v + lane) >> p.page_shift)] : 0;
+            }
+        };
+        const auto values_of = [&](int64_t at, int d) {
+            if constexpr (FP8) {
+                half8 lo, hi;
+                widen(*reinterpret_cast<const u32x4 *>(p.v + at + (d * 32 + col) * 16), lo, hi);
+                return h ? hi : lo;
+            } else {
+                return *reinterpret_cast<const half8 *>(p.v + at + (d * 32 + v_chunk) * 16);
+            }
+        };
+        top = kNegInf;
+        total = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+        for (int v = v0; v < v1; v += 2) {
+            refresh(v);
+            const int64_t first = offset_of(v), second = offset_of(v + 1), mine = (col >> 4) ? second : first;
+            const uint8_t *keys = p.k + max(mine, (int64_t)0);
+            floatx16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                half8 x;
+                if constexpr (FP8) {
+                    half8 lo, hi;
+                    widen(*reinterpret_cast<const u32x4 *>(keys + (k * 16 + k_token) * 16), lo, hi);
+                    x = h ? hi : lo;
+                } else {
+                    x = *reinterpret_cast<const half8 *>(keys + (k * 32 + h * 16 + k_token) * 16);
+                }
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[k], s, 0, 0, 0);
+            }
+            float m = top;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int t = first_token(v + (i >> 3)) + 8 * h + (i & 7);
+                s[i] = (i >> 3 ? second : first) < 0 ? __builtin_nanf("") : s[i] * scale;
+                if (!sees(t, pos, low, p.sinks)) s[i] = kNegInf;
+                m = fmaxf(m, s[i]);
+            }
+            uint32_t x = __float_as_uint(m), y = x;
+            swap32(x, y);
+            m = fmaxf(__uint_as_float(x), __uint_as_float(y));
+            const float shrink = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - fmaxf(m, -1e30f)), from = fmaxf(m, -1e30f) - kTileShift;
+            top = m;
+            total *= shrink;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= shrink;
+            half8 pr[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(s[i] - from);
+                total += e;
+                pr[i >> 3][i & 7] = (_Float16)e;
+            }
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int64_t at = k ? second : first;
+                    const u32x4 vv = only_finite<false>(__builtin_bit_cast(u32x4, values_of(max(at, (int64_t)0), d)));
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vv), pr[k], acc[d], 0, 0, 0);
+                }
+        }
+        // ... then what these add to the rows that do see them
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+#pragma unroll 1
+            for (int kind = kPlusInf; kind <= kNaN; ++kind) {
+                floatx16 count;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) count[i] = 0.0f;
+#pragma unroll 1
+                for (int v = v0; v < v1; ++v) {
+                    refresh(v);
+                    const int64_t at = offset_of(v);
+                    if (at < 0) continue;
+                    const int t = w.block(v) * 16 + 8 * h;
+                    half8 seen;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) seen[i] = sees(t + i, pos, low, p.sinks) ? (_Float16)1.0f : (_Float16)0.0f;
+                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_kind(values_of(at, d), kind), seen, count, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (count[i] > 0.0f) acc[d][i] += of_kind_value(kind);
+            }
+        }
+    }
+    {
+        uint32_t x = __float_as_uint(total), y = x;
+        swap32(x, y);
+        total = __uint_as_float(x) + __uint_as_float(y);
+    }
+    const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
+    if (chunks == 1) {
+        if (row > row1) return;
+        uint16_t *dst = p.O + (int64_t)(sq.first + token) * p.ldo + (int64_t)(head * p.group + g) * D + 4 * h;
+        const float f = v_scale / total;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<u32x2 *>(dst + 32 * d + 2 * i) = pos < 0 ? u32x2{0u, 0u} :
+                    u32x2{float2_to_half2_bits(acc[d][i] * f, acc[d][i + 1] * f), float2_to_half2_bits(acc[d][i + 2] * f, acc[d][i + 3] * f)};
+        return;
+    }
+    const int stride = D + 2;
+    if (row <= row1) {
+        float *dst = p.partials + (((int64_t)tile * p.chunks + chunk) * p.part_rows + row - row0) * stride;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+                __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3)),
+                                   (unsigned long long)__float_as_uint(acc[d][i]) | (unsigned long long)__float_as_uint(acc[d][i + 1]) << 32,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (h == 0)
+            __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + D),
+                               (unsigned long long)__float_as_uint(top) | (unsigned long long)__float_as_uint(total) << 32,
+                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    join(p, tile, chunks, sq, row0, row1, past, head, D, T, v_scale, reinterpret_cast<int *>(lds));
 }
 
 // ---- launch shapes ----------------------------------------------------------------------------------------------------------
 
-AttentionPlan attention_plan(const AttentionShape &s) {
-    AttentionPlan a;
-    const int64_t rows = (int64_t)s.max_new * s.group;
-    a.rt = rows <= 16 || s.D > 128 ? 1 : 2;            // (two tiles of 256 dims do not fit the registers)
-    a.row_tiles = (rows + 16 * a.rt - 1) / (16 * a.rt);
-    a.part_rows = rows < 16 * a.rt ? rows : 16 * a.rt;
-    const int64_t tiles = s.batch * s.kv_heads * a.row_tiles;
-    // blocks that a tile of rows sees at most
+// Blocks that a tile of `rows` rows sees at most.
+static int64_t blocks_seen(const AttentionShape &s, int64_t rows) {
     int64_t blocks = (s.max_len + 15) / 16;
     if (s.window > 0) {
-        const int64_t near = (s.window + 16 * a.rt / s.group + 17) / 16 + 1 + (s.sinks + 15) / 16;
+        const int64_t near = (s.window + rows / s.group + 17) / 16 + 1 + (s.sinks + 15) / 16;
         if (near < blocks) blocks = near;
     }
-    if (blocks < 1) blocks = 1;
-    const int64_t least = s.fp8 ? 16 : 8;              // one step of each wave
-    int64_t chunk = (blocks * tiles + 1535) / 1536;
+    return blocks < 1 ? 1 : blocks;
+}
+
+static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t rows, int64_t tile_rows, int64_t least, int64_t wanted) {
+    a.row_tiles = (rows + tile_rows - 1) / tile_rows;
+    a.part_rows = rows < tile_rows ? rows : tile_rows;
+    a.tiles = s.batch * s.kv_heads * a.row_tiles;
+    const int64_t blocks = blocks_seen(s, tile_rows);
+    int64_t chunk = (blocks * a.tiles + wanted - 1) / wanted;
     if (tuning().attn_chunk > 0) chunk = tuning().attn_chunk / 16;
     if (chunk < least) chunk = least;
     chunk = (chunk + least - 1) / least * least;
-    if (tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
+    if (a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
     a.chunk_blocks = chunk;
     a.chunks = (blocks + chunk - 1) / chunk;
-    a.tiles = tiles;
-    a.partial_bytes = a.chunks > 1 ? (size_t)tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
+    a.partial_bytes = a.chunks > 1 ? (size_t)a.tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
+}
+
+AttentionPlan attention_plan(const AttentionShape &s) {
+    AttentionPlan a;
+    const int64_t rows = s.max_new * s.group, stream_rows = s.D > 128 ? 16 : 32;      // (two tiles of 256 dims do not fit the registers)
+    a.few = 0;
+    a.stream.tiles = a.tile.tiles = 0;
+    a.stream.partial_bytes = a.tile.partial_bytes = 0;
+    const bool many = s.D <= 128 && (tuning().attn_tiles >= 0 ? tuning().attn_tiles > 0 : rows > stream_rows);
+    if (many) {
+        // sequences of few rows beside the others: none if all have as many new tokens
+        a.few = s.ragged && rows > stream_rows && s.group <= stream_rows ? stream_rows : 0;
+        plan_launch(a.tile, s, rows, 256, 16, 512);
+    }
+    if (!many || a.few > 0) {
+        const int64_t most = many ? a.few / s.group * s.group : rows;
+        a.rt = most <= 16 || s.D > 128 ? 1 : 2;
+        plan_launch(a.stream, s, most, 16 * a.rt, s.fp8 ? 16 : 8, 1536);
+    }
+    a.partial_bytes = a.stream.partial_bytes > a.tile.partial_bytes ? a.stream.partial_bytes : a.tile.partial_bytes;
     return a;
+}
+
+static bool shape_of(const AttentionLaunch &l, AttentionArgs &a, dim3 &grid) {
+    const int64_t groups = l.tiles * l.chunks;
+    if (groups > 0x7fffffff) return false;
+    a.row_tiles = (int)l.row_tiles;
+    a.part_rows = (int)l.part_rows;
+    a.chunk_blocks = (int)l.chunk_blocks;
+    a.chunks = (int)l.chunks;
+    grid = dim3((unsigned)groups);
+    return true;
 }
 
 template <int D, bool FP8>
@@ -571,23 +989,44 @@ static void launch_stream(int64_t rt, const AttentionArgs &a, dim3 grid, hipStre
     attention_stream_kernel<D, FP8, 1><<<grid, 256, 0, stream>>>(a);
 }
 
-int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream) {
-    a.row_tiles = (int)plan.row_tiles;
-    a.part_rows = (int)plan.part_rows;
-    a.chunk_blocks = (int)plan.chunk_blocks;
-    a.chunks = (int)plan.chunks;
-    const int64_t groups = plan.tiles * plan.chunks;
-    if (groups > 0x7fffffff) return kErrShape;
-    const dim3 grid((unsigned)groups);
-#define NFP_STREAM(D) (s.fp8 ? launch_stream<D, true>(plan.rt, a, grid, stream) : launch_stream<D, false>(plan.rt, a, grid, stream))
-    switch (s.D) {
-        case 64: NFP_STREAM(64); break;
-        case 96: NFP_STREAM(96); break;
-        case 128: NFP_STREAM(128); break;
-        default: NFP_STREAM(256); break;
+template <int D, bool FP8>
+static int launch_tile(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
+    if constexpr (D <= 128) {
+        constexpr int NW = 8, TK = 64, LDS = 8 * TK * D;             // two buffers of keys and values in FP16
+        static_assert(LDS <= 65536, "");
+        attention_tile_kernel<D, FP8, NW, TK><<<grid, 64 * NW, LDS, stream>>>(a);
+        return hip_ok(hipGetLastError());
     }
+    return kErrShape;
+}
+
+int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream) {
+    dim3 grid;
+    a.few = (int)plan.few;
+    int st = kOk;
+#define NFP_FOR_D(CALL)                                                     \
+    switch (s.D) {                                                          \
+        case 64: if (s.fp8) { CALL(64, true); } else { CALL(64, false); } break;    \
+        case 96: if (s.fp8) { CALL(96, true); } else { CALL(96, false); } break;    \
+        case 128: if (s.fp8) { CALL(128, true); } else { CALL(128, false); } break; \
+        default: if (s.fp8) { CALL(256, true); } else { CALL(256, false); } break;  \
+    }
+    if (plan.tile.tiles > 0) {
+        if (!shape_of(plan.tile, a, grid)) return kErrShape;
+#define NFP_TILE(D, FP8) st = launch_tile<D, FP8>(a, grid, stream)
+        NFP_FOR_D(NFP_TILE)
+#undef NFP_TILE
+        if (st != kOk) return st;
+    }
+    if (plan.stream.tiles > 0) {
+        if (!shape_of(plan.stream, a, grid)) return kErrShape;
+#define NFP_STREAM(D, FP8) launch_stream<D, FP8>(plan.rt, a, grid, stream)
+        NFP_FOR_D(NFP_STREAM)
 #undef NFP_STREAM
-    return hip_ok(hipGetLastError());
+        st = hip_ok(hipGetLastError());
+    }
+#undef NFP_FOR_D
+    return st;
 }
 
 }  // namespace nfp

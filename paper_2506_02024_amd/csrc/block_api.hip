@@ -58,6 +58,7 @@ static int attention_shape(int64_t tokens, int64_t batch, int64_t heads, const n
     s.window = window < 0x7fffffff ? window : 0;
     s.sinks = sinks < 0x7ffffff0 ? sinks : 0x7ffffff0;
     s.fp8 = c->type == NESTEDFP_CACHE_E4M3;
+    s.ragged = tokens != batch * s.max_new;                          // (else every sequence has max_new)
     return kOk;
 }
 
