@@ -547,6 +547,22 @@ attention_stream_kernel(AttentionArgs p) {
 constexpr float kLag = 8.0f;
 constexpr float kTileShift = 4.0f;                     // probabilities up to 2^(kLag + kTileShift)
 
+// v *= f where any bit of `mask` is set.  The branch is inside the statement: around a product in C++ the compiler keeps the sums in
+// two sets of registers and copies one to the other in every step, 64 moves and 64 registers at 128 dims.  (The values come from
+// matrix instructions that `f` depends on having ended; the waits are for `f`, an exponential, and for those that read the values next.)
+__device__ __forceinline__ void scale_if(uint64_t mask, float f, floatx16 &v) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+        float a = v[i], b = v[i + 1], c = v[i + 2], d = v[i + 3], e = v[i + 4], g = v[i + 5], h = v[i + 6], j = v[i + 7];
+        asm("s_cmp_eq_u64 %9, 0\n\ts_cbranch_scc1 .Lscaled%=\n\ts_nop 1\n\t"
+            "v_mul_f32 %0, %8, %0\n\tv_mul_f32 %1, %8, %1\n\tv_mul_f32 %2, %8, %2\n\tv_mul_f32 %3, %8, %3\n\t"
+            "v_mul_f32 %4, %8, %4\n\tv_mul_f32 %5, %8, %5\n\tv_mul_f32 %6, %8, %6\n\tv_mul_f32 %7, %8, %7\n\ts_nop 1\n"
+            ".Lscaled%=:"
+            : "+v"(a), "+v"(b), "+v"(c), "+v"(d), "+v"(e), "+v"(g), "+v"(h), "+v"(j) : "v"(f), "s"(mask) : "scc");
+        v[i] = a;  v[i + 1] = b;  v[i + 2] = c;  v[i + 3] = d;  v[i + 4] = e;  v[i + 5] = g;  v[i + 6] = h;  v[i + 7] = j;
+    }
+}
+
 template <int D, bool FP8, int NW, int TK>
 __global__ void __launch_bounds__(64 * NW)
 attention_tile_kernel(AttentionArgs p) {
@@ -583,14 +599,21 @@ attention_tile_kernel(AttentionArgs p) {
     const int clamped = min(row, row1), token = clamped / p.group, g = clamped - token * p.group;
     const int pos = past + token, low = before(p, pos);
     const int wave_low = past + min(wave_row0, row1) / p.group, wave_high = past + min(wave_row0 + 31, row1) / p.group;
-    const int wave_first_low = before(p, wave_low), wave_last_low = before(p, wave_high);
+    const int wave_last_low = before(p, wave_high);
     half8 q[KS];
     {
         const uint16_t *src = p.Q + (int64_t)(sq.first + token) * p.ldq + (int64_t)(head * p.group + g) * D + 8 * h;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const half8 *>(src + 16 * s);
     }
-    const float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
+    // (a negative scale turns the queries round, so that the largest product has the largest score)
+    float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
+    if (scale < 0.0f) {
+        scale = -scale;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = -q[s];
+    }
+    scale = fmaxf(scale, 1e-30f);                                // (zero: a masked score has to stay -Inf)
     const int in_page = (1 << p.page_shift) - 1;
     // the row of S^T that this lane's operand of K holds is one of these tokens of a half: with it the lane's scores are those of the 8
     // tokens that its operand of V holds (8 h ... of each block)
@@ -607,48 +630,49 @@ attention_tile_kernel(AttentionArgs p) {
         const int64_t at = ((((int64_t)pg * p.kv_heads + head) << p.page_shift) + (w.block(v) & in_page)) * (CB * 16);
         return (uint32_t)pg < (uint32_t)p.pages ? at : -1;
     };
-    uint32_t gone = 0;                                           // blocks of the tile last loaded that are not in the cache
+    // Steps from `from` to `to` see nothing but tokens that the rows from position low to high (and windows from after first to after
+    // last) see whole, one block behind the other.
+    struct Span { int from, to; };
+    const auto whole = [&](int low_pos, int last_low) {
+        const int behind = max(w.sink_blocks, w.sink_blocks + ((last_low + 16) >> 4) - w.low_block);    // the first block of the walk that starts after last_low
+        const int until = min(v1, w.sink_blocks + ((low_pos + 1) >> 4) - w.low_block);                  // blocks before it end by low_pos
+        return Span{max(0, behind - v0 + NB - 1) / NB, until > v0 ? (until - v0) / NB : 0};
+    };
+    const Span staged = whole(high_pos, first_low), plain_steps = whole(wave_low, wave_last_low);
+
+    bool holes = false;                                          // some block so far is not in the cache
     const auto load = [&](int step) {
         const int v = v0 + step * NB;
         if (v >= page_base + 64) {
             page_base = v;
             page = v + lane < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v + lane) >> p.page_shift)] : 0;
-        }
-        int64_t at[NB];
-        gone = 0;
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-            at[k] = offset_of(v + k);
-            gone |= at[k] < 0 ? 1u << k : 0u;
-            at[k] = max(at[k], (int64_t)0);
+            holes |= __builtin_amdgcn_ballot_w64((uint32_t)page >= (uint32_t)p.pages && v + lane < v1) != 0;
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int id = threadIdx.x + i * T;
-            if (CHUNKS % T != 0 && id >= CHUNKS) break;
-            const int block = id / CB;
-            int64_t from = at[0];
-#pragma unroll
-            for (int k = 1; k < NB; ++k) from = block == k ? at[k] : from;
-            from += (id - block * CB) * 16;
-            kreg[i] = *reinterpret_cast<const u32x4 *>(p.k + from);
-            vreg[i] = *reinterpret_cast<const u32x4 *>(p.v + from);
+            const int id = threadIdx.x + i * T, first = (64 * wave + i * T) / CB;
+            if (CHUNKS % T != 0 && 64 * wave + i * T >= CHUNKS) break;
+            int64_t from = max(offset_of(v + first), (int64_t)0);
+            int block = first;
+            if (CB % 64 != 0) {                                  // (64 chunks from two blocks)
+                const int64_t next = max(offset_of(v + first + 1), (int64_t)0);
+                block = id / CB;
+                from = block == first ? from : next;
+            }
+            const uint32_t place = (uint32_t)(id - block * CB) * 16;
+            kreg[i] = *reinterpret_cast<const u32x4 *>(p.k + from + place);
+            vreg[i] = *reinterpret_cast<const u32x4 *>(p.v + from + place);
         }
     };
     const auto first_token = [&](int v) { return v < v1 ? w.block(v) * 16 : 0x7ffffff0; };     // (nothing sees those)
     const auto store = [&](int step, int buffer) {
         const int v = v0 + step * NB;
-        bool plain = true;
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-            const int t = first_token(v + k);
-            plain &= t + 15 <= high_pos && (t > first_low || t + 15 < p.sinks);
-        }
+        const bool plain = step >= staged.from && step < staged.to;
         u32x4 *keys = lds + buffer * BUFFER, *values = keys + HALF;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int id = threadIdx.x + i * T;
-            if (CHUNKS % T != 0 && id >= CHUNKS) break;
+            if (CHUNKS % T != 0 && 64 * wave + i * T >= CHUNKS) break;
             const int block = id / CB, place = id - block * CB;
             u32x4 vv = vreg[i];
             if (!plain) {
@@ -684,99 +708,76 @@ attention_tile_kernel(AttentionArgs p) {
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
-    uint32_t gone_now = 0, gone_next = 0;
     if (steps > 0) {
         load(0);
-        gone_now = gone;
         store(0, 0);
         if (steps > 1) load(1);
-        gone_next = gone;
     }
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
         const u32x4 *keys = lds + (step & 1) * BUFFER, *values = keys + HALF;
-        const int v = v0 + step * NB;
-        int t0[NB];
-        bool plain = gone_now == 0, any = false;
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-            t0[k] = first_token(v + k);
-            plain &= t0[k] + 15 <= wave_low && (t0[k] > wave_last_low || t0[k] + 15 < p.sinks);
-            any |= t0[k] <= wave_high && (t0[k] + 15 > wave_first_low || t0[k] < p.sinks);
-        }
-        const bool work = any && !idle;
         floatx16 s[HB];
-        if (work) {
 #pragma unroll
-            for (int t = 0; t < HB; ++t) {
+        for (int t = 0; t < HB; ++t) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, keys[t * 4 * D + k * 32 + k_chunk]), q[k], s[t], 0, 0, 0);
-            }
+            for (int k = 0; k < KS; ++k)
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, keys[t * 4 * D + k * 32 + k_chunk]), q[k], s[t], 0, 0, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (step + 1 < steps) store(step + 1, (step + 1) & 1);
         if (step + 2 < steps) load(step + 2);
-        __builtin_amdgcn_sched_barrier(0);
-        if (work) {
-            if (!plain) {
+        if (holes || step < plain_steps.from || step >= plain_steps.to) {
+            const int v = v0 + step * NB;
 #pragma unroll
-                for (int t = 0; t < HB; ++t)
+            for (int k = 0; k < NB; ++k) {
+                const int t = first_token(v + k) + 8 * h;
+                bool there = true;
+                if (holes) there = (uint32_t)p.table[(int64_t)b * p.ld_table + (w.block(min(v + k, v1 - 1)) >> p.page_shift)] < (uint32_t)p.pages;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
-                        if (gone_now >> (2 * t + (i >> 3)) & 1) s[t][i] = __builtin_nanf("");
-                        // (before the scale: its sign must not matter)
-                        s[t][i] *= scale;
-                        if (!sees(t0[2 * t + (i >> 3)] + 8 * h + (i & 7), pos, low, p.sinks)) s[t][i] = kNegInf;
-                    }
-            } else {
-#pragma unroll
-                for (int t = 0; t < HB; ++t) s[t] *= scale;
-            }
-            float m = kNegInf;
-#pragma unroll
-            for (int t = 0; t < HB; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) m = fmaxf(fmaxf(m, s[t][i]), s[t][i + 1]);
-            {
-                uint32_t x = __float_as_uint(m), y = x;
-                swap32(x, y);
-                m = fmaxf(__uint_as_float(x), __uint_as_float(y));
-            }
-            // (also where the first score is seen: top is -Inf until then)
-            if (__builtin_amdgcn_ballot_w64(m > top + kLag)) {
-                const float next = fmaxf(top, m);
-                const float shrink = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - fmaxf(next, -1e30f));
-                top = next;
-                total *= shrink;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] *= shrink;
-            }
-            const float from = fmaxf(top, -1e30f) - kTileShift;
-            half8 pr[2 * HB];
-#pragma unroll
-            for (int t = 0; t < HB; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) pr[2 * t + (i >> 3)][i & 7] = (_Float16)__builtin_amdgcn_exp2f(s[t][i] - from);
-            typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-            const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-            for (int k = 0; k < 2 * HB; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) total = __builtin_amdgcn_fdot2(half2v{pr[k][i], pr[k][i + 1]}, ones, total, false);
-#pragma unroll
-            for (int k = 0; k < 2 * HB; ++k) {
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, values[k * 2 * D + d * 32 + v_chunk]), pr[k], acc[d], 0, 0, 0);
+                for (int i = 0; i < 8; ++i) {
+                    // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
+                    const float x = there ? s[k >> 1][8 * (k & 1) + i] : __builtin_nanf("");
+                    s[k >> 1][8 * (k & 1) + i] = sees(t + i, pos, low, p.sinks) ? x : kNegInf;
+                }
             }
         }
-        gone_now = gone_next;
-        gone_next = gone;
+        float m = kNegInf;
+#pragma unroll
+        for (int t = 0; t < HB; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) m = fmaxf(fmaxf(m, s[t][i]), s[t][i + 1]);
+        {
+            uint32_t x = __float_as_uint(m), y = x;
+            swap32(x, y);
+            m = fmaxf(__uint_as_float(x), __uint_as_float(y));
+        }
+        m *= scale;
+        // (also where the first score is seen: top is -Inf until then)
+        const uint64_t behind = __builtin_amdgcn_ballot_w64(m > top + kLag);
+        const float next = behind ? fmaxf(top, m) : top;
+        const float shrink = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - fmaxf(next, -1e30f));
+        top = next;
+        total *= shrink;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) scale_if(behind, shrink, acc[d]);
+        const float from = kTileShift - fmaxf(top, -1e30f);
+        half8 pr[2 * HB];
+#pragma unroll
+        for (int t = 0; t < HB; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pr[2 * t + (i >> 3)][i & 7] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, from));
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+        const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+        for (int k = 0; k < 2 * HB; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) total = __builtin_amdgcn_fdot2(half2v{pr[k][i], pr[k][i + 1]}, ones, total, false);
+#pragma unroll
+        for (int k = 0; k < 2 * HB; ++k)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, values[k * 2 * D + d * 32 + v_chunk]), pr[k], acc[d], 0, 0, 0);
         __syncthreads();
     }
     bool bad = false;
