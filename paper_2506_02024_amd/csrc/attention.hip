@@ -547,6 +547,37 @@ attention_stream_kernel(AttentionArgs p) {
 constexpr float kLag = 8.0f;
 constexpr float kTileShift = 4.0f;                     // probabilities up to 2^(kLag + kTileShift)
 
+// The sequence that the t-th tile of rows belongs to, and which of its tiles it is; b < 0: there are not so many.  Sequences of few rows have
+// none (the streaming kernel's), the others one for every `tile_rows` rows.
+struct TileOf { int b, index; };
+__device__ __forceinline__ TileOf tile_of(const AttentionArgs &p, int t, int tile_rows) {
+    if (!p.starts) {
+        const int each = (p.per * p.group + tile_rows - 1) / tile_rows, b = t / each;
+        return {b < p.batch ? b : -1, t - b * each};
+    }
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < p.batch; base += 64) {
+        int mine = 0;
+        if (base + lane < p.batch) {
+            const int rows = sequence(p, base + lane).fresh * p.group;
+            mine = rows > p.few ? (rows + tile_rows - 1) / tile_rows : 0;
+        }
+        int sum = mine;                                // of this lane's sequence and those before it
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const int other = __shfl_up(sum, i);
+            if (lane >= i) sum += other;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(t < sum);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            return {base + at, t - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at))};
+        }
+        t -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return {-1, 0};
+}
+
 // v *= f where any bit of `mask` is set.  The branch is inside the statement: around a product in C++ the compiler keeps the sums in
 // two sets of registers and copies one to the other in every step, 64 moves and 64 registers at 128 dims.  (The values come from
 // matrix instructions that `f` depends on having ended; the waits are for `f`, an exponential, and for those that read the values next.)
@@ -563,8 +594,31 @@ __device__ __forceinline__ void scale_if(uint64_t mask, float f, floatx16 &v) {
     }
 }
 
+// What a workgroup of the tile kernel has to do; rows1 < 0: nothing.
+struct TilePlace {
+    int head, b, row0, row1, past, chunks;
+    Sequence sq;
+    Walk w;
+};
+__device__ __forceinline__ TilePlace tile_place(const AttentionArgs &p, int tile, int tile_rows) {
+    TilePlace o;
+    o.row1 = -1;
+    o.head = tile % p.kv_heads;
+    const TileOf at = tile_of(p, tile / p.kv_heads, tile_rows);
+    if (at.b < 0) return o;
+    o.b = at.b;
+    o.sq = sequence(p, o.b);
+    const int rows = o.sq.fresh * p.group, row_tiles = (rows + tile_rows - 1) / tile_rows;
+    o.row0 = (row_tiles - 1 - at.index) * tile_rows;       // rows of late tokens, which see most, first
+    o.row1 = min(rows, o.row0 + tile_rows) - 1;
+    o.past = o.sq.length - o.sq.fresh;
+    o.w = walk(p, o.past + o.row0 / p.group, o.past + o.row1 / p.group);
+    o.chunks = min(p.chunks, max(1, (o.w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+    return o;
+}
+
 template <int D, bool FP8, int NW, int TK>
-__global__ void __launch_bounds__(64 * NW)
+__global__ void __launch_bounds__(64 * NW, 2)
 attention_tile_kernel(AttentionArgs p) {
     constexpr int T = 64 * NW, NB = TK / 16, HB = TK / 32;       // threads, blocks and halves (of 32 tokens) of a tile of tokens
     constexpr int CB = FP8 ? D : 2 * D;                          // 16-byte chunks of a block in memory
@@ -574,21 +628,15 @@ attention_tile_kernel(AttentionArgs p) {
     constexpr int HALF = NB * 2 * D, BUFFER = 2 * HALF;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
-    // rows of late tokens, which see most, first; the heads of a sequence on different XCDs
-    const int tiles = p.batch * p.kv_heads * p.row_tiles;
+    // the heads of a sequence on different XCDs
+    const int tiles = p.kv_heads * p.row_tiles;
     const int chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
-    const int head = tile % p.kv_heads, b = tile / p.kv_heads % p.batch, from_last = tile / p.kv_heads / p.batch;
-    const Sequence sq = sequence(p, b);
-    const int rows = sq.fresh * p.group;
-    if (rows <= p.few) return;                                   // (the streaming kernel's)
-    const int row_tiles = (rows + 32 * NW - 1) / (32 * NW);
-    if (from_last >= row_tiles) return;
-    const int row0 = (row_tiles - 1 - from_last) * 32 * NW, row1 = min(rows, row0 + 32 * NW) - 1;
-    const int past = sq.length - sq.fresh;
+    const TilePlace place = tile_place(p, tile, 32 * NW);
+    if (place.row1 < 0 || chunk >= place.chunks) return;
+    const int head = place.head, b = place.b, row0 = place.row0, row1 = place.row1, past = place.past, chunks = place.chunks;
+    const Sequence sq = place.sq;
+    const Walk w = place.w;
     const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
-    const Walk w = walk(p, low_pos, high_pos);
-    const int chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
-    if (chunk >= chunks) return;
     const int v0 = chunk * p.chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
     const int steps = (v1 - v0 + NB - 1) / NB;
     const int first_low = before(p, low_pos);
@@ -902,22 +950,55 @@ attention_tile_kernel(AttentionArgs p) {
                     u32x2{float2_to_half2_bits(acc[d][i] * f, acc[d][i + 1] * f), float2_to_half2_bits(acc[d][i + 2] * f, acc[d][i + 3] * f)};
         return;
     }
-    const int stride = D + 2;
-    if (row <= row1) {
-        float *dst = p.partials + (((int64_t)tile * p.chunks + chunk) * p.part_rows + row - row0) * stride;
+    // this wave's part: the sums as its lanes hold them, then the rows' maxima and sums of probabilities
+    float *part = p.partials + (((int64_t)tile * p.chunks + chunk) * NW + wave) * (32 * (D + 2));
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2)
-                __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3)),
-                                   (unsigned long long)__float_as_uint(acc[d][i]) | (unsigned long long)__float_as_uint(acc[d][i + 1]) << 32,
-                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (h == 0)
-            __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + D),
-                               (unsigned long long)__float_as_uint(top) | (unsigned long long)__float_as_uint(total) << 32,
-                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<floatx4 *>(part + ((d * 4 + (i >> 2)) * 64 + lane) * 4) = floatx4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+    if (h == 0) {
+        part[32 * D + 2 * col] = top;
+        part[32 * D + 2 * col + 1] = total;
     }
-    join(p, tile, chunks, sq, row0, row1, past, head, D, T, v_scale, reinterpret_cast<int *>(lds));
+}
+
+// Joins the parts of split tiles, in order: a launch of its own, since a tile's parts are hundreds of kilobytes and all of the chip can
+// read them then, where the last workgroup of a tile would read them alone (64 tokens after 16384, 4 query heads to a key/value head: 287
+// us in all that way).  A workgroup has the 32 rows of one wave.
+template <int D>
+__global__ void __launch_bounds__(256)
+attention_join_kernel(AttentionArgs p, int waves, const float *v_scales) {
+    constexpr int DB = D / 32;
+    const int tile = blockIdx.x / waves, wave = blockIdx.x - tile * waves;
+    const TilePlace place = tile_place(p, tile, 32 * waves);
+    const int lane = threadIdx.x & 63, col = lane & 31, i4 = threadIdx.x >> 6;
+    const int row = place.row0 + 32 * wave + col;
+    if (place.row1 < 0 || place.chunks <= 1 || place.row0 + 32 * wave > place.row1) return;
+    const float *part = p.partials + ((int64_t)tile * p.chunks * waves + wave) * (32 * (D + 2));
+    const int64_t next = (int64_t)waves * (32 * (D + 2));
+    float top = kNegInf, total = 0.0f;
+    floatx4 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = floatx4{0, 0, 0, 0};
+#pragma unroll 4
+    for (int c = 0; c < place.chunks; ++c, part += next) {
+        const float m = part[32 * D + 2 * col], l = part[32 * D + 2 * col + 1];
+        const float now = fmaxf(top, m), ref = fmaxf(now, -1e30f);
+        const float f = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref);
+        top = now;
+        total = total * f + l * g;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[d] = acc[d] * f + *reinterpret_cast<const floatx4 *>(part + ((d * 4 + i4) * 64 + lane) * 4) * g;
+    }
+    if (row > place.row1) return;
+    const int token = row / p.group, g = row - token * p.group;
+    uint16_t *dst = p.O + (int64_t)(place.sq.first + token) * p.ldo + (int64_t)(place.head * p.group + g) * D + 8 * i4 + 4 * (lane >> 5);
+    const float f = (v_scales ? v_scales[place.head] : 1.0f) / total;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        *reinterpret_cast<u32x2 *>(dst + 32 * d) = place.past + token < 0 ? u32x2{0u, 0u} :
+            u32x2{float2_to_half2_bits(acc[d][0] * f, acc[d][1] * f), float2_to_half2_bits(acc[d][2] * f, acc[d][3] * f)};
 }
 
 // ---- launch shapes ----------------------------------------------------------------------------------------------------------
@@ -932,16 +1013,15 @@ static int64_t blocks_seen(const AttentionShape &s, int64_t rows) {
     return blocks < 1 ? 1 : blocks;
 }
 
-static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t rows, int64_t tile_rows, int64_t least, int64_t wanted) {
-    a.row_tiles = (rows + tile_rows - 1) / tile_rows;
-    a.part_rows = rows < tile_rows ? rows : tile_rows;
-    a.tiles = s.batch * s.kv_heads * a.row_tiles;
+// `busy`: tiles among a.tiles that are expected to have work; `wanted`: workgroups that fill the chip; `least`: blocks below
+// which a workgroup has too little to do; `tickets`: the parts are joined by the last workgroup of a tile, which takes a counter.
+static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t tile_rows, int64_t busy, int64_t least, int64_t wanted, bool tickets) {
     const int64_t blocks = blocks_seen(s, tile_rows);
-    int64_t chunk = (blocks * a.tiles + wanted - 1) / wanted;
+    int64_t chunk = (blocks * busy + wanted - 1) / wanted;
     if (tuning().attn_chunk > 0) chunk = tuning().attn_chunk / 16;
     if (chunk < least) chunk = least;
     chunk = (chunk + least - 1) / least * least;
-    if (a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
+    if (tickets && a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
     a.chunk_blocks = chunk;
     a.chunks = (blocks + chunk - 1) / chunk;
     a.partial_bytes = a.chunks > 1 ? (size_t)a.tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
@@ -957,12 +1037,30 @@ AttentionPlan attention_plan(const AttentionShape &s) {
     if (many) {
         // sequences of few rows beside the others: none if all have as many new tokens
         a.few = s.ragged && rows > stream_rows && s.group <= stream_rows ? stream_rows : 0;
-        plan_launch(a.tile, s, rows, 256, 16, 512);
+        const int64_t total = s.tokens * s.group;
+        a.waves = tuning().attn_waves > 0 ? tuning().attn_waves : (total + 255) / 256 * s.kv_heads >= 512 ? 8 : 4;
+        const int64_t tile_rows = 32 * a.waves;
+        int64_t most = s.batch * ((rows + tile_rows - 1) / tile_rows), likely = most;
+        if (s.ragged) {
+            // rows lie in whole tiles, but for the last one of every sequence that has any
+            const int64_t with = s.tokens / (a.few / s.group + 1);
+            const int64_t bound = total / tile_rows + (with < s.batch ? with : s.batch);
+            if (bound < most) most = bound;
+            likely = (total + tile_rows - 1) / tile_rows;
+            if (likely > most) likely = most;
+        }
+        a.tile.row_tiles = most;
+        a.tile.tiles = most * s.kv_heads;
+        a.tile.part_rows = tile_rows;
+        plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, 16, a.waves == 8 ? 256 : 512, false);
     }
     if (!many || a.few > 0) {
         const int64_t most = many ? a.few / s.group * s.group : rows;
         a.rt = most <= 16 || s.D > 128 ? 1 : 2;
-        plan_launch(a.stream, s, most, 16 * a.rt, s.fp8 ? 16 : 8, 1536);
+        a.stream.row_tiles = (most + 16 * a.rt - 1) / (16 * a.rt);
+        a.stream.tiles = s.batch * s.kv_heads * a.stream.row_tiles;
+        a.stream.part_rows = most < 16 * a.rt ? most : 16 * a.rt;
+        plan_launch(a.stream, s, 16 * a.rt, a.stream.tiles, s.fp8 ? 16 : 8, 1536, true);
     }
     a.partial_bytes = a.stream.partial_bytes > a.tile.partial_bytes ? a.stream.partial_bytes : a.tile.partial_bytes;
     return a;
@@ -970,7 +1068,7 @@ AttentionPlan attention_plan(const AttentionShape &s) {
 
 static bool shape_of(const AttentionLaunch &l, AttentionArgs &a, dim3 &grid) {
     const int64_t groups = l.tiles * l.chunks;
-    if (groups > 0x7fffffff) return false;
+    if (groups > 0xfffffff) return false;
     a.row_tiles = (int)l.row_tiles;
     a.part_rows = (int)l.part_rows;
     a.chunk_blocks = (int)l.chunk_blocks;
@@ -991,11 +1089,15 @@ static void launch_stream(int64_t rt, const AttentionArgs &a, dim3 grid, hipStre
 }
 
 template <int D, bool FP8>
-static int launch_tile(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
+static int launch_tile(int64_t waves, const AttentionArgs &a, dim3 grid, hipStream_t stream) {
     if constexpr (D <= 128) {
-        constexpr int NW = 8, TK = 64, LDS = 8 * TK * D;             // two buffers of keys and values in FP16
+        constexpr int TK = 64, LDS = 8 * TK * D;                     // two buffers of keys and values in FP16
         static_assert(LDS <= 65536, "");
-        attention_tile_kernel<D, FP8, NW, TK><<<grid, 64 * NW, LDS, stream>>>(a);
+        if (waves == 8) attention_tile_kernel<D, FP8, 8, TK><<<grid, 512, LDS, stream>>>(a);
+        else attention_tile_kernel<D, FP8, 4, TK><<<grid, 256, LDS, stream>>>(a);
+        const int st = hip_ok(hipGetLastError());
+        if (a.chunks == 1 || st != kOk) return st;
+        attention_join_kernel<D><<<dim3(grid.x / a.chunks * waves), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
         return hip_ok(hipGetLastError());
     }
     return kErrShape;
@@ -1014,7 +1116,7 @@ int launch_attention(const AttentionShape &s, const AttentionPlan &plan, Attenti
     }
     if (plan.tile.tiles > 0) {
         if (!shape_of(plan.tile, a, grid)) return kErrShape;
-#define NFP_TILE(D, FP8) st = launch_tile<D, FP8>(a, grid, stream)
+#define NFP_TILE(D, FP8) st = launch_tile<D, FP8>(plan.waves, a, grid, stream)
         NFP_FOR_D(NFP_TILE)
 #undef NFP_TILE
         if (st != kOk) return st;
