@@ -145,9 +145,21 @@ __device__ __forceinline__ Walk walk(const AttentionArgs &p, int low_pos, int hi
 // ---- sequences split over workgroups -----------------------------------------------------------------------------------------
 // A workgroup's sums lie in the workspace as [tile][chunk][row]: D sums, then the maximum and the sum of the row's
 // probabilities.  They are stored past the caches (every XCD has an L2 of its own) before the tile's ticket is drawn;
-// the workgroup with the last ticket joins the chunks in their order and leaves the counter cleared.  Nobody waits for anybody.
+// the workgroup with the last ticket joins the chunks in a fixed order and leaves the counter cleared.  Nobody waits for anybody.
+// The joining workgroup first turns all maxima into weights, in `room` (kMaxChunks + 1 words for every row), then adds up with many
+// loads under way: one after the other, 64 chunks took about 40 us.
+constexpr int kMaxChunks = 256;
+__device__ __forceinline__ float2 pair_of(unsigned long long x) { return {__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))}; }
+__device__ __forceinline__ unsigned long long past_caches(const float *p) {
+    return __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void past_caches(float *p, float a, float b) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32,
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int D, int THREADS, int ROWS>
 __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunks, const Sequence &sq, int row0, int row1, int past, int head,
-                                     int D, int threads, float v_scale, int *last) {
+                                     float v_scale, float *room, int *last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -157,26 +169,59 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunk
     }
     __syncthreads();
     if (!*last) return;
-    const int count = row1 - row0 + 1, stride = D + 2;
-    for (int item = threadIdx.x; item < count * (D / 2); item += threads) {
-        const int r = item / (D / 2), d = 2 * (item - r * (D / 2));
-        float m = kNegInf, l = 0.0f, a0 = 0.0f, a1 = 0.0f;
-        for (int c = 0; c < chunks; ++c) {
-            const float *src = p.partials + (((int64_t)tile * p.chunks + c) * p.part_rows + r) * stride;
-            const unsigned long long ml = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + D), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const unsigned long long o = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(src + d), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const float mc = __uint_as_float((uint32_t)ml), lc = __uint_as_float((uint32_t)(ml >> 32));
-            const float next = fmaxf(m, mc), ref = fmaxf(next, -1e30f);
-            const float f = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(mc, -1e30f) - ref);
-            l = l * f + lc * g;
-            a0 = a0 * f + __uint_as_float((uint32_t)o) * g;
-            a1 = a1 * f + __uint_as_float((uint32_t)(o >> 32)) * g;
-            m = next;
+    const int count = row1 - row0 + 1;
+    constexpr int stride = D + 2;
+    const float *parts = p.partials + (int64_t)tile * p.chunks * p.part_rows * stride;
+    // weights: a wave takes one row after the other, a lane four chunks
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < count; r += THREADS / 64) {
+        float m[4], l[4], top = kNegInf, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 64 * i;
+            const float2 ml = pair_of(c < chunks ? past_caches(parts + ((int64_t)c * p.part_rows + r) * stride + D) : 0xff800000ull);
+            m[i] = ml.x;
+            l[i] = ml.y;
+            top = fmaxf(top, m[i]);
+        }
+        for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+        const float ref = fmaxf(top, -1e30f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = __builtin_amdgcn_exp2f(fmaxf(m[i], -1e30f) - ref);
+            if (lane + 64 * i < chunks) room[r * kMaxChunks + lane + 64 * i] = f;
+            sum += l[i] * f;
+        }
+        for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+        if (lane == 0) room[ROWS * kMaxChunks + r] = v_scale / sum;
+    }
+    __syncthreads();
+    for (int item = threadIdx.x; item < count * (D / 4); item += THREADS) {
+        const int r = item / (D / 4), d = 4 * (item - r * (D / 4));
+        const float *src = parts + r * stride + d;
+        const int64_t next = (int64_t)p.part_rows * stride;
+        const float *weight = room + r * kMaxChunks;
+        floatx4 acc = floatx4{0, 0, 0, 0};
+        constexpr int N = 8;
+        for (int c = 0; c < chunks; c += N) {
+            unsigned long long x[N][2];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float *at = src + min(c + i, chunks - 1) * next;
+                x[i][0] = past_caches(at);
+                x[i][1] = past_caches(at + 2);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float f = c + i < chunks ? weight[c + i] : 0.0f;
+                const float2 a = pair_of(x[i][0]), b = pair_of(x[i][1]);
+                if (c + i < chunks) acc += floatx4{a.x, a.y, b.x, b.y} * f;
+            }
         }
         const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
-        const float f = v_scale / l;
-        *reinterpret_cast<uint32_t *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) =
-            past + i < 0 ? 0u : float2_to_half2_bits(a0 * f, a1 * f);
+        const float f = room[ROWS * kMaxChunks + r];
+        *reinterpret_cast<u32x2 *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) = past + i < 0 ? u32x2{0u, 0u} :
+            u32x2{float2_to_half2_bits(acc[0] * f, acc[1] * f), float2_to_half2_bits(acc[2] * f, acc[3] * f)};
     }
 }
 
@@ -188,7 +233,7 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunk
 // P is carried as two FP16 terms (its FP16 rounding and the rest): the second product costs nothing here, and the
 // result then has the precision of the 32-bit sums.
 template <int D, bool FP8, int RT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, D <= 128 && RT == 1 ? 3 : 2)
 attention_stream_kernel(AttentionArgs p) {
     constexpr int NT = FP8 ? 4 : 2;                    // blocks per step
     constexpr int BLOCK = 16 * D * (FP8 ? 1 : 2);      // bytes of a block
@@ -196,7 +241,10 @@ attention_stream_kernel(AttentionArgs p) {
     constexpr int QS = FP8 ? 2 * KL : KL;              // operands of 32 dims
     constexpr int DB = D / 16;
     constexpr int LD = D + 4;
-    __shared__ float part[2][16 * RT][LD];
+    // the waves' sums on their way together, then the join's weights
+    constexpr int PART = 2 * 16 * RT * LD, ROOM = 16 * RT * (kMaxChunks + 1);
+    __shared__ float shared[PART > ROOM ? PART : ROOM];
+    float (*part)[16 * RT][LD] = reinterpret_cast<float (*)[16 * RT][LD]>(shared);
     __shared__ float stat[4][2][16 * RT];
     __shared__ int last;
 
@@ -523,19 +571,14 @@ attention_stream_kernel(AttentionArgs p) {
             if (row[r] > row1) continue;
             float *dst = p.partials + (slot + 16 * r + col) * stride;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; i += 2)
-                    __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + 16 * d + 4 * group + i),
-                                       (unsigned long long)__float_as_uint(acc[r][d][i]) | (unsigned long long)__float_as_uint(acc[r][d][i + 1]) << 32,
-                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (group == 0)
-                __hip_atomic_store(reinterpret_cast<unsigned long long *>(dst + D),
-                                   (unsigned long long)__float_as_uint(all_top[r]) | (unsigned long long)__float_as_uint(sum[r]) << 32,
-                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int d = 0; d < DB; ++d) {
+                past_caches(dst + 16 * d + 4 * group, acc[r][d][0], acc[r][d][1]);
+                past_caches(dst + 16 * d + 4 * group + 2, acc[r][d][2], acc[r][d][3]);
+            }
+            if (group == 0) past_caches(dst + D, all_top[r], sum[r]);
         }
     }
-    join(p, tile, chunks, sq, row0, row1, past, head, D, 256, v_scale, &last);
+    join<D, 256, 16 * RT>(p, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
 }
 
 // ---- tile kernel --------------------------------------------------------------------------------------------------------------
@@ -1022,6 +1065,7 @@ static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t til
     if (chunk < least) chunk = least;
     chunk = (chunk + least - 1) / least * least;
     if (tickets && a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
+    if (tickets && chunk * kMaxChunks < blocks) chunk = ((blocks + kMaxChunks - 1) / kMaxChunks + least - 1) / least * least;
     a.chunk_blocks = chunk;
     a.chunks = (blocks + chunk - 1) / chunk;
     a.partial_bytes = a.chunks > 1 ? (size_t)a.tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
