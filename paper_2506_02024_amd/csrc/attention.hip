@@ -11,6 +11,8 @@
 #include "nfp_device.h"
 #include "nfp_host.h"
 
+#include <algorithm>
+
 namespace nfp {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -158,11 +160,11 @@ __device__ __forceinline__ void past_caches(float *p, float a, float b) {
                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 template <int D, int THREADS, int ROWS>
-__device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunks, const Sequence &sq, int row0, int row1, int past, int head,
+__device__ __forceinline__ void join(const AttentionArgs &p, int thread, int tile, int chunks, const Sequence &sq, int row0, int row1, int past, int head,
                                      float v_scale, float *room, int *last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (thread == 0) {
         const uint32_t ticket = __hip_atomic_fetch_add(p.counters + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         *last = ticket == (uint32_t)chunks - 1;
         if (*last) __hip_atomic_store(p.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -173,8 +175,8 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunk
     constexpr int stride = D + 2;
     const float *parts = p.partials + (int64_t)tile * p.chunks * p.part_rows * stride;
     // weights: a wave takes one row after the other, a lane four chunks
-    const int lane = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < count; r += THREADS / 64) {
+    const int lane = thread & 63;
+    for (int r = thread >> 6; r < count; r += THREADS / 64) {
         float m[4], l[4], top = kNegInf, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -196,7 +198,7 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunk
         if (lane == 0) room[ROWS * kMaxChunks + r] = v_scale / sum;
     }
     __syncthreads();
-    for (int item = threadIdx.x; item < count * (D / 4); item += THREADS) {
+    for (int item = thread; item < count * (D / 4); item += THREADS) {
         const int r = item / (D / 4), d = 4 * (item - r * (D / 4));
         const float *src = parts + r * stride + d;
         const int64_t next = (int64_t)p.part_rows * stride;
@@ -225,6 +227,97 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int tile, int chunk
     }
 }
 
+// ---- who does what --------------------------------------------------------------------------------------------------------------
+// The host does not know the sequences' lengths (a captured graph is replayed as they grow), so every workgroup of the streaming
+// kernel works out the same schedule from them, one sequence per thread: how many blocks there are in all, from that the stretch that one
+// workgroup takes, and where each sequence's stretches begin in a list that the workgroups walk.  A launch over all
+// stretches that the largest length would have costs 1 to 2 us for every few hundred that turn out empty.
+// (Every wave does it by itself, with four sequences to a lane and sums by DPP moves: through LDS, with barriers and shuffles,
+// it took 3 us.)
+constexpr int kScan = 256;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_before(int v) {
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+// the sum over this lane and those before it
+__device__ __forceinline__ int sum_to_lane(int v) {
+    v = plus_before<0x111, 0xf>(v);                    // the lane 1, 2, 4, 8 before, in its row of 16
+    v = plus_before<0x112, 0xf>(v);
+    v = plus_before<0x114, 0xf>(v);
+    v = plus_before<0x118, 0xf>(v);
+    v = plus_before<0x142, 0xa>(v);                    // the last lane of the row before
+    return plus_before<0x143, 0xc>(v);                 // lane 31
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_before(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float sum_of_lanes(float v) {
+    v = plus_before<0x111, 0xf>(v);
+    v = plus_before<0x112, 0xf>(v);
+    v = plus_before<0x114, 0xf>(v);
+    v = plus_before<0x118, 0xf>(v);
+    v = plus_before<0x142, 0xa>(v);
+    v = plus_before<0x143, 0xc>(v);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+struct Schedule {
+    int begin[kScan / 64];                             // of sequence 64 i + lane in the list
+    int items, chunk_blocks;
+};
+__device__ __forceinline__ Schedule schedule(const AttentionArgs &p, int tile_rows, int least) {
+    constexpr int N = kScan / 64;
+    const int lane = threadIdx.x & 63;
+    Schedule plan;
+    int tiles[N], blocks[N];                           // of this lane's sequences; tiles: of rows, over all heads
+    float work = 0.0f, lists = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int t = 64 * i + lane;
+        tiles[i] = blocks[i] = 0;
+        if (64 * i >= p.batch) continue;
+        const Sequence sq = sequence(p, min(t, p.batch - 1));
+        const int rows = sq.fresh * p.group;
+        if (t < p.batch && rows > 0 && !(p.few > 0 && rows > p.few)) {
+            tiles[i] = (rows + tile_rows - 1) / tile_rows * p.kv_heads;
+            blocks[i] = walk(p, sq.length - sq.fresh, sq.length - 1).blocks;
+        }
+        work += (float)tiles[i] * (float)blocks[i];
+        lists += (float)tiles[i];
+    }
+    plan.chunk_blocks = p.chunk_blocks;
+    if (!p.fixed) {
+        work = sum_of_lanes(work);
+        lists = sum_of_lanes(lists);
+        // As many stretches as there are workgroups, or twice that; on average half of one is lost where each list ends.
+        const float slots = (float)gridDim.x;
+        const float wanted = 2.0f * lists <= slots ? slots - 0.5f * lists : fmaxf(2.0f * slots - 0.5f * lists, slots);
+        const int even = (int)fminf(work / wanted, 1e8f) + 1;
+        plan.chunk_blocks = __builtin_amdgcn_readfirstlane(max(plan.chunk_blocks, (even + least - 1) / least * least));
+    }
+    plan.items = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        plan.begin[i] = 0x7fffffff;
+        if (64 * i >= p.batch) continue;
+        const int count = tiles[i] * min(p.chunks, max(1, (blocks[i] + plan.chunk_blocks - 1) / plan.chunk_blocks)), sum = sum_to_lane(count);
+        plan.begin[i] = plan.items + sum - count;
+        plan.items += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return plan;
+}
+// the sequence of an item of the list, and the item's place among the sequence's
+__device__ __forceinline__ int place_of(const Schedule &plan, int item, int batch, int &b) {
+    int at = -1, first = 0;
+#pragma unroll
+    for (int i = 0; i < kScan / 64; ++i) at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.begin[i] <= item));
+    b = min(at, batch - 1);                            // (lanes behind the last sequence begin where it ends)
+#pragma unroll
+    for (int i = 0; i < kScan / 64; ++i)
+        if (b >> 6 == i) first = __builtin_amdgcn_readlane(plan.begin[i], b & 63);
+    return item - first;
+}
+
 // ---- streaming kernel -------------------------------------------------------------------------------------------------------
 // For few rows: bound by the bytes of the cache.  A workgroup of four waves takes 16 * RT rows and a stretch of the
 // sequence's blocks; a wave loads keys and values of 32 tokens (64 in E4M3) straight into registers, in operand order, every
@@ -242,27 +335,51 @@ attention_stream_kernel(AttentionArgs p) {
     constexpr int DB = D / 16;
     constexpr int LD = D + 4;
     // the waves' sums on their way together, then the join's weights
-    constexpr int PART = 2 * 16 * RT * LD, ROOM = 16 * RT * (kMaxChunks + 1);
+    constexpr int PART = 4 * 16 * RT * LD, ROOM = 16 * RT * (kMaxChunks + 1);
     __shared__ float shared[PART > ROOM ? PART : ROOM];
     float (*part)[16 * RT][LD] = reinterpret_cast<float (*)[16 * RT][LD]>(shared);
     __shared__ float stat[4][2][16 * RT];
     __shared__ int last;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, col = lane & 15;
-    const int tiles = p.batch * p.kv_heads * p.row_tiles;
-    const int chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
-    const int rt0 = tile % p.row_tiles, head = tile / p.row_tiles % p.kv_heads, b = tile / p.row_tiles / p.kv_heads;
-    const Sequence sq = sequence(p, b);
+    constexpr int LEAST = 4 * NT;                      // blocks: one step of each wave
+    Schedule plan;
+    if (p.scan) plan = schedule(p, 16 * RT, LEAST);
+    else plan.items = gridDim.x, plan.chunk_blocks = p.chunk_blocks;
+    const int items = plan.items, chunk_blocks = plan.chunk_blocks;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    __syncthreads();
+    // (hidden from the compiler, which otherwise works out before the loop what every lane needs in it, and keeps it in 40 registers)
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), group = lane >> 4, col = lane & 15;
+    int chunk, rt0, head, b;
+    Sequence sq;
+    if (p.scan) {
+        const int mine = place_of(plan, item, p.batch, b);
+        sq = sequence(p, b);
+        const int tiles = (sq.fresh * p.group + 16 * RT - 1) / (16 * RT);
+        head = mine % p.kv_heads;
+        rt0 = mine / p.kv_heads % tiles;
+        chunk = mine / p.kv_heads / tiles;
+    } else {
+        const int tiles = p.batch * p.kv_heads * p.row_tiles;
+        chunk = item / tiles;
+        head = item % p.kv_heads;
+        rt0 = item % tiles / p.kv_heads % p.row_tiles;
+        b = item % tiles / p.kv_heads / p.row_tiles;
+        sq = sequence(p, b);
+    }
+    const int tile = (b * p.row_tiles + rt0) * p.kv_heads + head;
     const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
-    if (row0 >= rows || (p.few > 0 && rows > p.few)) return;     // (the tile kernel's)
+    if (row0 >= rows || (p.few > 0 && rows > p.few)) continue;   // (the tile kernel's)
     const int row1 = min(rows, row0 + 16 * RT) - 1;
     const int past = sq.length - sq.fresh;
     const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
     const Walk w = walk(p, low_pos, high_pos);
     // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
-    const int chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
-    if (chunk >= chunks) return;
-    const int v0 = chunk * p.chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
+    const int chunks = min(p.chunks, max(1, (w.blocks + chunk_blocks - 1) / chunk_blocks));
+    if (chunk >= chunks) continue;
+    const int v0 = chunk * chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + chunk_blocks;
 
     // queries, as the second operand: column = row, dims in the order in which the keys' chunks come
     int row[RT], pos[RT], low[RT];
@@ -505,80 +622,55 @@ attention_stream_kernel(AttentionArgs p) {
         }
     }
 
-    // the four waves' sums: waves 2 and 3 hand theirs to 0 and 1, then 1 to 0
-    float mine_top[RT], all_top[RT];
+    // the four waves' sums: statistics first, then each wave's sums relative to the largest maximum; of rows that there are
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         total[r] = sum_of_groups(total[r]);
-        mine_top[r] = top[r];
         if (group == 0) {
             stat[wave][0][16 * r + col] = top[r];
             stat[wave][1][16 * r + col] = total[r];
         }
     }
     __syncthreads();
-    float sum[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         float m = kNegInf;
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][16 * r + col]);
-        all_top[r] = m;
-        const float ref = fmaxf(m, -1e30f);
-        sum[r] = 0.0f;
+        const float f = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
+        if (row[r] <= row1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[r] += stat[i][1][16 * r + col] * __builtin_amdgcn_exp2f(fmaxf(stat[i][0][16 * r + col], -1e30f) - ref);
-        const float f = __builtin_amdgcn_exp2f(fmaxf(mine_top[r], -1e30f) - ref);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[r][d] *= f;
-    }
-#pragma unroll
-    for (int half = 2; half >= 1; half >>= 1) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) *reinterpret_cast<floatx4 *>(&part[wave - half][16 * r + col][16 * d + 4 * group]) = acc[r][d];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) acc[r][d] += *reinterpret_cast<const floatx4 *>(&part[wave][16 * r + col][16 * d + 4 * group]);
-        __syncthreads();
-    }
-    const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
-    if (chunks == 1) {
-        if (wave == 0)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (row[r] > row1) continue;
-                const int i = row[r] / p.group, g = row[r] - i * p.group;
-                uint16_t *dst = p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + 4 * group;
-                const float f = pos[r] < 0 ? 0.0f : v_scale / sum[r];       // a row that sees nothing is zero
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    *reinterpret_cast<u32x2 *>(dst + 16 * d) = pos[r] < 0 ? u32x2{0u, 0u} :
-                        u32x2{float2_to_half2_bits(acc[r][d][0] * f, acc[r][d][1] * f), float2_to_half2_bits(acc[r][d][2] * f, acc[r][d][3] * f)};
-            }
-        return;
-    }
-    const int stride = D + 2;
-    const int64_t slot = ((int64_t)tile * p.chunks + chunk) * p.part_rows;
-    if (wave == 0) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (row[r] > row1) continue;
-            float *dst = p.partials + (slot + 16 * r + col) * stride;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                past_caches(dst + 16 * d + 4 * group, acc[r][d][0], acc[r][d][1]);
-                past_caches(dst + 16 * d + 4 * group + 2, acc[r][d][2], acc[r][d][3]);
-            }
-            if (group == 0) past_caches(dst + D, all_top[r], sum[r]);
+            for (int d = 0; d < DB; ++d) *reinterpret_cast<floatx4 *>(&part[wave][16 * r + col][16 * d + 4 * group]) = acc[r][d] * f;
         }
     }
-    join<D, 256, 16 * RT>(p, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
+    __syncthreads();
+    const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
+    for (int at = thread; at < (row1 - row0 + 1) * (D / 4); at += 256) {
+        const int r = at / (D / 4), d = 4 * (at - r * (D / 4));
+        float m = kNegInf, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][r]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += stat[i][1][r] * __builtin_amdgcn_exp2f(fmaxf(stat[i][0][r], -1e30f) - fmaxf(m, -1e30f));
+        floatx4 o = *reinterpret_cast<const floatx4 *>(&part[0][r][d]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) o += *reinterpret_cast<const floatx4 *>(&part[i][r][d]);
+        if (chunks == 1) {
+            const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
+            const float f = v_scale / sum;
+            // a row that sees nothing is zero
+            *reinterpret_cast<u32x2 *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) = past + i < 0 ? u32x2{0u, 0u} :
+                u32x2{float2_to_half2_bits(o[0] * f, o[1] * f), float2_to_half2_bits(o[2] * f, o[3] * f)};
+        } else {
+            float *dst = p.partials + (((int64_t)tile * p.chunks + chunk) * p.part_rows + r) * (D + 2);
+            past_caches(dst + d, o[0], o[1]);
+            past_caches(dst + d + 2, o[2], o[3]);
+            if (d == 0) past_caches(dst + D, m, sum);
+        }
+    }
+    if (chunks == 1) continue;
+    join<D, 256, 16 * RT>(p, thread, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
+    }
 }
 
 // ---- tile kernel --------------------------------------------------------------------------------------------------------------
@@ -1104,7 +1196,7 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.stream.row_tiles = (most + 16 * a.rt - 1) / (16 * a.rt);
         a.stream.tiles = s.batch * s.kv_heads * a.stream.row_tiles;
         a.stream.part_rows = most < 16 * a.rt ? most : 16 * a.rt;
-        plan_launch(a.stream, s, 16 * a.rt, a.stream.tiles, s.fp8 ? 16 : 8, 1536, true);
+        plan_launch(a.stream, s, 16 * a.rt, a.stream.tiles, s.fp8 ? 16 : 8, s.batch <= kScan ? 4096 : 1536, true);
     }
     a.partial_bytes = a.stream.partial_bytes > a.tile.partial_bytes ? a.stream.partial_bytes : a.tile.partial_bytes;
     return a;
@@ -1167,6 +1259,10 @@ int launch_attention(const AttentionShape &s, const AttentionPlan &plan, Attenti
     }
     if (plan.stream.tiles > 0) {
         if (!shape_of(plan.stream, a, grid)) return kErrShape;
+        a.scan = s.batch <= kScan && plan.stream.chunks > 1;
+        a.fixed = tuning().attn_chunk > 0;
+        // (what the chip holds at once: three workgroups per CU, two of the larger ones)
+        if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, plan.rt == 1 && s.D <= 128 ? 768 : 512));
 #define NFP_STREAM(D, FP8) launch_stream<D, FP8>(plan.rt, a, grid, stream)
         NFP_FOR_D(NFP_STREAM)
 #undef NFP_STREAM

@@ -240,6 +240,7 @@ struct AttentionArgs {
     int32_t tokens, batch, per, max_new, columns;      // per: new tokens of every sequence where there are no starts
     int32_t kv_heads, group, pages, page_shift, window, sinks;
     int32_t row_tiles, part_rows, chunk_blocks, chunks, few;
+    bool scan, fixed;                                  // workgroups work out who does what; in stretches of chunk_blocks
 };
 struct AttentionShape { int64_t tokens, batch, kv_heads, group, D, max_new, max_len, window, sinks;  bool fp8, ragged; };
 struct AttentionLaunch { int64_t row_tiles, part_rows, chunk_blocks, chunks, tiles;  size_t partial_bytes; };
