@@ -478,9 +478,15 @@ def linear(X, layer, mode, act_scale=None, out=None, workspace=None):
     return out
 
 
-def _dtype(t, dtype, name):
-    if t.dtype != dtype:
-        raise ValueError("%s must be %s" % (name, dtype))
+_F16, _F32, _I32, _U8 = torch.float16, torch.float32, torch.int32, torch.uint8
+
+
+def _like(t, shape, name):
+    """(address, row stride) of a float16 matrix that has to have a shape."""
+    ld, inner = t.stride()
+    if t.shape != shape or t.dtype is not _F16 or inner != 1:
+        raise ValueError("%s must be float16 %s with unit inner stride" % (name, tuple(shape)))
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
 
 
 def add_rms_norm(X, weight, eps=1e-5, residual=None, sum_out=None, out=None, Xq=None, scales=None):
@@ -488,29 +494,32 @@ def add_rms_norm(X, weight, eps=1e-5, residual=None, sum_out=None, out=None, Xq=
 
     Writes those of sum_out (h; may be residual or X), out (fp16 y), Xq (uint8 [M,K], E4M3 codes of y) with scales (float32
     [M]) that are given, and returns (out, Xq, scales, sum_out).  With neither out nor Xq, out is made."""
-    M, K, ldx = _rowmajor(X, "X")
-    _dtype(X, torch.float16, "X")
-    if weight.dtype != torch.float16 or weight.shape != (K,) or not weight.is_contiguous():
+    shape = X.shape
+    if len(shape) != 2 or X.dtype is not _F16:
+        raise ValueError("X must be float16 [M,K]")
+    M, K = shape
+    x, ldx = _like(X, shape, "X")
+    if weight.dtype is not _F16 or weight.numel() != K or not weight.is_contiguous():
         raise ValueError("weight must be a contiguous float16 [K] tensor")
     if out is None and Xq is None:
-        out = torch.empty((M, K), dtype=torch.float16, device=X.device)
-    lds = []
-    for t, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")):
-        if t is None:
-            lds.append(0)
-            continue
-        rows, cols, ld = _rowmajor(t, name)
-        if rows != M or cols != K or t.dtype != torch.float16:
-            raise ValueError("%s must be float16 [M,K]" % name)
-        lds.append(ld)
+        out = torch.empty((M, K), dtype=_F16, device=X.device)
+    r = h = y = q = s = None
+    ldr = ldh = ldy = 0
+    if residual is not None:
+        r, ldr = _like(residual, shape, "residual")
+    if sum_out is not None:
+        h, ldh = _like(sum_out, shape, "sum_out")
+    if out is not None:
+        y, ldy = _like(out, shape, "out")
     if Xq is not None:
-        if Xq.dtype != torch.uint8 or Xq.shape != (M, K) or not Xq.is_contiguous():
+        if Xq.dtype is not _U8 or Xq.shape != shape or not Xq.is_contiguous():
             raise ValueError("Xq must be a contiguous uint8 [M,K] tensor")
-        if scales is None or scales.dtype != torch.float32 or scales.shape != (M,) or not scales.is_contiguous():
+        if scales is None or scales.dtype is not _F32 or scales.numel() != M or not scales.is_contiguous():
             raise ValueError("scales must be a contiguous float32 [M] tensor")
-    st = lib().nestedfp_add_rms_norm(_ptr(X), M, K, ldx, _ptr(residual), lds[0], _ptr(weight), eps, _ptr(sum_out), lds[1],
-                                     _ptr(out), lds[2], _ptr(Xq), _ptr(scales), _stream())
-    _check(st, "nestedfp_add_rms_norm")
+        q, s = Xq.data_ptr(), scales.data_ptr()
+    st = (_lib or lib()).nestedfp_add_rms_norm(x, M, K, ldx, r, ldr, weight.data_ptr(), eps, h, ldh, y, ldy, q, s, _stream())
+    if st:
+        raise NestedFPError(st, "nestedfp_add_rms_norm")
     return out, Xq, scales, sum_out
 
 
@@ -573,14 +582,16 @@ class KVCache:
 
 
 def _heads(t, dim, name):
-    rows, cols, ld = _rowmajor(t, name)
-    if t.dtype != torch.float16 or cols == 0 or cols % dim:
+    """(rows, heads, address, row stride) of a float16 [tokens, heads * head_dim] matrix."""
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if t.dtype is not _F16 or inner != 1 or cols == 0 or cols % dim:
         raise ValueError("%s must be float16 [tokens, heads * head_dim]" % name)
-    return rows, cols // dim, ld
+    return rows, cols // dim, t.data_ptr(), ld if rows > 1 else max(ld, cols)
 
 
 def _indices(t, n, name):
-    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 tensor of %d" % (name, n))
     return t.data_ptr()
 
@@ -589,28 +600,31 @@ def rope_append(q, k, v, positions, slots, cache, cos=None, sin=None, out=None):
     """Rotates the heads of q (fp16 [M, heads * head_dim]) and k by the rows of cos and sin (float32 [positions, rotary_dim / 2];
     None: no rotation) at `positions` (int32 [M]), and writes k and v ([M, kv_heads * head_dim]) to `slots` (int32 [M]) of the
     cache.  Returns the rotated q (out, which may be q; made if None)."""
-    dim = cache.head_dim
-    M, heads, ldq = _heads(q, dim, "q")
-    rows_k, kv_k, ldk = _heads(k, dim, "k")
-    rows_v, kv_v, ldv = _heads(v, dim, "v")
-    if rows_k != M or rows_v != M or kv_k != cache.kv_heads or kv_v != cache.kv_heads:
+    dim, kv = cache.head_dim, cache.kv_heads
+    M, heads, q_at, ldq = _heads(q, dim, "q")
+    rows_k, kv_k, k_at, ldk = _heads(k, dim, "k")
+    rows_v, kv_v, v_at, ldv = _heads(v, dim, "v")
+    if rows_k != M or rows_v != M or kv_k != kv or kv_v != kv:
         raise ValueError("k and v must be [tokens, kv_heads * head_dim] of the cache")
     known = rotary = 0
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin go together")
-    if cos is not None:
-        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()):
+    c = s = at = None
+    if cos is not None and sin is not None:
+        known, pairs = shape = cos.shape
+        if cos.dtype is not _F32 or sin.dtype is not _F32 or sin.shape != shape or not (cos.is_contiguous() and sin.is_contiguous()):
             raise ValueError("cos and sin must be contiguous float32 [positions, rotary_dim / 2] tensors")
-        known, rotary = cos.shape[0], 2 * cos.shape[1]
+        c, s, rotary = cos.data_ptr(), sin.data_ptr(), 2 * pairs
+        at = _indices(positions, M, "positions")
+    elif cos is not None or sin is not None:
+        raise ValueError("cos and sin go together")
     if out is None:
-        out = torch.empty((M, heads * dim), dtype=torch.float16, device=q.device)
-    rows_o, heads_o, ldo = _heads(out, dim, "out")
+        out = torch.empty((M, heads * dim), dtype=_F16, device=q.device)
+    rows_o, heads_o, o_at, ldo = _heads(out, dim, "out")
     if rows_o != M or heads_o != heads:
         raise ValueError("out must have the shape of q")
-    st = lib().nestedfp_rope_append(_ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, M, heads, _ptr(cos), _ptr(sin), known, rotary,
-                                    _indices(positions, M, "positions") if rotary else None, _indices(slots, M, "slots"),
-                                    _ptr(out), ldo, cache._ref, _stream())
-    _check(st, "nestedfp_rope_append")
+    st = (_lib or lib()).nestedfp_rope_append(q_at, ldq, k_at, ldk, v_at, ldv, M, heads, c, s, known, rotary, at,
+                                              _indices(slots, M, "slots"), o_at, ldo, cache._ref, _stream())
+    if st:
+        raise NestedFPError(st, "nestedfp_rope_append")
     return out
 
 
@@ -628,31 +642,33 @@ def paged_attention(q, cache, table, lens, starts=None, max_new=None, max_len=No
     the sequences' new tokens and lengths (None: what the shapes of q and table allow; a tight max_len makes a better launch).
     scale: head_dim ** -0.5 if None.  window, sinks: see include/nestedfp.h."""
     dim = cache.head_dim
-    tokens, heads, ldq = _heads(q, dim, "q")
-    batch = lens.shape[0]
-    if table.dtype != torch.int32:
-        raise ValueError("table must be int32")
-    rows, columns, ld_table = _rowmajor(table, "table")
-    if rows != batch:
-        raise ValueError("table must be [batch, columns]")
+    tokens, heads, q_at, ldq = _heads(q, dim, "q")
+    rows, columns = table.shape
+    ld_table, inner = table.stride()
+    if table.dtype is not _I32 or inner != 1 and columns > 1:
+        raise ValueError("table must be int32 with unit inner stride")
+    if rows <= 1 or columns == 0:
+        ld_table = max(ld_table, columns)
+    lens_at = _indices(lens, rows, "lens")
+    starts_at = None if starts is None else _indices(starts, rows + 1, "starts")
     if max_new is None:
-        max_new = tokens if starts is not None else tokens // max(batch, 1)
+        max_new = tokens if starts is not None else tokens // max(rows, 1)
     if max_len is None:
         max_len = columns * cache.page_tokens
     if out is None:
-        out = torch.empty((tokens, heads * dim), dtype=torch.float16, device=q.device)
-    rows_o, heads_o, ldo = _heads(out, dim, "out")
+        out = torch.empty((tokens, heads * dim), dtype=_F16, device=q.device)
+    rows_o, heads_o, o_at, ldo = _heads(out, dim, "out")
     if rows_o != tokens or heads_o != heads:
         raise ValueError("out must have the shape of q")
-    L = lib()
+    L = _lib or lib()
     if workspace is None:
-        workspace = _workspace(L.nestedfp_paged_attention_workspace_size(tokens, batch, heads, cache._ref, max_new, max_len, window, sinks),
+        workspace = _workspace(L.nestedfp_paged_attention_workspace_size(tokens, rows, heads, cache._ref, max_new, max_len, window, sinks),
                                q.device)
-    st = L.nestedfp_paged_attention(q.data_ptr(), tokens, ldq, heads, cache._ref, table.data_ptr(), ld_table, columns,
-                                    _indices(lens, batch, "lens"), batch, None if starts is None else _indices(starts, batch + 1, "starts"),
-                                    max_new, max_len, dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ldo,
+    st = L.nestedfp_paged_attention(q_at, tokens, ldq, heads, cache._ref, table.data_ptr(), ld_table, columns, lens_at, rows, starts_at,
+                                    max_new, max_len, dim ** -0.5 if scale is None else scale, window, sinks, o_at, ldo,
                                     workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "nestedfp_paged_attention")
+    if st:
+        raise NestedFPError(st, "nestedfp_paged_attention")
     return out
 
 

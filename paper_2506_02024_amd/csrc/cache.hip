@@ -5,6 +5,8 @@
 #include "nfp_device.h"
 #include "nfp_host.h"
 
+#include <algorithm>
+
 namespace nfp {
 
 constexpr int kAppendThreads = 256;
@@ -55,34 +57,31 @@ __device__ __forceinline__ void put8(const AppendArgs &p, bool query, int head, 
         *reinterpret_cast<u32x4 *>(block + ((dim >> 3) * 16 + token) * 16) = pack8(f);
 }
 
-// grid: (groups of tokens, heads of q, then of k, then of v).  Queries and keys: a lane has 8 dims and their 8 partners
-// (or 8 dims that are not rotated) of one token.  Values: a lane has one dim, of one token after the other.
-__global__ void __launch_bounds__(kAppendThreads)
-rope_append_kernel(AppendArgs p) {
-    const int head = blockIdx.y;
-    if (head < p.heads + p.kv_heads) {
-        const bool query = head < p.heads;
-        const int h = query ? head : head - p.heads;
-        const int r = p.rotary / 2, turns = r / 8, items = turns + (p.D - p.rotary) / 8;
-        const int token = threadIdx.x / items, item = threadIdx.x - token * items;
-        const int64_t m = (int64_t)blockIdx.x * p.group + token;
-        if (token >= p.group || m >= p.M) return;
-        int slot = -1;
-        if (!query) {
-            slot = p.slots[m];
-            if (slot >= p.slot_count) slot = -1;
-        }
-        const uint16_t *x = (query ? p.q + m * p.ldq : p.new_k + m * p.ldk) + (int64_t)h * p.D;
-        float a[8];
-        if (item >= turns) {
-            const int dim = p.rotary + 8 * (item - turns);
-            unpack8(*reinterpret_cast<const u32x4 *>(x + dim), a);
-            put8(p, query, h, m, slot, dim, a);
-            return;
-        }
-        float b[8], c[8], s[8], lo[8], hi[8];
-        unpack8(*reinterpret_cast<const u32x4 *>(x + 8 * item), a);
-        unpack8(*reinterpret_cast<const u32x4 *>(x + r + 8 * item), b);
+// Queries and keys of HEADS heads: a lane has 8 dims and their 8 partners (or 8 dims that are not rotated) of one token, in every
+// head, with the token's angles in registers (with one head to a lane the tables were read 48 times over).
+template <int HEADS>
+__device__ __forceinline__ void rotate(const AppendArgs &p, int first_head) {
+    const int r = p.rotary / 2, turns = r / 8, items = turns + (p.D - p.rotary) / 8;
+    const int token = threadIdx.x / items, item = threadIdx.x - token * items;
+    const int64_t m = (int64_t)blockIdx.x * p.group + token;
+    if (token >= p.group || m >= p.M) return;
+    const bool turned = item < turns;
+    const int lo_dim = turned ? 8 * item : p.rotary + 8 * (item - turns), hi_dim = lo_dim + r;
+    u32x4 lo[HEADS], hi[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        const int head = min(first_head + i, p.heads + p.kv_heads - 1);
+        const uint16_t *x = head < p.heads ? p.q + m * p.ldq + (int64_t)head * p.D : p.new_k + m * p.ldk + (int64_t)(head - p.heads) * p.D;
+        lo[i] = *reinterpret_cast<const u32x4 *>(x + lo_dim);
+        if (turned) hi[i] = *reinterpret_cast<const u32x4 *>(x + hi_dim);
+    }
+    int slot = -1;
+    if (first_head + HEADS > p.heads) {
+        slot = p.slots[m];
+        if (slot >= p.slot_count) slot = -1;
+    }
+    float c[8], s[8];
+    if (turned) {
         const int position = p.positions[m];
         const bool known = position >= 0 && position < p.positions_known;
         const int64_t at = (known ? (int64_t)position : 0) * r + 8 * item;
@@ -91,38 +90,106 @@ rope_append_kernel(AppendArgs p) {
             // a position that the tables do not have gives NaN, not another position's angles
             c[i] = known ? p.cos[at + i] : __builtin_nanf("");
             s[i] = known ? p.sin[at + i] : __builtin_nanf("");
-            lo[i] = __builtin_fmaf(a[i], c[i], -(b[i] * s[i]));
-            hi[i] = __builtin_fmaf(b[i], c[i], a[i] * s[i]);
         }
-        put8(p, query, h, m, slot, 8 * item, lo);
-        put8(p, query, h, m, slot, r + 8 * item, hi);
-        return;
     }
-    const int h = head - p.heads - p.kv_heads;
-    const float scale = p.fp8 && p.v_scale ? p.v_scale[h] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        const int head = first_head + i;
+        if (head >= p.heads + p.kv_heads) break;
+        const bool query = head < p.heads;
+        const int h = query ? head : head - p.heads;
+        float a[8];
+        unpack8(lo[i], a);
+        if (!turned) {
+            put8(p, query, h, m, slot, lo_dim, a);
+            continue;
+        }
+        float b[8], x[8], y[8];
+        unpack8(hi[i], b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = __builtin_fmaf(a[j], c[j], -(b[j] * s[j]));
+            y[j] = __builtin_fmaf(b[j], c[j], a[j] * s[j]);
+        }
+        put8(p, query, h, m, slot, lo_dim, x);
+        put8(p, query, h, m, slot, hi_dim, y);
+    }
+}
+
+// Values of one head: E tokens of a dim are 16 bytes of the cache, so the tokens of a workgroup are turned in LDS.  A lane then has
+// one dim of a run of tokens that end where a chunk of the cache ends; a whole chunk is one store, lines are written whole by
+// neighbouring lanes.  (Value by value, each lane waiting for its own, 4101 tokens took 64 us in all.)
+constexpr int kMaxTokens = 64;                         // tokens of a workgroup
+__device__ __forceinline__ void turn_values(const AppendArgs &p, int h, uint16_t *lds, int *slots) {
     const int64_t first = (int64_t)blockIdx.x * p.group;
-    const int count = (int)min((int64_t)p.group, p.M - first);
-    for (int i = threadIdx.x; i < count * p.D; i += kAppendThreads) {
-        const int token = i / p.D, d = i - token * p.D;
-        const int slot = p.slots[first + token];
-        if (slot < 0 || slot >= p.slot_count) continue;
-        const uint16_t v = p.new_v[(first + token) * p.ldv + (int64_t)h * p.D + d];
-        uint8_t *block = p.v + block_offset(p, slot, h);
-        const int t = slot & 15;
+    const int count = (int)min((int64_t)p.group, p.M - first), pieces = p.D / 8, ld = p.D + 8;
+    for (int i = threadIdx.x; i < count * pieces; i += kAppendThreads) {
+        const int token = i / pieces, piece = i - token * pieces;
+        *reinterpret_cast<u32x4 *>(lds + token * ld + 8 * piece) =
+            *reinterpret_cast<const u32x4 *>(p.new_v + (first + token) * p.ldv + (int64_t)h * p.D + 8 * piece);
+    }
+    if ((int)threadIdx.x < count) slots[threadIdx.x] = p.slots[first + threadIdx.x];
+    __syncthreads();
+    const float scale = p.fp8 && p.v_scale ? p.v_scale[h] : 1.0f;
+    const int chunk = p.fp8 ? 16 : 8, lead = slots[0] & (chunk - 1);         // the first run ends at a chunk's end
+    const int runs = (lead + count + chunk - 1) / chunk;
+    for (int i = threadIdx.x; i < runs * p.D; i += kAppendThreads) {
+        const int run = i / p.D, d = i - run * p.D;
+        const int from = max(run * chunk - lead, 0), to = min((run + 1) * chunk - lead, count);
+        const int start = slots[from];
+        bool whole = to - from == chunk && (start & (chunk - 1)) == 0 && start >= 0 && start < p.slot_count;
+        for (int t = from; whole && t < to; ++t) whole = slots[t] == start + t - from;
         if (p.fp8) {
-            const float q = quotient(half_bits_to_float(v), scale);
-            block[d * 16 + t] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false);
+            uint32_t w[4] = {0, 0, 0, 0};
+            for (int t = from; t < to; ++t) {
+                const float q = quotient(half_bits_to_float(lds[t * ld + d]), scale);
+                const uint32_t code = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false) & 0xffu;
+                const int j = t - from;
+                if (whole) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] |= j >> 2 == k ? code << (8 * (j & 3)) : 0u;
+                } else if (slots[t] >= 0 && slots[t] < p.slot_count) {
+                    p.v[block_offset(p, slots[t], h) + d * 16 + (slots[t] & 15)] = (uint8_t)code;
+                }
+            }
+            if (whole) *reinterpret_cast<u32x4 *>(p.v + block_offset(p, start, h) + d * 16) = u32x4{w[0], w[1], w[2], w[3]};
+        } else if (whole) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[k] = lds[(from + 2 * k) * ld + d] | (uint32_t)lds[(from + 2 * k + 1) * ld + d] << 16;
+            *reinterpret_cast<u32x4 *>(p.v + block_offset(p, start, h) + (((start >> 3) & 1) * p.D + d) * 16) = u32x4{w[0], w[1], w[2], w[3]};
         } else {
-            reinterpret_cast<uint16_t *>(block)[((t >> 3) * p.D + d) * 8 + (t & 7)] = v;
+            for (int t = from; t < to; ++t) {
+                const int slot = slots[t];
+                if (slot < 0 || slot >= p.slot_count) continue;
+                reinterpret_cast<uint16_t *>(p.v + block_offset(p, slot, h))[(((slot >> 3) & 1) * p.D + d) * 8 + (slot & 7)] = lds[t * ld + d];
+            }
         }
     }
 }
 
+// grid: (groups of tokens, heads of the values, then groups of heads of queries and keys)
+template <int HEADS>
+__global__ void __launch_bounds__(kAppendThreads)
+rope_append_kernel(AppendArgs p) {
+    __shared__ u32x4 lds[(16 * kAppendThreads + 8 * kMaxTokens) / 8];     // (16 dims to a lane at most, and 8 more for every token)
+    __shared__ int slots[kMaxTokens];
+    if ((int)blockIdx.y < p.kv_heads) turn_values(p, blockIdx.y, reinterpret_cast<uint16_t *>(lds), slots);
+    else rotate<HEADS>(p, (blockIdx.y - p.kv_heads) * HEADS);
+}
+
 int launch_rope_append(AppendArgs a, hipStream_t stream) {
     const int items = a.rotary / 16 + (a.D - a.rotary) / 8;
-    a.group = kAppendThreads / items;
-    const dim3 grid((unsigned)((a.M + a.group - 1) / a.group), (unsigned)(a.heads + 2 * a.kv_heads));
-    rope_append_kernel<<<grid, kAppendThreads, 0, stream>>>(a);
+    a.group = std::min(kAppendThreads / items, kMaxTokens);
+    const int heads = a.heads + a.kv_heads;
+    const int64_t groups = (a.M + a.group - 1) / a.group;
+    // four heads to a lane where there is work for the chip all the same
+    if (groups * heads >= 4096) {
+        rope_append_kernel<4><<<dim3((unsigned)groups, (unsigned)(a.kv_heads + (heads + 3) / 4)), kAppendThreads, 0, stream>>>(a);
+    } else {
+        rope_append_kernel<1><<<dim3((unsigned)groups, (unsigned)(a.kv_heads + heads)), kAppendThreads, 0, stream>>>(a);
+    }
     return hip_ok(hipGetLastError());
 }
 
