@@ -148,9 +148,8 @@ __device__ __forceinline__ Walk walk(const AttentionArgs &p, int low_pos, int hi
 // A workgroup's sums lie in the workspace as [tile][chunk][row]: D sums, then the maximum and the sum of the row's
 // probabilities.  They are stored past the caches (every XCD has an L2 of its own) before the tile's ticket is drawn;
 // the workgroup with the last ticket joins the chunks in a fixed order and leaves the counter cleared.  Nobody waits for anybody.
-// The joining workgroup first turns all maxima into weights, in `room` (kMaxChunks + 1 words for every row), then adds up with many
-// loads under way: one after the other, 64 chunks took about 40 us.
-constexpr int kMaxChunks = 256;
+// The joining workgroup has many loads under way, groups of its lanes take every so many chunks each: one after the other, 64 chunks took
+// about 40 us.
 __device__ __forceinline__ float2 pair_of(unsigned long long x) { return {__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))}; }
 __device__ __forceinline__ unsigned long long past_caches(const float *p) {
     return __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -159,7 +158,7 @@ __device__ __forceinline__ void past_caches(float *p, float a, float b) {
     __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32,
                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <int D, int THREADS, int ROWS>
+template <int D, int THREADS>
 __device__ __forceinline__ void join(const AttentionArgs &p, int thread, int tile, int chunks, const Sequence &sq, int row0, int row1, int past, int head,
                                      float v_scale, float *room, int *last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -171,57 +170,63 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int thread, int til
     }
     __syncthreads();
     if (!*last) return;
-    const int count = row1 - row0 + 1;
+    const int items = (row1 - row0 + 1) * (D / 4);     // four columns of a row
     constexpr int stride = D + 2;
     const float *parts = p.partials + (int64_t)tile * p.chunks * p.part_rows * stride;
-    // weights: a wave takes one row after the other, a lane four chunks
-    const int lane = thread & 63;
-    for (int r = thread >> 6; r < count; r += THREADS / 64) {
-        float m[4], l[4], top = kNegInf, sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = lane + 64 * i;
-            const float2 ml = pair_of(c < chunks ? past_caches(parts + ((int64_t)c * p.part_rows + r) * stride + D) : 0xff800000ull);
-            m[i] = ml.x;
-            l[i] = ml.y;
-            top = fmaxf(top, m[i]);
-        }
-        for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-        const float ref = fmaxf(top, -1e30f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float f = __builtin_amdgcn_exp2f(fmaxf(m[i], -1e30f) - ref);
-            if (lane + 64 * i < chunks) room[r * kMaxChunks + lane + 64 * i] = f;
-            sum += l[i] * f;
-        }
-        for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
-        if (lane == 0) room[ROWS * kMaxChunks + r] = v_scale / sum;
-    }
-    __syncthreads();
-    for (int item = thread; item < count * (D / 4); item += THREADS) {
-        const int r = item / (D / 4), d = 4 * (item - r * (D / 4));
-        const float *src = parts + r * stride + d;
-        const int64_t next = (int64_t)p.part_rows * stride;
-        const float *weight = room + r * kMaxChunks;
+    const int64_t next = (int64_t)p.part_rows * stride;
+    const int groups = max(1, min(THREADS / items, chunks));
+    for (int base = 0; base < items; base += THREADS) {
+        const int group = groups > 1 ? thread / items : 0, item = base + (groups > 1 ? thread - group * items : thread);
+        const int r = min(item, items - 1) / (D / 4), d = 4 * (min(item, items - 1) - r * (D / 4));
+        const float *src = parts + r * stride;
+        float top = kNegInf, sum = 0.0f;
         floatx4 acc = floatx4{0, 0, 0, 0};
         constexpr int N = 8;
-        for (int c = 0; c < chunks; c += N) {
-            unsigned long long x[N][2];
+        for (int c = group; c < chunks && group < groups; c += N * groups) {
+            float2 stat[N], a[N], b[N];
+            float now = top;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float *at = src + min(c + i, chunks - 1) * next;
-                x[i][0] = past_caches(at);
-                x[i][1] = past_caches(at + 2);
+                const float *at = src + min(c + i * groups, chunks - 1) * next;
+                stat[i] = pair_of(past_caches(at + D));
+                a[i] = pair_of(past_caches(at + d));
+                b[i] = pair_of(past_caches(at + d + 2));
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float f = c + i < chunks ? weight[c + i] : 0.0f;
-                const float2 a = pair_of(x[i][0]), b = pair_of(x[i][1]);
-                if (c + i < chunks) acc += floatx4{a.x, a.y, b.x, b.y} * f;
+            for (int i = 0; i < N; ++i)
+                if (c + i * groups < chunks) now = fmaxf(now, stat[i].x);
+            const float ref = fmaxf(now, -1e30f), f = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - ref);
+            sum *= f;
+            acc *= f;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (c + i * groups < chunks) {
+                    const float g = __builtin_amdgcn_exp2f(fmaxf(stat[i].x, -1e30f) - ref);
+                    sum += stat[i].y * g;
+                    acc += floatx4{a[i].x, a[i].y, b[i].x, b[i].y} * g;
+                }
+            top = now;
+        }
+        if (groups > 1) {                              // (then one round of the loop has all items)
+            if (group < groups) {
+                *reinterpret_cast<floatx4 *>(room + 8 * thread) = acc;
+                room[8 * thread + 4] = top;
+                room[8 * thread + 5] = sum;
+            }
+            __syncthreads();
+            if (group > 0) continue;
+            for (int i = 1; i < groups; ++i) {
+                const float *other = room + 8 * (thread + i * items);
+                const float now = fmaxf(top, other[4]), ref = fmaxf(now, -1e30f);
+                const float f = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(other[4], -1e30f) - ref);
+                sum = sum * f + other[5] * g;
+                acc = acc * f + *reinterpret_cast<const floatx4 *>(other) * g;
+                top = now;
             }
         }
+        if (item >= items) continue;
         const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
-        const float f = room[ROWS * kMaxChunks + r];
+        const float f = v_scale / sum;
         *reinterpret_cast<u32x2 *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) = past + i < 0 ? u32x2{0u, 0u} :
             u32x2{float2_to_half2_bits(acc[0] * f, acc[1] * f), float2_to_half2_bits(acc[2] * f, acc[3] * f)};
     }
@@ -229,11 +234,10 @@ __device__ __forceinline__ void join(const AttentionArgs &p, int thread, int til
 
 // ---- who does what --------------------------------------------------------------------------------------------------------------
 // The host does not know the sequences' lengths (a captured graph is replayed as they grow), so every workgroup of the streaming
-// kernel works out the same schedule from them, one sequence per thread: how many blocks there are in all, from that the stretch that one
-// workgroup takes, and where each sequence's stretches begin in a list that the workgroups walk.  A launch over all
-// stretches that the largest length would have costs 1 to 2 us for every few hundred that turn out empty.
-// (Every wave does it by itself, with four sequences to a lane and sums by DPP moves: through LDS, with barriers and shuffles,
-// it took 3 us.)
+// kernel works out the same schedule from them: the blocks of all tiles of rows in one row, of which each workgroup takes a stretch of
+// the same length, which may end one tile and begin the next.  Equal shares for two workgroups per CU: with three, loads wait for each other
+// (7 us instead of 2), and so does every step of the prologue and of the join; with one launch of all stretches that the
+// largest length would have, those that turn out empty cost 1 to 2 us for every few hundred.
 constexpr int kScan = 256;
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int plus_before(int v) {
@@ -262,60 +266,53 @@ __device__ __forceinline__ float sum_of_lanes(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 struct Schedule {
-    int begin[kScan / 64];                             // of sequence 64 i + lane in the list
-    int items, chunk_blocks;
+    int begin[kScan / 64];                             // of sequence 64 i + lane in the row of all blocks
+    int all, share;                                    // blocks, and of them a workgroup's
 };
+__device__ __forceinline__ int up_to(int v, int multiple) { return (v + multiple - 1) / multiple * multiple; }
+// blocks that a tile of a sequence's rows has in the row: whole steps
+__device__ __forceinline__ int padded_blocks(const AttentionArgs &p, const Sequence &sq, int least) {
+    return up_to(max(1, walk(p, sq.length - sq.fresh, sq.length - 1).blocks), least);
+}
 __device__ __forceinline__ Schedule schedule(const AttentionArgs &p, int tile_rows, int least) {
     constexpr int N = kScan / 64;
     const int lane = threadIdx.x & 63;
     Schedule plan;
-    int tiles[N], blocks[N];                           // of this lane's sequences; tiles: of rows, over all heads
-    float work = 0.0f, lists = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int t = 64 * i + lane;
-        tiles[i] = blocks[i] = 0;
-        if (64 * i >= p.batch) continue;
-        const Sequence sq = sequence(p, min(t, p.batch - 1));
-        const int rows = sq.fresh * p.group;
-        if (t < p.batch && rows > 0 && !(p.few > 0 && rows > p.few)) {
-            tiles[i] = (rows + tile_rows - 1) / tile_rows * p.kv_heads;
-            blocks[i] = walk(p, sq.length - sq.fresh, sq.length - 1).blocks;
-        }
-        work += (float)tiles[i] * (float)blocks[i];
-        lists += (float)tiles[i];
-    }
-    plan.chunk_blocks = p.chunk_blocks;
-    if (!p.fixed) {
-        work = sum_of_lanes(work);
-        lists = sum_of_lanes(lists);
-        // As many stretches as there are workgroups, or twice that; on average half of one is lost where each list ends.
-        const float slots = (float)gridDim.x;
-        const float wanted = 2.0f * lists <= slots ? slots - 0.5f * lists : fmaxf(2.0f * slots - 0.5f * lists, slots);
-        const int even = (int)fminf(work / wanted, 1e8f) + 1;
-        plan.chunk_blocks = __builtin_amdgcn_readfirstlane(max(plan.chunk_blocks, (even + least - 1) / least * least));
-    }
-    plan.items = 0;
+    plan.all = 0;
+    uint32_t longest = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         plan.begin[i] = 0x7fffffff;
         if (64 * i >= p.batch) continue;
-        const int count = tiles[i] * min(p.chunks, max(1, (blocks[i] + plan.chunk_blocks - 1) / plan.chunk_blocks)), sum = sum_to_lane(count);
-        plan.begin[i] = plan.items + sum - count;
-        plan.items += __builtin_amdgcn_readlane(sum, 63);
+        const int t = 64 * i + lane;
+        const Sequence sq = sequence(p, min(t, p.batch - 1));
+        const int rows = sq.fresh * p.group;
+        int blocks = 0;
+        if (t < p.batch && rows > 0 && !(p.few > 0 && rows > p.few)) {
+            const int each = padded_blocks(p, sq, least);
+            longest = max(longest, (uint32_t)each);
+            blocks = each * ((rows + tile_rows - 1) / tile_rows * p.kv_heads);
+        }
+        const int sum = sum_to_lane(blocks);
+        plan.begin[i] = plan.all + sum - blocks;
+        plan.all += __builtin_amdgcn_readlane(sum, 63);
     }
+    plan.share = p.chunk_blocks;
+    if (!p.fixed) plan.share = max(plan.share, (plan.all + (int)gridDim.x - 1) / (int)gridDim.x);
+    // (a tile's parts have to fit the workspace, also where a sequence is longer than the launch was sized for)
+    plan.share = up_to(max(plan.share, ((int)max_of_wave(longest) + p.chunks - 2) / max(p.chunks - 1, 1)), least);
     return plan;
 }
-// the sequence of an item of the list, and the item's place among the sequence's
-__device__ __forceinline__ int place_of(const Schedule &plan, int item, int batch, int &b) {
+// the sequence that a block of the row belongs to, and the block's place among the sequence's
+__device__ __forceinline__ int place_of(const Schedule &plan, int x, int batch, int &b) {
     int at = -1, first = 0;
 #pragma unroll
-    for (int i = 0; i < kScan / 64; ++i) at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.begin[i] <= item));
+    for (int i = 0; i < kScan / 64; ++i) at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.begin[i] <= x));
     b = min(at, batch - 1);                            // (lanes behind the last sequence begin where it ends)
 #pragma unroll
     for (int i = 0; i < kScan / 64; ++i)
         if (b >> 6 == i) first = __builtin_amdgcn_readlane(plan.begin[i], b & 63);
-    return item - first;
+    return x - first;
 }
 
 // ---- streaming kernel -------------------------------------------------------------------------------------------------------
@@ -334,9 +331,9 @@ attention_stream_kernel(AttentionArgs p) {
     constexpr int QS = FP8 ? 2 * KL : KL;              // operands of 32 dims
     constexpr int DB = D / 16;
     constexpr int LD = D + 4;
-    // the waves' sums on their way together, then the join's weights
-    constexpr int PART = 4 * 16 * RT * LD, ROOM = 16 * RT * (kMaxChunks + 1);
-    __shared__ float shared[PART > ROOM ? PART : ROOM];
+    // the waves' sums on their way together, then the groups' of the join (8 words for every lane)
+    __shared__ __align__(16) float shared[4 * 16 * RT * LD];
+    static_assert(4 * 16 * RT * LD >= 8 * 256, "");
     float (*part)[16 * RT][LD] = reinterpret_cast<float (*)[16 * RT][LD]>(shared);
     __shared__ float stat[4][2][16 * RT];
     __shared__ int last;
@@ -344,31 +341,38 @@ attention_stream_kernel(AttentionArgs p) {
     constexpr int LEAST = 4 * NT;                      // blocks: one step of each wave
     Schedule plan;
     if (p.scan) plan = schedule(p, 16 * RT, LEAST);
-    else plan.items = gridDim.x, plan.chunk_blocks = p.chunk_blocks;
-    const int items = plan.items, chunk_blocks = plan.chunk_blocks;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    else plan.all = gridDim.x, plan.share = 1;
+    // (without a schedule: a workgroup is a chunk of a tile)
+    for (int first = blockIdx.x; (int64_t)first * plan.share < plan.all; first += gridDim.x)
+    for (int x = first * plan.share, end = min(plan.all, x + plan.share); x < end;) {
     __syncthreads();
     // (hidden from the compiler, which otherwise works out before the loop what every lane needs in it, and keeps it in 40 registers)
     int thread = threadIdx.x;
     asm volatile("" : "+v"(thread));
     const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), group = lane >> 4, col = lane & 15;
-    int chunk, rt0, head, b;
+    int chunk, rt0, head, b, offset_in_tile, here;        // (blocks of the tile before this stretch, and in it)
     Sequence sq;
     if (p.scan) {
-        const int mine = place_of(plan, item, p.batch, b);
+        const int mine = place_of(plan, x, p.batch, b);
         sq = sequence(p, b);
-        const int tiles = (sq.fresh * p.group + 16 * RT - 1) / (16 * RT);
-        head = mine % p.kv_heads;
-        rt0 = mine / p.kv_heads % tiles;
-        chunk = mine / p.kv_heads / tiles;
+        const int each = padded_blocks(p, sq, LEAST), index = mine / each;
+        offset_in_tile = mine - index * each;
+        here = min(end - x, each - offset_in_tile);
+        head = index % p.kv_heads;
+        rt0 = index / p.kv_heads;
+        chunk = x / plan.share - (x - offset_in_tile) / plan.share;
     } else {
         const int tiles = p.batch * p.kv_heads * p.row_tiles;
-        chunk = item / tiles;
-        head = item % p.kv_heads;
-        rt0 = item % tiles / p.kv_heads % p.row_tiles;
-        b = item % tiles / p.kv_heads / p.row_tiles;
+        chunk = x / tiles;
+        head = x % p.kv_heads;
+        rt0 = x % tiles / p.kv_heads % p.row_tiles;
+        b = x % tiles / p.kv_heads / p.row_tiles;
         sq = sequence(p, b);
+        offset_in_tile = chunk * p.chunk_blocks;
+        here = 1;
     }
+    const int start_of_tile = x - offset_in_tile;
+    x += here;
     const int tile = (b * p.row_tiles + rt0) * p.kv_heads + head;
     const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
     if (row0 >= rows || (p.few > 0 && rows > p.few)) continue;   // (the tile kernel's)
@@ -376,10 +380,17 @@ attention_stream_kernel(AttentionArgs p) {
     const int past = sq.length - sq.fresh;
     const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
     const Walk w = walk(p, low_pos, high_pos);
-    // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
-    const int chunks = min(p.chunks, max(1, (w.blocks + chunk_blocks - 1) / chunk_blocks));
+    int chunks, v1;
+    const int v0 = offset_in_tile;
+    if (p.scan) {
+        chunks = (start_of_tile + max(w.blocks, 1) - 1) / plan.share - start_of_tile / plan.share + 1;
+        v1 = min(w.blocks, v0 + here);
+    } else {
+        // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
+        chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+        v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
+    }
     if (chunk >= chunks) continue;
-    const int v0 = chunk * chunk_blocks, v1 = chunk == chunks - 1 ? w.blocks : v0 + chunk_blocks;
 
     // queries, as the second operand: column = row, dims in the order in which the keys' chunks come
     int row[RT], pos[RT], low[RT];
@@ -669,7 +680,7 @@ attention_stream_kernel(AttentionArgs p) {
         }
     }
     if (chunks == 1) continue;
-    join<D, 256, 16 * RT>(p, thread, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
+    join<D, 256>(p, thread, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
     }
 }
 
@@ -1157,7 +1168,6 @@ static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t til
     if (chunk < least) chunk = least;
     chunk = (chunk + least - 1) / least * least;
     if (tickets && a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
-    if (tickets && chunk * kMaxChunks < blocks) chunk = ((blocks + kMaxChunks - 1) / kMaxChunks + least - 1) / least * least;
     a.chunk_blocks = chunk;
     a.chunks = (blocks + chunk - 1) / chunk;
     a.partial_bytes = a.chunks > 1 ? (size_t)a.tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
@@ -1167,6 +1177,7 @@ AttentionPlan attention_plan(const AttentionShape &s) {
     AttentionPlan a;
     const int64_t rows = s.max_new * s.group, stream_rows = s.D > 128 ? 16 : 32;      // (two tiles of 256 dims do not fit the registers)
     a.few = 0;
+    a.scan = false;
     a.stream.tiles = a.tile.tiles = 0;
     a.stream.partial_bytes = a.tile.partial_bytes = 0;
     const bool many = s.D <= 128 && (tuning().attn_tiles >= 0 ? tuning().attn_tiles > 0 : rows > stream_rows);
@@ -1197,6 +1208,14 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.stream.tiles = s.batch * s.kv_heads * a.stream.row_tiles;
         a.stream.part_rows = most < 16 * a.rt ? most : 16 * a.rt;
         plan_launch(a.stream, s, 16 * a.rt, a.stream.tiles, s.fp8 ? 16 : 8, s.batch <= kScan ? 4096 : 1536, true);
+        // a schedule worked out by the workgroups, unless there is nothing to share out; its parts of a tile are one more, since a tile
+        // may begin anywhere in a stretch
+        AttentionLaunch &l = a.stream;
+        a.scan = s.batch <= kScan && l.chunks > 1;
+        if (a.scan) {
+            l.chunks += 1;
+            l.partial_bytes = (size_t)l.tiles * (size_t)l.chunks * (size_t)l.part_rows * (size_t)(s.D + 2) * sizeof(float);
+        }
     }
     a.partial_bytes = a.stream.partial_bytes > a.tile.partial_bytes ? a.stream.partial_bytes : a.tile.partial_bytes;
     return a;
@@ -1259,10 +1278,10 @@ int launch_attention(const AttentionShape &s, const AttentionPlan &plan, Attenti
     }
     if (plan.stream.tiles > 0) {
         if (!shape_of(plan.stream, a, grid)) return kErrShape;
-        a.scan = s.batch <= kScan && plan.stream.chunks > 1;
+        // (the lengths are bounded by the table alone, and the blocks of all tiles are counted in 31 bits)
+        a.scan = plan.scan && plan.stream.tiles * (((int64_t)a.columns << a.page_shift) + 16) < (int64_t)1 << 30;
         a.fixed = tuning().attn_chunk > 0;
-        // (what the chip holds at once: three workgroups per CU, two of the larger ones)
-        if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, plan.rt == 1 && s.D <= 128 ? 768 : 512));
+        if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, tuning().attn_groups > 0 ? tuning().attn_groups : 512));
 #define NFP_STREAM(D, FP8) launch_stream<D, FP8>(plan.rt, a, grid, stream)
         NFP_FOR_D(NFP_STREAM)
 #undef NFP_STREAM

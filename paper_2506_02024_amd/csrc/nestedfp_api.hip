@@ -12,7 +12,7 @@
 namespace nfp {
 
 Tuning &tuning() {
-    static Tuning t = {-1, -1, -1, -1, -1, -1, -1, -1, -1, 1, -1, -1, -1, -1, -1, -1, -1, -1, -1, -1};
+    static Tuning t = {-1, -1, -1, -1, -1, -1, -1, -1, -1, 1, -1, -1, -1, -1, -1, -1, -1, -1, -1, -1, -1};
     return t;
 }
 
@@ -691,7 +691,7 @@ int nestedfp_probe_mfma(const void *operands, int fp8, int iters, uint32_t *sink
 
 static const char *const kKnobs[] = {"small_max_m", "small_split", "small_spw", "small_tiles", "small_interleave",
                                      "large_split", "large_bm", "large_bn", "small_fuse_quant", "quant_hw", "large_xcd_map",
-                                     "fused_reduce", "large_deep", "large_height", "large_rows", "tuned_table", "quant_onepass", "attn_tiles", "attn_waves", "attn_chunk", nullptr};
+                                     "fused_reduce", "large_deep", "large_height", "large_rows", "tuned_table", "quant_onepass", "attn_tiles", "attn_waves", "attn_groups", "attn_chunk", nullptr};
 
 const char *nestedfp_tune_name(int index) {
     if (index < 0 || index >= (int)(sizeof(kKnobs) / sizeof(kKnobs[0]))) return nullptr;
@@ -721,6 +721,7 @@ int nestedfp_tune(const char *knob, int64_t value) {
     else if (!strcmp(knob, "quant_onepass")) t.quant_onepass = value;
     else if (!strcmp(knob, "attn_tiles")) t.attn_tiles = value;
     else if (!strcmp(knob, "attn_waves")) t.attn_waves = value;
+    else if (!strcmp(knob, "attn_groups")) t.attn_groups = value;
     else if (!strcmp(knob, "attn_chunk")) t.attn_chunk = value;
     else return NESTEDFP_ERR_ARG;
     // after the knob: a launch shape worked out from its old value is remembered under the old count

@@ -89,6 +89,7 @@ struct Tuning {
     int64_t quant_onepass;   // 1 / 0: force / forbid the single-pass activation quantisation (rows kept in registers) where it fits
     int64_t attn_tiles;      // 1 / 0: attention by the tile kernel / by the streaming kernel whatever the number of rows
     int64_t attn_waves;      // waves per workgroup of the tile kernel (4 or 8), 32 rows each
+    int64_t attn_groups;     // workgroups of the streaming attention kernel where they work out who does what
     int64_t attn_chunk;      // tokens of the cache per workgroup of the attention kernels, rounded up to what their waves take in a step
 };
 Tuning &tuning();
@@ -245,7 +246,7 @@ struct AttentionArgs {
 struct AttentionShape { int64_t tokens, batch, kv_heads, group, D, max_new, max_len, window, sinks;  bool fp8, ragged; };
 struct AttentionLaunch { int64_t row_tiles, part_rows, chunk_blocks, chunks, tiles;  size_t partial_bytes; };
 // few > 0: sequences of up to `few` rows go to the streaming kernel, the others to the tile kernel
-struct AttentionPlan { AttentionLaunch stream, tile;  int64_t few, rt, waves;  size_t partial_bytes; };
+struct AttentionPlan { AttentionLaunch stream, tile;  int64_t few, rt, waves;  bool scan;  size_t partial_bytes; };
 AttentionPlan attention_plan(const AttentionShape &s);
 int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream);
 
