@@ -764,7 +764,7 @@ __device__ __forceinline__ TilePlace tile_place(const AttentionArgs &p, int tile
 }
 
 template <int D, bool FP8, int NW, int TK>
-__global__ void __launch_bounds__(64 * NW, 2)
+__global__ void __launch_bounds__(64 * NW, D > 128 ? 1 : 2)
 attention_tile_kernel(AttentionArgs p) {
     constexpr int T = 64 * NW, NB = TK / 16, HB = TK / 32;       // threads, blocks and halves (of 32 tokens) of a tile of tokens
     constexpr int CB = FP8 ? D : 2 * D;                          // 16-byte chunks of a block in memory
@@ -1180,12 +1180,16 @@ AttentionPlan attention_plan(const AttentionShape &s) {
     a.scan = false;
     a.stream.tiles = a.tile.tiles = 0;
     a.stream.partial_bytes = a.tile.partial_bytes = 0;
-    const bool many = s.D <= 128 && (tuning().attn_tiles >= 0 ? tuning().attn_tiles > 0 : rows > stream_rows);
+    const bool many = tuning().attn_tiles >= 0 ? tuning().attn_tiles > 0 : rows > stream_rows;
     if (many) {
         // sequences of few rows beside the others: none if all have as many new tokens
         a.few = s.ragged && rows > stream_rows && s.group <= stream_rows ? stream_rows : 0;
         const int64_t total = s.tokens * s.group;
-        a.waves = tuning().attn_waves > 0 ? tuning().attn_waves : (total + 255) / 256 * s.kv_heads >= 512 ? 8 : 4;
+        // 128-row tiles where 256-row tiles would leave CUs without work, unless the sequences are long, whose keys and values are then
+        // read twice as often: 777 tokens of 64 dims 17.0 against 18.5 us, a prompt of 2048 65.8 / 68.4; 512 tokens after 8192
+        // 100 against 89.  (256 dims: the sums of 32 rows fill the registers of a SIMD.)
+        a.waves = s.D > 128 ? 4 : tuning().attn_waves > 0 ? tuning().attn_waves :
+                  (total + 255) / 256 * s.kv_heads >= 512 || s.max_len >= 4096 ? 8 : 4;
         const int64_t tile_rows = 32 * a.waves;
         int64_t most = s.batch * ((rows + tile_rows - 1) / tile_rows), likely = most;
         if (s.ragged) {
@@ -1199,11 +1203,12 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.tile.row_tiles = most;
         a.tile.tiles = most * s.kv_heads;
         a.tile.part_rows = tile_rows;
-        plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, 16, a.waves == 8 ? 256 : 512, false);
+        plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, 16, a.waves == 8 || s.D > 128 ? 256 : 512, false);
     }
     if (!many || a.few > 0) {
         const int64_t most = many ? a.few / s.group * s.group : rows;
-        a.rt = most <= 16 || s.D > 128 ? 1 : 2;
+        // (beside prompt chunks most sequences have one new token; the others read their keys and values twice)
+        a.rt = most <= 16 || many || s.D > 128 ? 1 : 2;
         a.stream.row_tiles = (most + 16 * a.rt - 1) / (16 * a.rt);
         a.stream.tiles = s.batch * s.kv_heads * a.stream.row_tiles;
         a.stream.part_rows = most < 16 * a.rt ? most : 16 * a.rt;
@@ -1245,17 +1250,16 @@ static void launch_stream(int64_t rt, const AttentionArgs &a, dim3 grid, hipStre
 
 template <int D, bool FP8>
 static int launch_tile(int64_t waves, const AttentionArgs &a, dim3 grid, hipStream_t stream) {
+    constexpr int TK = D <= 128 ? 64 : 32, LDS = 8 * TK * D;         // two buffers of keys and values in FP16
+    static_assert(LDS <= 65536, "");
     if constexpr (D <= 128) {
-        constexpr int TK = 64, LDS = 8 * TK * D;                     // two buffers of keys and values in FP16
-        static_assert(LDS <= 65536, "");
         if (waves == 8) attention_tile_kernel<D, FP8, 8, TK><<<grid, 512, LDS, stream>>>(a);
-        else attention_tile_kernel<D, FP8, 4, TK><<<grid, 256, LDS, stream>>>(a);
-        const int st = hip_ok(hipGetLastError());
-        if (a.chunks == 1 || st != kOk) return st;
-        attention_join_kernel<D><<<dim3(grid.x / a.chunks * waves), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
-        return hip_ok(hipGetLastError());
     }
-    return kErrShape;
+    if (waves == 4) attention_tile_kernel<D, FP8, 4, TK><<<grid, 256, LDS, stream>>>(a);
+    const int st = hip_ok(hipGetLastError());
+    if (a.chunks == 1 || st != kOk) return st;
+    attention_join_kernel<D><<<dim3(grid.x / a.chunks * waves), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
+    return hip_ok(hipGetLastError());
 }
 
 int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream) {
@@ -1281,7 +1285,7 @@ int launch_attention(const AttentionShape &s, const AttentionPlan &plan, Attenti
         // (the lengths are bounded by the table alone, and the blocks of all tiles are counted in 31 bits)
         a.scan = plan.scan && plan.stream.tiles * (((int64_t)a.columns << a.page_shift) + 16) < (int64_t)1 << 30;
         a.fixed = tuning().attn_chunk > 0;
-        if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, tuning().attn_groups > 0 ? tuning().attn_groups : 512));
+        if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, tuning().attn_groups > 0 ? tuning().attn_groups : plan.stream.tiles <= 128 ? 256 : 512));
 #define NFP_STREAM(D, FP8) launch_stream<D, FP8>(plan.rt, a, grid, stream)
         NFP_FOR_D(NFP_STREAM)
 #undef NFP_STREAM

@@ -60,7 +60,7 @@ def test_window_and_sinks(nfp, knobs, window, sinks, fp8):
 
 
 @pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
-@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
 @pytest.mark.parametrize("chunk", [256, 512, 100000])
 def test_split_over_workgroups(nfp, knobs, chunk, d, fp8):
     news, lens = [70, 1, 300, 40], [1500, 700, 300, 41]
@@ -74,7 +74,7 @@ def test_split_over_workgroups(nfp, knobs, chunk, d, fp8):
 
 
 @pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
-@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_few_rows_by_tiles_and_many_by_the_streaming_kernel(nfp, knobs, d, fp8):
     for tiles, lens, news in ((1, [1, 2, 15, 16, 17, 33, 64, 100, 257, 700], [1] * 10), (1, [0, 5, 2, 40], [3] * 4), (0, [90, 300], [90, 40])):
         knobs(attn_tiles=tiles)
@@ -102,7 +102,7 @@ def test_an_entry_outside_the_cache_gives_nan_where_it_is_seen(nfp):
 
 
 @pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
-@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_a_value_that_is_not_finite_reaches_no_row_before_it(nfp, knobs, d, fp8):
     lens, news = [600, 600], [200, 200]
     cache, table, q = _case(lens, news, 4, 2, d, 32, fp8)
