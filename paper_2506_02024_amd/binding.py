@@ -1,4 +1,5 @@
-"""Python binding of the NestedFP C ABI (include/nestedfp.h): argument marshalling only.
+"""Python binding of the NestedFP C ABI (include/nestedfp.h): argument marshalling only, by ctypes and, for the calls that
+stand between a layer's linears, by a small compiled module (csrc/marshal.cpp).
 
 Tensors are torch CUDA tensors (device memory and the current stream come from
 PyTorch); every computation runs in the HIP library.  The library is loaded on first
@@ -20,6 +21,7 @@ WORKSPACE_COUNTER_BYTES = 16384
 OK, ERR_ARG, ERR_SHAPE, ERR_RANGE, ERR_WORKSPACE, ERR_HIP = range(6)
 
 _lib = None
+_marshal = None
 
 
 class NestedFPError(RuntimeError):
@@ -114,6 +116,23 @@ def lib():
     L.nestedfp_tune_name.argtypes = [ci]
     _lib = L
     return L
+
+
+def _marshalled():
+    """The compiled part of this binding (csrc/marshal.cpp), bound to the loaded library: the calls that stand between
+    a layer's linears, whose checks cost more in Python than a small kernel takes."""
+    global _marshal
+    if _marshal is None:
+        L = lib()
+        if not os.path.exists(_build.MARSHAL):
+            raise RuntimeError("the binding's compiled part is not built: %s is missing; run "
+                               "`python -c 'import __graft_entry__ as g; g.build()'` first" % _build.MARSHAL)
+        from . import _marshal as m
+
+        m.bind(*(ctypes.cast(getattr(L, "nestedfp_" + name), ctypes.c_void_p).value
+                 for name in ("add_rms_norm", "rope_append", "paged_attention")))
+        _marshal = m
+    return _marshal
 
 
 def status_string(status):
@@ -478,46 +497,14 @@ def linear(X, layer, mode, act_scale=None, out=None, workspace=None):
     return out
 
 
-_F16, _F32, _I32, _U8 = torch.float16, torch.float32, torch.int32, torch.uint8
-
-
-def _like(t, shape, name):
-    """(address, row stride) of a float16 matrix that has to have a shape."""
-    ld, inner = t.stride()
-    if t.shape != shape or t.dtype is not _F16 or inner != 1:
-        raise ValueError("%s must be float16 %s with unit inner stride" % (name, tuple(shape)))
-    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
-
-
 def add_rms_norm(X, weight, eps=1e-5, residual=None, sum_out=None, out=None, Xq=None, scales=None):
     """h = fp16(X + residual), y = h / sqrt(mean(h^2) + eps) * weight over the rows of X (fp16 [M,K]).
 
     Writes those of sum_out (h; may be residual or X), out (fp16 y), Xq (uint8 [M,K], E4M3 codes of y) with scales (float32
     [M]) that are given, and returns (out, Xq, scales, sum_out).  With neither out nor Xq, out is made."""
-    shape = X.shape
-    if len(shape) != 2 or X.dtype is not _F16:
-        raise ValueError("X must be float16 [M,K]")
-    M, K = shape
-    x, ldx = _like(X, shape, "X")
-    if weight.dtype is not _F16 or weight.numel() != K or not weight.is_contiguous():
-        raise ValueError("weight must be a contiguous float16 [K] tensor")
     if out is None and Xq is None:
-        out = torch.empty((M, K), dtype=_F16, device=X.device)
-    r = h = y = q = s = None
-    ldr = ldh = ldy = 0
-    if residual is not None:
-        r, ldr = _like(residual, shape, "residual")
-    if sum_out is not None:
-        h, ldh = _like(sum_out, shape, "sum_out")
-    if out is not None:
-        y, ldy = _like(out, shape, "out")
-    if Xq is not None:
-        if Xq.dtype is not _U8 or Xq.shape != shape or not Xq.is_contiguous():
-            raise ValueError("Xq must be a contiguous uint8 [M,K] tensor")
-        if scales is None or scales.dtype is not _F32 or scales.numel() != M or not scales.is_contiguous():
-            raise ValueError("scales must be a contiguous float32 [M] tensor")
-        q, s = Xq.data_ptr(), scales.data_ptr()
-    st = (_lib or lib()).nestedfp_add_rms_norm(x, M, K, ldx, r, ldr, weight.data_ptr(), eps, h, ldh, y, ldy, q, s, _stream())
+        out = torch.empty(X.shape, dtype=torch.float16, device=X.device)
+    st = (_marshal or _marshalled()).add_rms_norm(X, weight, eps, residual, sum_out, out, Xq, scales, _stream())
     if st:
         raise NestedFPError(st, "nestedfp_add_rms_norm")
     return out, Xq, scales, sum_out
@@ -568,7 +555,7 @@ class KVCache:
         self._c = _CacheStruct(self.pages, self.page_tokens, self.kv_heads, self.head_dim,
                                CACHE_FP16 if k.dtype == torch.float16 else CACHE_E4M3, k.data_ptr(), v.data_ptr(),
                                _ptr(k_scale), _ptr(v_scale))
-        self._ref = ctypes.byref(self._c)
+        self._ref, self._at = ctypes.byref(self._c), ctypes.addressof(self._c)
         if pages and not lib().nestedfp_kv_cache_bytes(self._ref):
             raise ValueError("a cache has pages of 16, 32, 64, 128 or 256 tokens and heads of 64, 96, 128 or 256 dims")
 
@@ -581,48 +568,13 @@ class KVCache:
         return self.v.permute(0, 2, 3, 5, 1, 4)
 
 
-def _heads(t, dim, name):
-    """(rows, heads, address, row stride) of a float16 [tokens, heads * head_dim] matrix."""
-    rows, cols = t.shape
-    ld, inner = t.stride()
-    if t.dtype is not _F16 or inner != 1 or cols == 0 or cols % dim:
-        raise ValueError("%s must be float16 [tokens, heads * head_dim]" % name)
-    return rows, cols // dim, t.data_ptr(), ld if rows > 1 else max(ld, cols)
-
-
-def _indices(t, n, name):
-    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of %d" % (name, n))
-    return t.data_ptr()
-
-
 def rope_append(q, k, v, positions, slots, cache, cos=None, sin=None, out=None):
     """Rotates the heads of q (fp16 [M, heads * head_dim]) and k by the rows of cos and sin (float32 [positions, rotary_dim / 2];
     None: no rotation) at `positions` (int32 [M]), and writes k and v ([M, kv_heads * head_dim]) to `slots` (int32 [M]) of the
     cache.  Returns the rotated q (out, which may be q; made if None)."""
-    dim, kv = cache.head_dim, cache.kv_heads
-    M, heads, q_at, ldq = _heads(q, dim, "q")
-    rows_k, kv_k, k_at, ldk = _heads(k, dim, "k")
-    rows_v, kv_v, v_at, ldv = _heads(v, dim, "v")
-    if rows_k != M or rows_v != M or kv_k != kv or kv_v != kv:
-        raise ValueError("k and v must be [tokens, kv_heads * head_dim] of the cache")
-    known = rotary = 0
-    c = s = at = None
-    if cos is not None and sin is not None:
-        known, pairs = shape = cos.shape
-        if cos.dtype is not _F32 or sin.dtype is not _F32 or sin.shape != shape or not (cos.is_contiguous() and sin.is_contiguous()):
-            raise ValueError("cos and sin must be contiguous float32 [positions, rotary_dim / 2] tensors")
-        c, s, rotary = cos.data_ptr(), sin.data_ptr(), 2 * pairs
-        at = _indices(positions, M, "positions")
-    elif cos is not None or sin is not None:
-        raise ValueError("cos and sin go together")
     if out is None:
-        out = torch.empty((M, heads * dim), dtype=_F16, device=q.device)
-    rows_o, heads_o, o_at, ldo = _heads(out, dim, "out")
-    if rows_o != M or heads_o != heads:
-        raise ValueError("out must have the shape of q")
-    st = (_lib or lib()).nestedfp_rope_append(q_at, ldq, k_at, ldk, v_at, ldv, M, heads, c, s, known, rotary, at,
-                                              _indices(slots, M, "slots"), o_at, ldo, cache._ref, _stream())
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+    st = (_marshal or _marshalled()).rope_append(q, k, v, positions, slots, cache._at, cos, sin, out, _stream())
     if st:
         raise NestedFPError(st, "nestedfp_rope_append")
     return out
@@ -641,32 +593,19 @@ def paged_attention(q, cache, table, lens, starts=None, max_new=None, max_len=No
     the last; starts: int32 [batch + 1], rows of q at which the sequences begin (None: as many for each).  max_new and max_len bound
     the sequences' new tokens and lengths (None: what the shapes of q and table allow; a tight max_len makes a better launch).
     scale: head_dim ** -0.5 if None.  window, sinks: see include/nestedfp.h."""
-    dim = cache.head_dim
-    tokens, heads, q_at, ldq = _heads(q, dim, "q")
-    rows, columns = table.shape
-    ld_table, inner = table.stride()
-    if table.dtype is not _I32 or inner != 1 and columns > 1:
-        raise ValueError("table must be int32 with unit inner stride")
-    if rows <= 1 or columns == 0:
-        ld_table = max(ld_table, columns)
-    lens_at = _indices(lens, rows, "lens")
-    starts_at = None if starts is None else _indices(starts, rows + 1, "starts")
     if max_new is None:
-        max_new = tokens if starts is not None else tokens // max(rows, 1)
+        max_new = q.shape[0] if starts is not None else q.shape[0] // max(lens.shape[0], 1)
     if max_len is None:
-        max_len = columns * cache.page_tokens
+        max_len = table.shape[1] * cache.page_tokens
+    if scale is None:
+        scale = cache.head_dim ** -0.5
     if out is None:
-        out = torch.empty((tokens, heads * dim), dtype=_F16, device=q.device)
-    rows_o, heads_o, o_at, ldo = _heads(out, dim, "out")
-    if rows_o != tokens or heads_o != heads:
-        raise ValueError("out must have the shape of q")
-    L = _lib or lib()
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
     if workspace is None:
-        workspace = _workspace(L.nestedfp_paged_attention_workspace_size(tokens, rows, heads, cache._ref, max_new, max_len, window, sinks),
-                               q.device)
-    st = L.nestedfp_paged_attention(q_at, tokens, ldq, heads, cache._ref, table.data_ptr(), ld_table, columns, lens_at, rows, starts_at,
-                                    max_new, max_len, dim ** -0.5 if scale is None else scale, window, sinks, o_at, ldo,
-                                    workspace.data_ptr(), workspace.numel(), _stream())
+        workspace = _workspace(paged_attention_workspace_size(q.shape[0], q.shape[1] // cache.head_dim, cache, lens.shape[0], max_new, max_len,
+                                                              window, sinks), q.device)
+    st = (_marshal or _marshalled()).paged_attention(q, cache._at, table, lens, starts, max_new, max_len, scale, window, sinks, out, workspace,
+                                                     _stream())
     if st:
         raise NestedFPError(st, "nestedfp_paged_attention")
     return out

@@ -98,3 +98,33 @@ def test_attention_workspace_does_not_grow_with_the_cache(nfp):
     assert size(4, 4, 5, ctypes.byref(_cache(nfp)), 1, 100, 0, 0) == 0
     assert size(4, 4, 4, None, 1, 100, 0, 0) == 0
     assert size(4, 4, 4, ctypes.byref(_cache(nfp)), 1, 16, 0, 0) == 0          # nothing to split
+
+
+def test_the_binding_refuses_what_is_not_on_the_gpu_or_has_another_shape(nfp):
+    import torch
+
+    x, w = torch.zeros((4, 64), dtype=torch.float16), torch.ones(64, dtype=torch.float16)
+    at = torch.zeros(4, dtype=torch.int32)
+    cache = nfp.KVCache(2, 16, 1, 64, device="cpu")
+    for call in (lambda: nfp.add_rms_norm(x, w), lambda: nfp.rope_append(x, x, x, at, at, cache),
+                 lambda: nfp.paged_attention(x, cache, at.reshape(4, 1), at, workspace=torch.zeros(16, dtype=torch.uint8)),
+                 lambda: nfp.add_rms_norm(x, None, out=x)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        nfp.KVCache(k=torch.zeros((2, 1, 1, 8, 16, 8), dtype=torch.float16), v=torch.zeros((2, 1, 1, 2, 64, 4), dtype=torch.float16))
+    with pytest.raises(ValueError):
+        nfp.KVCache(2, 16, 1, 64, device="cpu", k_scale=torch.ones(2))
+
+
+def test_keys_and_values_of_a_cache_as_views(nfp):
+    import torch
+
+    from block_helpers import HostCache
+
+    for fp8 in (False, True):
+        host = HostCache(3, 64, 2, 96, fp8, seed=4)
+        k, v = (torch.from_numpy(a) for a in host.storage())
+        cache = nfp.KVCache(k=k, v=v)
+        for view, rows in ((cache.keys(), host.k), (cache.values(), host.v)):
+            assert (view.reshape(rows.shape).numpy().view("uint8") == rows.view("uint8")).all()
