@@ -322,6 +322,12 @@ __device__ __forceinline__ int place_of(const Schedule &plan, int x, int batch, 
 // in the workspace and the one that comes last joins them in order.
 // P is carried as two FP16 terms (its FP16 rounding and the rest): the second product costs nothing here, and the
 // result then has the precision of the 32-bit sums.
+// Measured (128 dims, 8 key/value heads; a read-only stream reaches 7.15 TB/s): 768 equal tiles of 1600 tokens 96 us (6.6 TB/s), one token over
+// 131072 84 us (6.4), 32 sequences of 500 ... 8192 tokens 67 us (5.5), 48 of 1000 ... 20000 in E4M3 113 us (5.6), one of 613 8.6 us.  Beside
+// the bytes a call costs about 9 us: launch, lengths, page numbers and first keys one after the other, at the end sums, ticket
+// and join.
+// Tried and dropped: the next step's loads under way during the work on one (two steps of registers, 113 -> 122 us on the 48 sequences);
+// loads that stay in L2 (130); three workgroups per CU (115 us, and 101 instead of 90 on the one long sequence).
 template <int D, bool FP8, int RT>
 __global__ void __launch_bounds__(256, D <= 128 && RT == 1 ? 3 : 2)
 attention_stream_kernel(AttentionArgs p) {
@@ -343,344 +349,345 @@ attention_stream_kernel(AttentionArgs p) {
     if (p.scan) plan = schedule(p, 16 * RT, LEAST);
     else plan.all = gridDim.x, plan.share = 1;
     // (without a schedule: a workgroup is a chunk of a tile)
-    for (int first = blockIdx.x; (int64_t)first * plan.share < plan.all; first += gridDim.x)
-    for (int x = first * plan.share, end = min(plan.all, x + plan.share); x < end;) {
-    __syncthreads();
-    // (hidden from the compiler, which otherwise works out before the loop what every lane needs in it, and keeps it in 40 registers)
-    int thread = threadIdx.x;
-    asm volatile("" : "+v"(thread));
-    const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), group = lane >> 4, col = lane & 15;
-    int chunk, rt0, head, b, offset_in_tile, here;        // (blocks of the tile before this stretch, and in it)
-    Sequence sq;
-    if (p.scan) {
-        const int mine = place_of(plan, x, p.batch, b);
-        sq = sequence(p, b);
-        const int each = padded_blocks(p, sq, LEAST), index = mine / each;
-        offset_in_tile = mine - index * each;
-        here = min(end - x, each - offset_in_tile);
-        head = index % p.kv_heads;
-        rt0 = index / p.kv_heads;
-        chunk = x / plan.share - (x - offset_in_tile) / plan.share;
-    } else {
-        const int tiles = p.batch * p.kv_heads * p.row_tiles;
-        chunk = x / tiles;
-        head = x % p.kv_heads;
-        rt0 = x % tiles / p.kv_heads % p.row_tiles;
-        b = x % tiles / p.kv_heads / p.row_tiles;
-        sq = sequence(p, b);
-        offset_in_tile = chunk * p.chunk_blocks;
-        here = 1;
-    }
-    const int start_of_tile = x - offset_in_tile;
-    x += here;
-    const int tile = (b * p.row_tiles + rt0) * p.kv_heads + head;
-    const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
-    if (row0 >= rows || (p.few > 0 && rows > p.few)) continue;   // (the tile kernel's)
-    const int row1 = min(rows, row0 + 16 * RT) - 1;
-    const int past = sq.length - sq.fresh;
-    const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
-    const Walk w = walk(p, low_pos, high_pos);
-    int chunks, v1;
-    const int v0 = offset_in_tile;
-    if (p.scan) {
-        chunks = (start_of_tile + max(w.blocks, 1) - 1) / plan.share - start_of_tile / plan.share + 1;
-        v1 = min(w.blocks, v0 + here);
-    } else {
-        // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
-        chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
-        v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
-    }
-    if (chunk >= chunks) continue;
+    for (int first = blockIdx.x; (int64_t)first * plan.share < plan.all; first += gridDim.x) {
+        for (int x = first * plan.share, end = min(plan.all, x + plan.share); x < end;) {
+            __syncthreads();
+            // (hidden from the compiler, which otherwise works out before the loop what every lane needs in it, and keeps it in 40 registers)
+            int thread = threadIdx.x;
+            asm volatile("" : "+v"(thread));
+            const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), group = lane >> 4, col = lane & 15;
+            int chunk, rt0, head, b, offset_in_tile, here;        // (blocks of the tile before this stretch, and in it)
+            Sequence sq;
+            if (p.scan) {
+                const int mine = place_of(plan, x, p.batch, b);
+                sq = sequence(p, b);
+                const int each = padded_blocks(p, sq, LEAST), index = mine / each;
+                offset_in_tile = mine - index * each;
+                here = min(end - x, each - offset_in_tile);
+                head = index % p.kv_heads;
+                rt0 = index / p.kv_heads;
+                chunk = x / plan.share - (x - offset_in_tile) / plan.share;
+            } else {
+                const int tiles = p.batch * p.kv_heads * p.row_tiles;
+                chunk = x / tiles;
+                head = x % p.kv_heads;
+                rt0 = x % tiles / p.kv_heads % p.row_tiles;
+                b = x % tiles / p.kv_heads / p.row_tiles;
+                sq = sequence(p, b);
+                offset_in_tile = chunk * p.chunk_blocks;
+                here = 1;
+            }
+            const int start_of_tile = x - offset_in_tile;
+            x += here;
+            const int tile = (b * p.row_tiles + rt0) * p.kv_heads + head;
+            const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
+            if (row0 >= rows || (p.few > 0 && rows > p.few)) continue;   // (the tile kernel's)
+            const int row1 = min(rows, row0 + 16 * RT) - 1;
+            const int past = sq.length - sq.fresh;
+            const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
+            const Walk w = walk(p, low_pos, high_pos);
+            int chunks, v1;
+            const int v0 = offset_in_tile;
+            if (p.scan) {
+                chunks = (start_of_tile + max(w.blocks, 1) - 1) / plan.share - start_of_tile / plan.share + 1;
+                v1 = min(w.blocks, v0 + here);
+            } else {
+                // (a sequence longer than the launch was sized for: its last workgroup takes what is left)
+                chunks = min(p.chunks, max(1, (w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+                v1 = chunk == chunks - 1 ? w.blocks : v0 + p.chunk_blocks;
+            }
+            if (chunk >= chunks) continue;
 
-    // queries, as the second operand: column = row, dims in the order in which the keys' chunks come
-    int row[RT], pos[RT], low[RT];
-    half8 q[RT][QS];
+            // queries, as the second operand: column = row, dims in the order in which the keys' chunks come
+            int row[RT], pos[RT], low[RT];
+            half8 q[RT][QS];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        row[r] = row0 + 16 * r + col;
-        const int i = min(row[r], row1) / p.group, g = min(row[r], row1) - i * p.group;
-        pos[r] = past + i;
-        low[r] = before(p, pos[r]);
-        const uint16_t *src = p.Q + (int64_t)(sq.first + i) * p.ldq + (int64_t)(head * p.group + g) * D;
+            for (int r = 0; r < RT; ++r) {
+                row[r] = row0 + 16 * r + col;
+                const int i = min(row[r], row1) / p.group, g = min(row[r], row1) - i * p.group;
+                pos[r] = past + i;
+                low[r] = before(p, pos[r]);
+                const uint16_t *src = p.Q + (int64_t)(sq.first + i) * p.ldq + (int64_t)(head * p.group + g) * D;
 #pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            const int dim = FP8 ? 16 * (4 * (s >> 1) + group) + 8 * (s & 1) : 8 * (4 * s + group);
-            q[r][s] = dim < D ? *reinterpret_cast<const half8 *>(src + dim) : half8{};
-        }
-    }
-    floatx4 acc[RT][DB];
-    float top[RT], total[RT];
-    const float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
-    const int in_page = (1 << p.page_shift) - 1;
-
-    // this wave's blocks of the 256 from `base`: step j takes blocks base + NT (4 j + wave) ...; lane NT j + k has the page of the k-th of step j
-    const auto pages_from = [&](int base) {
-        const int v = base + NT * (4 * (lane / NT) + wave) + lane % NT;
-        return v < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v) >> p.page_shift)] : 0;
-    };
-    const auto offset = [&](int block, int pg, bool valid) {
-        return ((((int64_t)(valid ? pg : 0) * p.kv_heads + head) << p.page_shift) + (valid ? block & in_page : 0)) * BLOCK;
-    };
-    // this lane's values: of its group's block, 8 (16 in E4M3) tokens of dims 16 d + col
-    const int mine_in_block = (FP8 ? 0 : (group & 1) * D * 16) + col * 16, mine_first = FP8 ? 0 : 8 * (group & 1);
-    const int first_low = before(p, low_pos), last_low = before(p, high_pos);
-
-    bool clean = false;
-    for (;;) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            top[r] = kNegInf;
-            total[r] = 0.0f;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) acc[r][d] = floatx4{0, 0, 0, 0};
-        }
-        for (int base = v0; base < v1; base += 64 * 4) {
-            const int page = pages_from(base);
-            for (int j = 0; j < 64 / NT; ++j) {
-                const int v = base + NT * (4 * j + wave);
-                if (v >= v1) break;
-                u32x4 kk[NT][KL], vv[DB];
-                int t0[NT];
-                bool plain = true;
-                uint32_t missing = 0;                      // blocks of this step that are not there
-                const uint8_t *mine = nullptr;             // of this lane's block of values
-#pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    const int block = w.block(min(v + k, v1 - 1)), pg = __builtin_amdgcn_readlane(page, NT * j + k);
-                    const bool there = v + k < v1;
-                    const bool valid = (uint32_t)pg < (uint32_t)p.pages;
-                    t0[k] = there ? block * 16 : 0x7ffffff0;          // (nothing sees those)
-                    if (there && !valid) missing |= 1u << k;
-                    plain &= there && valid && t0[k] + 15 <= low_pos && (t0[k] > last_low || t0[k] + 15 < p.sinks);
-                    const int64_t at = offset(block, pg, valid && there);
-                    const uint8_t *kb = p.k + at, *vb = p.v + at;
-#pragma unroll
-                    for (int s = 0; s < KL; ++s) {
-                        int off = s * 1024 + lane * 16;
-                        if (BLOCK % 1024 != 0 && off >= BLOCK) off -= 512;           // (those dims are multiplied by zero)
-                        kk[k][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kb + off));
-                    }
-                    if ((FP8 ? group : group >> 1) == k) mine = vb;
-                }
-                mine += mine_in_block;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) vv[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(mine + d * 256));
-                // scores, in units of log 2
-                floatx4 s4[RT][NT];
-#pragma unroll
-                for (int k = 0; k < NT; ++k)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        floatx4 s = floatx4{0, 0, 0, 0};
-#pragma unroll
-                        for (int i = 0; i < KL; ++i) {
-                            if constexpr (FP8) {
-                                half8 lo, hi;
-                                widen(kk[k][i], lo, hi);
-                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[r][2 * i], s, 0, 0, 0);
-                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[r][2 * i + 1], s, 0, 0, 0);
-                            } else {
-                                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kk[k][i]), q[r][i], s, 0, 0, 0);
-                            }
-                        }
-                        s4[r][k] = s * scale;
-                    }
-                if (!plain) {
-#pragma unroll
-                    for (int k = 0; k < NT; ++k)
-#pragma unroll
-                        for (int r = 0; r < RT; ++r)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (missing >> k & 1) s4[r][k][i] = __builtin_nanf("");
-                                if (!sees(t0[k] + 4 * group + i, pos[r], low[r], p.sinks)) s4[r][k][i] = kNegInf;
-                                // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
-                            }
-                    // values that no row sees may be anything: memory that was never written, another sequence's
-                    int t = mine_first;
-#pragma unroll
-                    for (int k = 0; k < NT; ++k)
-                        if ((FP8 ? group : group >> 1) == k) t += t0[k];
-                    uint32_t keep[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int i = 0; i < (FP8 ? 16 : 8); ++i)
-                        if (sees(t + i, high_pos, first_low, p.sinks)) keep[FP8 ? i >> 2 : i >> 1] |= FP8 ? 0xffu << (8 * (i & 3)) : 0xffffu << (16 * (i & 1));
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) vv[d] &= u32x4{keep[0], keep[1], keep[2], keep[3]};
-                }
-                if (clean)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) vv[d] = only_finite<FP8>(vv[d]);
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    float m = top[r];
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) m = fmaxf(fmaxf(fmaxf(m, s4[r][k][0]), fmaxf(s4[r][k][1], s4[r][k][2])), s4[r][k][3]);
-                    m = max_of_groups(m);
-                    const float from = fmaxf(m, -1e30f) - kShift;        // (a row that has seen nothing yet)
-                    const float shrink = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
-                    top[r] = m;
-                    uint32_t hi[NT][2], lo[NT][2];
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) {
-                        float e[4], rest[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            e[i] = __builtin_amdgcn_exp2f(s4[r][k][i] - from);
-                            sum += e[i];
-                            rest[i] = e[i] - (float)(_Float16)e[i];
-                        }
-                        hi[k][0] = float2_to_half2_bits(e[0], e[1]);
-                        hi[k][1] = float2_to_half2_bits(e[2], e[3]);
-                        lo[k][0] = float2_to_half2_bits(rest[0], rest[1]);
-                        lo[k][1] = float2_to_half2_bits(rest[2], rest[3]);
-                    }
-                    total[r] = total[r] * shrink + sum;
-                    if (__builtin_amdgcn_ballot_w64(shrink != 1.0f)) {
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) acc[r][d] *= shrink;
-                    }
-                    // from (block, tokens 4 group ...) to (group, the tokens that this group's values are of)
-                    half8 ph[NT / 2], pl[NT / 2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if constexpr (FP8) {
-                            swap32(hi[0][i], hi[2][i]);  swap32(hi[1][i], hi[3][i]);
-                            swap16(hi[0][i], hi[1][i]);  swap16(hi[2][i], hi[3][i]);
-                            swap32(lo[0][i], lo[2][i]);  swap32(lo[1][i], lo[3][i]);
-                            swap16(lo[0][i], lo[1][i]);  swap16(lo[2][i], lo[3][i]);
-                        } else {
-                            swap32(hi[0][i], hi[1][i]);  swap16(hi[0][i], hi[1][i]);
-                            swap32(lo[0][i], lo[1][i]);  swap16(lo[0][i], lo[1][i]);
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < NT / 2; ++k) {
-                        ph[k] = __builtin_bit_cast(half8, u32x4{hi[2 * k][0], hi[2 * k][1], hi[2 * k + 1][0], hi[2 * k + 1][1]});
-                        pl[k] = __builtin_bit_cast(half8, u32x4{lo[2 * k][0], lo[2 * k][1], lo[2 * k + 1][0], lo[2 * k + 1][1]});
-                    }
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        if constexpr (FP8) {
-                            half8 va, vb;
-                            widen(vv[d], va, vb);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, ph[1], acc[r][d], 0, 0, 0);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, pl[1], acc[r][d], 0, 0, 0);
-                        } else {
-                            const half8 va = __builtin_bit_cast(half8, vv[d]);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
-                        }
-                    }
+                for (int s = 0; s < QS; ++s) {
+                    const int dim = FP8 ? 16 * (4 * (s >> 1) + group) + 8 * (s & 1) : 8 * (4 * s + group);
+                    q[r][s] = dim < D ? *reinterpret_cast<const half8 *>(src + dim) : half8{};
                 }
             }
-        }
-        bool bad = false;
+            floatx4 acc[RT][DB];
+            float top[RT], total[RT];
+            const float scale = p.scale * kLog2e * (FP8 && p.k_scale ? p.k_scale[head] : 1.0f);
+            const int in_page = (1 << p.page_shift) - 1;
+
+            // this wave's blocks of the 256 from `base`: step j takes blocks base + NT (4 j + wave) ...; lane NT j + k has the page of the k-th of step j
+            const auto pages_from = [&](int base) {
+                const int v = base + NT * (4 * (lane / NT) + wave) + lane % NT;
+                return v < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v) >> p.page_shift)] : 0;
+            };
+            const auto offset = [&](int block, int pg, bool valid) {
+                return ((((int64_t)(valid ? pg : 0) * p.kv_heads + head) << p.page_shift) + (valid ? block & in_page : 0)) * BLOCK;
+            };
+            // this lane's values: of its group's block, 8 (16 in E4M3) tokens of dims 16 d + col
+            const int mine_in_block = (FP8 ? 0 : (group & 1) * D * 16) + col * 16, mine_first = FP8 ? 0 : 8 * (group & 1);
+            const int first_low = before(p, low_pos), last_low = before(p, high_pos);
+
+            bool clean = false;
+            for (;;) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+                for (int r = 0; r < RT; ++r) {
+                    top[r] = kNegInf;
+                    total[r] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) bad |= not_finite(acc[r][d]);
-        if (clean || !__builtin_amdgcn_ballot_w64(bad)) break;
-        clean = true;
-    }
-    if (clean) {
-        for (int kind = kPlusInf; kind <= kNaN; ++kind) {
-            floatx4 count[RT][DB];
+                    for (int d = 0; d < DB; ++d) acc[r][d] = floatx4{0, 0, 0, 0};
+                }
+                for (int base = v0; base < v1; base += 64 * 4) {
+                    const int page = pages_from(base);
+                    for (int j = 0; j < 64 / NT; ++j) {
+                        const int v = base + NT * (4 * j + wave);
+                        if (v >= v1) break;
+                        u32x4 kk[NT][KL], vv[DB];
+                        int t0[NT];
+                        bool plain = true;
+                        uint32_t missing = 0;                      // blocks of this step that are not there
+                        const uint8_t *mine = nullptr;             // of this lane's block of values
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+                        for (int k = 0; k < NT; ++k) {
+                            const int block = w.block(min(v + k, v1 - 1)), pg = __builtin_amdgcn_readlane(page, NT * j + k);
+                            const bool there = v + k < v1;
+                            const bool valid = (uint32_t)pg < (uint32_t)p.pages;
+                            t0[k] = there ? block * 16 : 0x7ffffff0;          // (nothing sees those)
+                            if (there && !valid) missing |= 1u << k;
+                            plain &= there && valid && t0[k] + 15 <= low_pos && (t0[k] > last_low || t0[k] + 15 < p.sinks);
+                            const int64_t at = offset(block, pg, valid && there);
+                            const uint8_t *kb = p.k + at, *vb = p.v + at;
 #pragma unroll
-                for (int d = 0; d < DB; ++d) count[r][d] = floatx4{0, 0, 0, 0};
-            for (int base = v0; base < v1; base += 64 * 4) {
-                const int page = pages_from(base);
-                for (int j = 0; j < 64 / NT; ++j) {
-                    const int v = base + NT * (4 * j + wave);
-                    if (v >= v1) break;
-                    const int k = FP8 ? group : group >> 1;
-                    const bool there = v + k < v1;
-                    const int block = w.block(min(v + k, v1 - 1)), pg = __shfl(page, NT * j + k);
-                    const bool valid = there && (uint32_t)pg < (uint32_t)p.pages;
-                    const int t = valid ? block * 16 + mine_first : 0x7ffffff0;
-                    const uint8_t *mine = p.v + offset(block, pg, valid) + mine_in_block;
-                    half8 seen[RT][NT / 2];
+                            for (int s = 0; s < KL; ++s) {
+                                int off = s * 1024 + lane * 16;
+                                if (BLOCK % 1024 != 0 && off >= BLOCK) off -= 512;           // (those dims are multiplied by zero)
+                                kk[k][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kb + off));
+                            }
+                            if ((FP8 ? group : group >> 1) == k) mine = vb;
+                        }
+                        mine += mine_in_block;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) vv[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(mine + d * 256));
+                        // scores, in units of log 2
+                        floatx4 s4[RT][NT];
+#pragma unroll
+                        for (int k = 0; k < NT; ++k)
+#pragma unroll
+                            for (int r = 0; r < RT; ++r) {
+                                floatx4 s = floatx4{0, 0, 0, 0};
+#pragma unroll
+                                for (int i = 0; i < KL; ++i) {
+                                    if constexpr (FP8) {
+                                        half8 lo, hi;
+                                        widen(kk[k][i], lo, hi);
+                                        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[r][2 * i], s, 0, 0, 0);
+                                        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[r][2 * i + 1], s, 0, 0, 0);
+                                    } else {
+                                        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kk[k][i]), q[r][i], s, 0, 0, 0);
+                                    }
+                                }
+                                s4[r][k] = s * scale;
+                            }
+                        if (!plain) {
+#pragma unroll
+                            for (int k = 0; k < NT; ++k)
+#pragma unroll
+                                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        if (missing >> k & 1) s4[r][k][i] = __builtin_nanf("");
+                                        if (!sees(t0[k] + 4 * group + i, pos[r], low[r], p.sinks)) s4[r][k][i] = kNegInf;
+                                        // (an entry outside the cache gives NaN where a token is seen, nothing elsewhere)
+                                    }
+                            // values that no row sees may be anything: memory that was never written, another sequence's
+                            int t = mine_first;
+#pragma unroll
+                            for (int k = 0; k < NT; ++k)
+                                if ((FP8 ? group : group >> 1) == k) t += t0[k];
+                            uint32_t keep[4] = {0, 0, 0, 0};
+#pragma unroll
+                            for (int i = 0; i < (FP8 ? 16 : 8); ++i)
+                                if (sees(t + i, high_pos, first_low, p.sinks)) keep[FP8 ? i >> 2 : i >> 1] |= FP8 ? 0xffu << (8 * (i & 3)) : 0xffffu << (16 * (i & 1));
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) vv[d] &= u32x4{keep[0], keep[1], keep[2], keep[3]};
+                        }
+                        if (clean)
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) vv[d] = only_finite<FP8>(vv[d]);
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            float m = top[r];
+#pragma unroll
+                            for (int k = 0; k < NT; ++k) m = fmaxf(fmaxf(fmaxf(m, s4[r][k][0]), fmaxf(s4[r][k][1], s4[r][k][2])), s4[r][k][3]);
+                            m = max_of_groups(m);
+                            const float from = fmaxf(m, -1e30f) - kShift;        // (a row that has seen nothing yet)
+                            const float shrink = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
+                            top[r] = m;
+                            uint32_t hi[NT][2], lo[NT][2];
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int k = 0; k < NT; ++k) {
+                                float e[4], rest[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    e[i] = __builtin_amdgcn_exp2f(s4[r][k][i] - from);
+                                    sum += e[i];
+                                    rest[i] = e[i] - (float)(_Float16)e[i];
+                                }
+                                hi[k][0] = float2_to_half2_bits(e[0], e[1]);
+                                hi[k][1] = float2_to_half2_bits(e[2], e[3]);
+                                lo[k][0] = float2_to_half2_bits(rest[0], rest[1]);
+                                lo[k][1] = float2_to_half2_bits(rest[2], rest[3]);
+                            }
+                            total[r] = total[r] * shrink + sum;
+                            if (__builtin_amdgcn_ballot_w64(shrink != 1.0f)) {
+#pragma unroll
+                                for (int d = 0; d < DB; ++d) acc[r][d] *= shrink;
+                            }
+                            // from (block, tokens 4 group ...) to (group, the tokens that this group's values are of)
+                            half8 ph[NT / 2], pl[NT / 2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                if constexpr (FP8) {
+                                    swap32(hi[0][i], hi[2][i]);  swap32(hi[1][i], hi[3][i]);
+                                    swap16(hi[0][i], hi[1][i]);  swap16(hi[2][i], hi[3][i]);
+                                    swap32(lo[0][i], lo[2][i]);  swap32(lo[1][i], lo[3][i]);
+                                    swap16(lo[0][i], lo[1][i]);  swap16(lo[2][i], lo[3][i]);
+                                } else {
+                                    swap32(hi[0][i], hi[1][i]);  swap16(hi[0][i], hi[1][i]);
+                                    swap32(lo[0][i], lo[1][i]);  swap16(lo[0][i], lo[1][i]);
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < NT / 2; ++k) {
+                                ph[k] = __builtin_bit_cast(half8, u32x4{hi[2 * k][0], hi[2 * k][1], hi[2 * k + 1][0], hi[2 * k + 1][1]});
+                                pl[k] = __builtin_bit_cast(half8, u32x4{lo[2 * k][0], lo[2 * k][1], lo[2 * k + 1][0], lo[2 * k + 1][1]});
+                            }
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) {
+                                if constexpr (FP8) {
+                                    half8 va, vb;
+                                    widen(vv[d], va, vb);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, ph[1], acc[r][d], 0, 0, 0);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, pl[1], acc[r][d], 0, 0, 0);
+                                } else {
+                                    const half8 va = __builtin_bit_cast(half8, vv[d]);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[0], acc[r][d], 0, 0, 0);
+                                    acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pl[0], acc[r][d], 0, 0, 0);
+                                }
+                            }
+                        }
+                    }
+                }
+                bool bad = false;
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) bad |= not_finite(acc[r][d]);
+                if (clean || !__builtin_amdgcn_ballot_w64(bad)) break;
+                clean = true;
+            }
+            if (clean) {
+                for (int kind = kPlusInf; kind <= kNaN; ++kind) {
+                    floatx4 count[RT][DB];
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
 #pragma unroll
-                        for (int i = 0; i < 4 * NT; ++i) seen[r][i >> 3][i & 7] = sees(t + i, pos[r], low[r], p.sinks) ? (_Float16)1.0f : (_Float16)0.0f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        const u32x4 vv = *reinterpret_cast<const u32x4 *>(mine + d * 256);
-                        half8 part_of[NT / 2];
-                        if constexpr (FP8) widen(vv, part_of[0], part_of[1]);
-                        else part_of[0] = __builtin_bit_cast(half8, vv);
-#pragma unroll
-                        for (int i = 0; i < NT / 2; ++i)
+                        for (int d = 0; d < DB; ++d) count[r][d] = floatx4{0, 0, 0, 0};
+                    for (int base = v0; base < v1; base += 64 * 4) {
+                        const int page = pages_from(base);
+                        for (int j = 0; j < 64 / NT; ++j) {
+                            const int v = base + NT * (4 * j + wave);
+                            if (v >= v1) break;
+                            const int k = FP8 ? group : group >> 1;
+                            const bool there = v + k < v1;
+                            const int block = w.block(min(v + k, v1 - 1)), pg = __shfl(page, NT * j + k);
+                            const bool valid = there && (uint32_t)pg < (uint32_t)p.pages;
+                            const int t = valid ? block * 16 + mine_first : 0x7ffffff0;
+                            const uint8_t *mine = p.v + offset(block, pg, valid) + mine_in_block;
+                            half8 seen[RT][NT / 2];
 #pragma unroll
                             for (int r = 0; r < RT; ++r)
-                                count[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(of_kind(part_of[i], kind), seen[r][i], count[r][d], 0, 0, 0);
+#pragma unroll
+                                for (int i = 0; i < 4 * NT; ++i) seen[r][i >> 3][i & 7] = sees(t + i, pos[r], low[r], p.sinks) ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) {
+                                const u32x4 vv = *reinterpret_cast<const u32x4 *>(mine + d * 256);
+                                half8 part_of[NT / 2];
+                                if constexpr (FP8) widen(vv, part_of[0], part_of[1]);
+                                else part_of[0] = __builtin_bit_cast(half8, vv);
+#pragma unroll
+                                for (int i = 0; i < NT / 2; ++i)
+#pragma unroll
+                                    for (int r = 0; r < RT; ++r)
+                                        count[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(of_kind(part_of[i], kind), seen[r][i], count[r][d], 0, 0, 0);
+                            }
+                        }
                     }
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int d = 0; d < DB; ++d)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (count[r][d][i] > 0.0f) acc[r][d][i] += of_kind_value(kind);
                 }
             }
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (count[r][d][i] > 0.0f) acc[r][d][i] += of_kind_value(kind);
-        }
-    }
 
-    // the four waves' sums: statistics first, then each wave's sums relative to the largest maximum; of rows that there are
+            // the four waves' sums: statistics first, then each wave's sums relative to the largest maximum; of rows that there are
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        total[r] = sum_of_groups(total[r]);
-        if (group == 0) {
-            stat[wave][0][16 * r + col] = top[r];
-            stat[wave][1][16 * r + col] = total[r];
+            for (int r = 0; r < RT; ++r) {
+                total[r] = sum_of_groups(total[r]);
+                if (group == 0) {
+                    stat[wave][0][16 * r + col] = top[r];
+                    stat[wave][1][16 * r + col] = total[r];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                float m = kNegInf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][16 * r + col]);
+                const float f = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
+                if (row[r] <= row1) {
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) *reinterpret_cast<floatx4 *>(&part[wave][16 * r + col][16 * d + 4 * group]) = acc[r][d] * f;
+                }
+            }
+            __syncthreads();
+            const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
+            for (int at = thread; at < (row1 - row0 + 1) * (D / 4); at += 256) {
+                const int r = at / (D / 4), d = 4 * (at - r * (D / 4));
+                float m = kNegInf, sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][r]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += stat[i][1][r] * __builtin_amdgcn_exp2f(fmaxf(stat[i][0][r], -1e30f) - fmaxf(m, -1e30f));
+                floatx4 o = *reinterpret_cast<const floatx4 *>(&part[0][r][d]);
+#pragma unroll
+                for (int i = 1; i < 4; ++i) o += *reinterpret_cast<const floatx4 *>(&part[i][r][d]);
+                if (chunks == 1) {
+                    const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
+                    const float f = v_scale / sum;
+                    // a row that sees nothing is zero
+                    *reinterpret_cast<u32x2 *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) = past + i < 0 ? u32x2{0u, 0u} :
+                        u32x2{float2_to_half2_bits(o[0] * f, o[1] * f), float2_to_half2_bits(o[2] * f, o[3] * f)};
+                } else {
+                    float *dst = p.partials + (((int64_t)tile * p.chunks + chunk) * p.part_rows + r) * (D + 2);
+                    past_caches(dst + d, o[0], o[1]);
+                    past_caches(dst + d + 2, o[2], o[3]);
+                    if (d == 0) past_caches(dst + D, m, sum);
+                }
+            }
+            if (chunks == 1) continue;
+            join<D, 256>(p, thread, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
         }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        float m = kNegInf;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][16 * r + col]);
-        const float f = __builtin_amdgcn_exp2f(fmaxf(top[r], -1e30f) - fmaxf(m, -1e30f));
-        if (row[r] <= row1) {
-#pragma unroll
-            for (int d = 0; d < DB; ++d) *reinterpret_cast<floatx4 *>(&part[wave][16 * r + col][16 * d + 4 * group]) = acc[r][d] * f;
-        }
-    }
-    __syncthreads();
-    const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
-    for (int at = thread; at < (row1 - row0 + 1) * (D / 4); at += 256) {
-        const int r = at / (D / 4), d = 4 * (at - r * (D / 4));
-        float m = kNegInf, sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = fmaxf(m, stat[i][0][r]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += stat[i][1][r] * __builtin_amdgcn_exp2f(fmaxf(stat[i][0][r], -1e30f) - fmaxf(m, -1e30f));
-        floatx4 o = *reinterpret_cast<const floatx4 *>(&part[0][r][d]);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) o += *reinterpret_cast<const floatx4 *>(&part[i][r][d]);
-        if (chunks == 1) {
-            const int i = (row0 + r) / p.group, g = row0 + r - i * p.group;
-            const float f = v_scale / sum;
-            // a row that sees nothing is zero
-            *reinterpret_cast<u32x2 *>(p.O + (int64_t)(sq.first + i) * p.ldo + (int64_t)(head * p.group + g) * D + d) = past + i < 0 ? u32x2{0u, 0u} :
-                u32x2{float2_to_half2_bits(o[0] * f, o[1] * f), float2_to_half2_bits(o[2] * f, o[3] * f)};
-        } else {
-            float *dst = p.partials + (((int64_t)tile * p.chunks + chunk) * p.part_rows + r) * (D + 2);
-            past_caches(dst + d, o[0], o[1]);
-            past_caches(dst + d + 2, o[2], o[3]);
-            if (d == 0) past_caches(dst + D, m, sum);
-        }
-    }
-    if (chunks == 1) continue;
-    join<D, 256>(p, thread, tile, chunks, sq, row0, row1, past, head, v_scale, shared, &last);
     }
 }
 
@@ -689,7 +696,13 @@ attention_stream_kernel(AttentionArgs p) {
 // values of TK tokens at a time go through two buffers of LDS, which all waves read, in the storage's own order: a wave's operand reads
 // are contiguous, nothing is transposed.  E4M3 codes become FP16 on their way into LDS, once for all rows.
 // A row's probabilities are taken relative to a maximum that follows the true one only when that is 2^kLag larger, so that
-// the sums are rarely rescaled; P is rounded to FP16 and its sum is that of the rounded values.
+// the sums are rarely rescaled; P is rounded to FP16 (2^-12 of a probability on average, as much as the output's own rounding) and its
+// sum is that of the rounded values.  32 rows per wave: a wave's operand reads from LDS then take as long as its products.
+// Measured: a prompt of 8192 tokens (32 query heads, 128 dims) 590-600 us, 915-935 TFLOP/s; a large matrix product of the vendor's library
+// reaches 1336 on this card, the matrix pipe alone 1580 under the power limit.  What is left are the exponentials: 512 of a wave's 2000
+// issue cycles per step of 64 tokens, beside 400 of other vector work and 1024 of the pipe.
+// Tried and dropped: scores one step ahead of their use (692 us), with an order of instructions given (643, 660); halves of the waves
+// taking turns at the pipe with two barriers per step (688, with raised priority 677).
 constexpr float kLag = 8.0f;
 constexpr float kTileShift = 4.0f;                     // probabilities up to 2^(kLag + kTileShift)
 
@@ -698,6 +711,7 @@ constexpr float kTileShift = 4.0f;                     // probabilities up to 2^
 struct TileOf { int b, index; };
 __device__ __forceinline__ TileOf tile_of(const AttentionArgs &p, int t, int tile_rows) {
     if (!p.starts) {
+        if (p.per * p.group <= p.few) return {-1, 0};
         const int each = (p.per * p.group + tile_rows - 1) / tile_rows, b = t / each;
         return {b < p.batch ? b : -1, t - b * each};
     }

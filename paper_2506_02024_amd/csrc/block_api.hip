@@ -47,7 +47,8 @@ static int attention_shape(int64_t tokens, int64_t batch, int64_t heads, const n
     const int st = check_cache(c);
     if (st != kOk) return st;
     if (heads % c->kv_heads != 0 || heads > 65535) return kErrShape;
-    if (tokens > kMaxRows || batch > 0xfffff || max_len > 0x7fffffff - 256) return kErrShape;
+    // (rows of a sequence, new tokens times heads, are counted in 31 bits)
+    if (tokens > kMaxRows / heads || batch > 0xfffff || max_len > 0x7fffffff - 256) return kErrShape;
     s.tokens = tokens;
     s.batch = batch;
     s.kv_heads = c->kv_heads;

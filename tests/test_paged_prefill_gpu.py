@@ -163,3 +163,16 @@ def test_strided_rows_and_the_same_bits_on_another_stream(nfp):
         again = call(torch.empty((290, 8 * d), dtype=torch.float16, device="cuda:0"))
     side.synchronize()
     assert np.array_equal(bits(again), bits(out[:, 64:]))
+
+
+@pytest.mark.parametrize("news", [1, 3, 40])
+def test_a_bound_on_new_tokens_that_is_not_reached(nfp, news):
+    # the launch is sized for chunks of 100 tokens, every sequence has fewer: each row is worked out once
+    lens = [300, 77, news]
+    cache, table, q = _case(lens, [news] * 3, 8, 2, 128, 32, False)
+    ref, a = attention_ref(q, cache, table, lens, [news] * 3, 8, 128 ** -0.5)
+    dev, td, ld = cache.to_device(nfp), _dev(table), _dev(np.asarray(lens, dtype=np.int32))
+    first = nfp.paged_attention(_dev(q), dev, td, ld, max_new=100, max_len=300)
+    assert_attention_close(first, ref, a)
+    for _ in range(5):
+        assert np.array_equal(bits(first), bits(nfp.paged_attention(_dev(q), dev, td, ld, max_new=100, max_len=300)))
