@@ -81,6 +81,11 @@ def main(hidden=4096, heads=32, kv_heads=8, head_dim=128, ffn=14336, prompt=1500
     def slots_of(owner, position):
         return (table[owner, position // page] * page + position % page).to(torch.int32)
 
+    # (the first calls load kernels; slots of -1: nothing is written)
+    few = torch.zeros((batch, hidden), dtype=torch.float16, device="cuda:0")
+    for mode in (nfp.MODE_FP16, nfp.MODE_FP8):
+        layer(few, few.clone(), mode, cache, at.to(torch.int32), torch.full_like(at, -1, dtype=torch.int32), table, torch.ones_like(at, dtype=torch.int32),
+              cos, sin, max_len=1)
     # every sequence's prompt in two chunks, the second beside the first ones of its kind: one ragged batch each
     for lo, hi in ((0, prompt * 2 // 3), (prompt * 2 // 3, prompt)):
         n = hi - lo
