@@ -698,8 +698,8 @@ attention_stream_kernel(AttentionArgs p) {
 // A row's probabilities are taken relative to a maximum that follows the true one only when that is 2^kLag larger, so that
 // the sums are rarely rescaled; P is rounded to FP16 (2^-12 of a probability on average, as much as the output's own rounding) and its
 // sum is that of the rounded values.  32 rows per wave: a wave's operand reads from LDS then take as long as its products.
-// Measured: a prompt of 8192 tokens (32 query heads, 128 dims) 590-600 us, 915-935 TFLOP/s; a large matrix product of the vendor's library
-// reaches 1336 on this card, the matrix pipe alone 1580 under the power limit.  What is left are the exponentials: 512 of a wave's 2000
+// Measured: a prompt of 8192 tokens (32 query heads, 128 dims; 16, 256 dims alike) 590-600 us, 915-935 TFLOP/s; a large matrix product of the
+// vendor's library reaches 1336 on this card, the matrix pipe alone 1580 under the power limit.  What is left are the exponentials: 512 of a wave's 2000
 // issue cycles per step of 64 tokens, beside 400 of other vector work and 1024 of the pipe.
 // Tried and dropped: scores one step ahead of their use (692 us), with an order of instructions given (643, 660); halves of the waves
 // taking turns at the pipe with two barriers per step (688, with raised priority 677).
@@ -778,7 +778,7 @@ __device__ __forceinline__ TilePlace tile_place(const AttentionArgs &p, int tile
 }
 
 template <int D, bool FP8, int NW, int TK>
-__global__ void __launch_bounds__(64 * NW, D > 128 ? 1 : 2)
+__global__ void __launch_bounds__(64 * NW, D > 128 && NW == 4 ? 1 : 2)
 attention_tile_kernel(AttentionArgs p) {
     constexpr int T = 64 * NW, NB = TK / 16, HB = TK / 32;       // threads, blocks and halves (of 32 tokens) of a tile of tokens
     constexpr int CB = FP8 ? D : 2 * D;                          // 16-byte chunks of a block in memory
@@ -802,9 +802,9 @@ attention_tile_kernel(AttentionArgs p) {
     const int first_low = before(p, low_pos);
 
     // this wave's rows
-    const int wave_row0 = row0 + 32 * wave, row = wave_row0 + col;
+    const int wave_row0 = row0 + 32 * wave;
     const bool idle = wave_row0 > row1;
-    const int clamped = min(row, row1), token = clamped / p.group, g = clamped - token * p.group;
+    const int clamped = min(wave_row0 + col, row1), token = clamped / p.group, g = clamped - token * p.group;
     const int pos = past + token, low = before(p, pos);
     const int wave_low = past + min(wave_row0, row1) / p.group, wave_high = past + min(wave_row0 + 31, row1) / p.group;
     const int wave_last_low = before(p, wave_high);
@@ -856,9 +856,12 @@ attention_tile_kernel(AttentionArgs p) {
             page = v + lane < v1 ? p.table[(int64_t)b * p.ld_table + (w.block(v + lane) >> p.page_shift)] : 0;
             holes |= __builtin_amdgcn_ballot_w64((uint32_t)page >= (uint32_t)p.pages && v + lane < v1) != 0;
         }
+        // (not known to be the same in every step: addresses per lane, kept over the loop, would be 64 bits each)
+        uint32_t thread = threadIdx.x;
+        if constexpr (D > 128) asm volatile("" : "+v"(thread));
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int id = threadIdx.x + i * T, first = (64 * wave + i * T) / CB;
+            const int id = thread + i * T, first = (64 * wave + i * T) / CB;
             if (CHUNKS % T != 0 && 64 * wave + i * T >= CHUNKS) break;
             int64_t from = max(offset_of(v + first), (int64_t)0);
             int block = first;
@@ -881,11 +884,13 @@ attention_tile_kernel(AttentionArgs p) {
         for (int i = 0; i < PER; ++i) {
             const int id = threadIdx.x + i * T;
             if (CHUNKS % T != 0 && 64 * wave + i * T >= CHUNKS) break;
-            const int block = id / CB, place = id - block * CB;
+            const int block = CB % 64 ? id / CB : (64 * wave + i * T) / CB, place = id - block * CB;
             u32x4 vv = vreg[i];
             if (!plain) {
                 // values that no row sees may be anything: memory that was never written, another sequence's
-                const int t = first_token(v + block) + (FP8 ? 0 : 8 * (place / D));
+                int at = place;                                  // (as in `load`)
+                if constexpr (D > 128) asm volatile("" : "+v"(at));
+                const int t = first_token(v + block) + (FP8 ? 0 : at >= D ? 8 : 0);
                 uint32_t keep[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int j = 0; j < (FP8 ? 16 : 8); ++j)
@@ -1099,38 +1104,47 @@ attention_tile_kernel(AttentionArgs p) {
     }
     const float v_scale = FP8 && p.v_scale ? p.v_scale[head] : 1.0f;
     if (chunks == 1) {
+        // (the row's place is worked out again: over the loop it would cost registers)
+        int again = lane;
+        asm volatile("" : "+v"(again));
+        const int row = wave_row0 + (again & 31), token = row / p.group, g = row - token * p.group;
         if (row > row1) return;
-        uint16_t *dst = p.O + (int64_t)(sq.first + token) * p.ldo + (int64_t)(head * p.group + g) * D + 4 * h;
+        uint16_t *dst = p.O + (int64_t)(sq.first + token) * p.ldo + (int64_t)(head * p.group + g) * D + 4 * (again >> 5);
         const float f = v_scale / total;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<u32x2 *>(dst + 32 * d + 2 * i) = pos < 0 ? u32x2{0u, 0u} :
+                *reinterpret_cast<u32x2 *>(dst + 32 * d + 2 * i) = past + token < 0 ? u32x2{0u, 0u} :
                     u32x2{float2_to_half2_bits(acc[d][i] * f, acc[d][i + 1] * f), float2_to_half2_bits(acc[d][i + 2] * f, acc[d][i + 3] * f)};
         return;
     }
+    int again = lane;
+    asm volatile("" : "+v"(again));
     // this wave's part: the sums as its lanes hold them, then the rows' maxima and sums of probabilities
     float *part = p.partials + (((int64_t)tile * p.chunks + chunk) * NW + wave) * (32 * (D + 2));
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<floatx4 *>(part + ((d * 4 + (i >> 2)) * 64 + lane) * 4) = floatx4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
-    if (h == 0) {
-        part[32 * D + 2 * col] = top;
-        part[32 * D + 2 * col + 1] = total;
+            *reinterpret_cast<floatx4 *>(part + ((d * 4 + (i >> 2)) * 64 + again) * 4) = floatx4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+    if (again < 32) {
+        part[32 * D + 2 * again] = top;
+        part[32 * D + 2 * again + 1] = total;
     }
 }
 
 // Joins the parts of split tiles, in order: a launch of its own, since a tile's parts are hundreds of kilobytes and all of the chip can
 // read them then, where the last workgroup of a tile would read them alone (64 tokens after 16384, 4 query heads to a key/value head: 287
-// us in all that way).  A workgroup has the 32 rows of one wave.
-template <int D>
+// us in all that way).  A workgroup has the 32 rows of one wave and DN dims,
+// and the loads of several parts
+// under way (17 parts of 256 rows of 256 dims 42 us with one at a time and all dims, now 7.6).  Few tiles: 32 dims each, to fill the chip
+// (22 parts of 256 rows of 128 dims, 8 tiles 11.8 -> 7.6); where there are many it costs, all of them look their tile up (1216 waves' rows 19.4 against 12.7).
+template <int D, int DN>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(AttentionArgs p, int waves, const float *v_scales) {
-    constexpr int DB = D / 32;
-    const int tile = blockIdx.x / waves, wave = blockIdx.x - tile * waves;
+    constexpr int DB = DN / 32, SPLIT = D / DN, AHEAD = DB == 1 ? 8 : 4;
+    const int of_tile = waves * SPLIT, tile = blockIdx.x / of_tile, rest = blockIdx.x - tile * of_tile, wave = rest / SPLIT, d0 = (rest - wave * SPLIT) * DB;
     const TilePlace place = tile_place(p, tile, 32 * waves);
     const int lane = threadIdx.x & 63, col = lane & 31, i4 = threadIdx.x >> 6;
     const int row = place.row0 + 32 * wave + col;
@@ -1141,19 +1155,31 @@ attention_join_kernel(AttentionArgs p, int waves, const float *v_scales) {
     floatx4 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = floatx4{0, 0, 0, 0};
-#pragma unroll 4
-    for (int c = 0; c < place.chunks; ++c, part += next) {
-        const float m = part[32 * D + 2 * col], l = part[32 * D + 2 * col + 1];
-        const float now = fmaxf(top, m), ref = fmaxf(now, -1e30f);
-        const float f = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(m, -1e30f) - ref);
-        top = now;
-        total = total * f + l * g;
+    for (int c = 0; c < place.chunks; c += AHEAD) {
+        float m[AHEAD], l[AHEAD];
+        floatx4 o[AHEAD][DB];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = acc[d] * f + *reinterpret_cast<const floatx4 *>(part + ((d * 4 + i4) * 64 + lane) * 4) * g;
+        for (int i = 0; i < AHEAD; ++i) {
+            const float *from = part + min(c + i, place.chunks - 1) * next;      // (behind the last part: that one again, left out below)
+            m[i] = from[32 * D + 2 * col];
+            l[i] = from[32 * D + 2 * col + 1];
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[i][d] = *reinterpret_cast<const floatx4 *>(from + (((d0 + d) * 4 + i4) * 64 + lane) * 4);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const bool there = c + i < place.chunks;
+            const float mine = there ? m[i] : kNegInf, now = fmaxf(top, mine), ref = fmaxf(now, -1e30f);
+            const float f = __builtin_amdgcn_exp2f(fmaxf(top, -1e30f) - ref), g = __builtin_amdgcn_exp2f(fmaxf(mine, -1e30f) - ref);
+            top = now;
+            total = total * f + (there ? l[i] : 0.0f) * g;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] = acc[d] * f + (there ? o[i][d] : floatx4{0, 0, 0, 0}) * g;
+        }
     }
     if (row > place.row1) return;
     const int token = row / p.group, g = row - token * p.group;
-    uint16_t *dst = p.O + (int64_t)(place.sq.first + token) * p.ldo + (int64_t)(place.head * p.group + g) * D + 8 * i4 + 4 * (lane >> 5);
+    uint16_t *dst = p.O + (int64_t)(place.sq.first + token) * p.ldo + (int64_t)(place.head * p.group + g) * D + 32 * d0 + 8 * i4 + 4 * (lane >> 5);
     const float f = (v_scales ? v_scales[place.head] : 1.0f) / total;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -1177,10 +1203,17 @@ static int64_t blocks_seen(const AttentionShape &s, int64_t rows) {
 // which a workgroup has too little to do; `tickets`: the parts are joined by the last workgroup of a tile, which takes a counter.
 static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t tile_rows, int64_t busy, int64_t least, int64_t wanted, bool tickets) {
     const int64_t blocks = blocks_seen(s, tile_rows);
-    int64_t chunk = (blocks * busy + wanted - 1) / wanted;
+    int64_t chunk = (blocks * busy + wanted - 1) / wanted, step = least;
+    if (!tickets && wanted >= 2 * busy) {
+        // equal parts, all in one round: 76 tiles of 4600 tokens and 256 dims in three 130 us, in three and a remainder, which waits for a
+        // free CU, 156; 32 tiles of 8320 tokens (128 dims) 36.9 against 39.3.  (Between one and two rounds the remainder pays: 152 tiles of
+        // 5800 tokens 167 us, whole 238.)
+        chunk = (blocks + wanted / busy - 1) / (wanted / busy);
+        step = 4;
+    }
     if (tuning().attn_chunk > 0) chunk = tuning().attn_chunk / 16;
     if (chunk < least) chunk = least;
-    chunk = (chunk + least - 1) / least * least;
+    chunk = (chunk + step - 1) / step * step;
     if (tickets && a.tiles > kMaxCounters) chunk = (blocks + least - 1) / least * least;
     a.chunk_blocks = chunk;
     a.chunks = (blocks + chunk - 1) / chunk;
@@ -1200,10 +1233,11 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.few = s.ragged && rows > stream_rows && s.group <= stream_rows ? stream_rows : 0;
         const int64_t total = s.tokens * s.group;
         // 128-row tiles where 256-row tiles would leave CUs without work, unless the sequences are long, whose keys and values are then
-        // read twice as often: 777 tokens of 64 dims 17.0 against 18.5 us, a prompt of 2048 65.8 / 68.4; 512 tokens after 8192
-        // 100 against 89.  (256 dims: the sums of 32 rows fill the registers of a SIMD.)
-        a.waves = s.D > 128 ? 4 : tuning().attn_waves > 0 ? tuning().attn_waves :
-                  (total + 255) / 256 * s.kv_heads >= 512 || s.max_len >= 4096 ? 8 : 4;
+        // read twice as often: 777 tokens of 64 dims 16.7 against 18.3 us, a prompt of 2048 68.2 / 69.7; 512 tokens after 8192
+        // 104 against 91.  256 dims: 16 query heads, 512 tokens 30 / 35, 1000 51 / 46, 2048 134 / 89 (four waves fill the registers of
+        // a CU, one to a SIMD, so that nothing runs beside a wave's exponentials; with eight the compiler keeps a wave in 256).
+        a.waves = tuning().attn_waves > 0 ? tuning().attn_waves :
+                  (total + 255) / 256 * s.kv_heads >= (s.D > 128 ? 64 : 512) || s.max_len >= 4096 ? 8 : 4;
         const int64_t tile_rows = 32 * a.waves;
         int64_t most = s.batch * ((rows + tile_rows - 1) / tile_rows), likely = most;
         if (s.ragged) {
@@ -1217,7 +1251,7 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.tile.row_tiles = most;
         a.tile.tiles = most * s.kv_heads;
         a.tile.part_rows = tile_rows;
-        plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, 16, a.waves == 8 || s.D > 128 ? 256 : 512, false);
+        plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, s.D > 128 ? 8 : 16, a.waves == 8 || s.D > 128 ? 256 : 512, false);
     }
     if (!many || a.few > 0) {
         const int64_t most = many ? a.few / s.group * s.group : rows;
@@ -1266,13 +1300,13 @@ template <int D, bool FP8>
 static int launch_tile(int64_t waves, const AttentionArgs &a, dim3 grid, hipStream_t stream) {
     constexpr int TK = D <= 128 ? 64 : 32, LDS = 8 * TK * D;         // two buffers of keys and values in FP16
     static_assert(LDS <= 65536, "");
-    if constexpr (D <= 128) {
-        if (waves == 8) attention_tile_kernel<D, FP8, 8, TK><<<grid, 512, LDS, stream>>>(a);
-    }
+    if (waves == 8) attention_tile_kernel<D, FP8, 8, TK><<<grid, 512, LDS, stream>>>(a);
     if (waves == 4) attention_tile_kernel<D, FP8, 4, TK><<<grid, 256, LDS, stream>>>(a);
     const int st = hip_ok(hipGetLastError());
     if (a.chunks == 1 || st != kOk) return st;
-    attention_join_kernel<D><<<dim3(grid.x / a.chunks * waves), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
+    const int64_t groups = grid.x / a.chunks * waves;
+    if (groups <= 256) attention_join_kernel<D, 32><<<dim3(groups * (D / 32)), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
+    else attention_join_kernel<D, D <= 128 ? D : 128><<<dim3(groups * (D <= 128 ? 1 : 2)), 256, 0, stream>>>(a, (int)waves, FP8 ? a.v_scale : nullptr);
     return hip_ok(hipGetLastError());
 }
 

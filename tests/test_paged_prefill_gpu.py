@@ -176,3 +176,43 @@ def test_a_bound_on_new_tokens_that_is_not_reached(nfp, news):
     assert_attention_close(first, ref, a)
     for _ in range(5):
         assert np.array_equal(bits(first), bits(nfp.paged_attention(_dev(q), dev, td, ld, max_new=100, max_len=300)))
+
+
+@pytest.fixture(params=[4, 8])
+def waves(nfp, request):
+    nfp.tune("attn_waves", request.param)
+    yield request.param
+    nfp.tune("attn_waves", -1)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 17)])
+@pytest.mark.parametrize("chunk", [-1, 256])
+def test_both_heights_of_a_tile(nfp, knobs, waves, chunk, window, sinks, d, fp8):
+    knobs(attn_chunk=chunk)
+    _check(nfp, [1300, 333, 95, 270], [70, 1, 95, 260], 4, 2, d, 32, fp8, window, sinks, seed=2)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_parts_of_many_tiles(nfp, knobs, waves, d, fp8):
+    # lengths that end in every part, tiles of one part among them
+    knobs(attn_chunk=256)
+    _check(nfp, [40 + 151 * i for i in range(10)], [40] * 10, 8, 8, d, 64, fp8, seed=3)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["fp16", "e4m3"])
+def test_values_that_are_not_finite_at_256_dims(nfp, waves, fp8):
+    lens, news, d = [400, 400], [150, 150], 256
+    cache, table, q = _case(lens, news, 4, 2, d, 32, fp8)
+    ref, a = attention_ref(q, cache, table, lens, news, 4, d ** -0.5)
+    cache.v[table[1, 340 // 32], 340 % 32, 1, d - 1] = 0xff if fp8 else np.float16(-np.inf)
+    got = _run(nfp, cache, table, q, lens, news)
+    assert_attention_close(got[:240], ref[:240], a[:240])
+    later = got[240:].float().cpu().numpy().reshape(-1, 4, d)
+    assert (np.isnan(later[:, 2:, d - 1]) if fp8 else later[:, 2:, d - 1] == -np.inf).all()
+    later[:, 2:, d - 1] = 0
+    want = ref[240:].copy()
+    want[:, 2:, d - 1] = 0
+    assert_attention_close(torch.from_numpy(later), want, a[240:])
