@@ -108,19 +108,22 @@ __device__ __forceinline__ bool not_finite(const floatx4 &v) {
 }
 
 // What a sequence's place in the batch and in the cache comes down to; lengths and starts that do not fit the arrays
-// they index are cut off, so that nothing outside is read.
-struct Sequence { int first, fresh, length; };
+// they index are cut off, so that nothing outside is read.  `fresh` are the new tokens that get an output, cut off at max_new and at the
+// end of Q; `past`, the position of the first of them, follows from all that the sequence has, so that a cut moves no position.
+struct Sequence { int first, fresh, past; };
 __device__ __forceinline__ Sequence sequence(const AttentionArgs &p, int b) {
     Sequence s;
-    s.length = max(0, min(p.lens[b], (int)min((int64_t)0x7fffffff, (int64_t)p.columns << (p.page_shift + 4))));
+    const int length = max(0, min(p.lens[b], (int)min((int64_t)0x7fffffff, (int64_t)p.columns << (p.page_shift + 4))));
     if (p.starts) {
-        const int from = p.starts[b], to = p.starts[b + 1];
-        s.first = max(0, min(from, p.tokens));
+        const int from = p.starts[b], to = p.starts[b + 1], begin = max(0, from);
+        s.first = min(begin, p.tokens);
         s.fresh = max(0, min(min(to, p.tokens) - s.first, p.max_new));
         if (from < 0) s.fresh = 0;
+        s.past = length - (max(to, begin) - begin);
     } else {
         s.first = b * p.per;
         s.fresh = p.per;
+        s.past = length - p.per;
     }
     return s;
 }
@@ -272,7 +275,7 @@ struct Schedule {
 __device__ __forceinline__ int up_to(int v, int multiple) { return (v + multiple - 1) / multiple * multiple; }
 // blocks that a tile of a sequence's rows has in the row: whole steps
 __device__ __forceinline__ int padded_blocks(const AttentionArgs &p, const Sequence &sq, int least) {
-    return up_to(max(1, walk(p, sq.length - sq.fresh, sq.length - 1).blocks), least);
+    return up_to(max(1, walk(p, sq.past, sq.past + sq.fresh - 1).blocks), least);
 }
 __device__ __forceinline__ Schedule schedule(const AttentionArgs &p, int tile_rows, int least) {
     constexpr int N = kScan / 64;
@@ -383,7 +386,7 @@ attention_stream_kernel(AttentionArgs p) {
             const int rows = sq.fresh * p.group, row0 = rt0 * 16 * RT;
             if (row0 >= rows || (p.few > 0 && rows > p.few)) continue;   // (the tile kernel's)
             const int row1 = min(rows, row0 + 16 * RT) - 1;
-            const int past = sq.length - sq.fresh;
+            const int past = sq.past;
             const int low_pos = past + row0 / p.group, high_pos = past + row1 / p.group;
             const Walk w = walk(p, low_pos, high_pos);
             int chunks, v1;
@@ -771,7 +774,7 @@ __device__ __forceinline__ TilePlace tile_place(const AttentionArgs &p, int tile
     const int rows = o.sq.fresh * p.group, row_tiles = (rows + tile_rows - 1) / tile_rows;
     o.row0 = (row_tiles - 1 - at.index) * tile_rows;       // rows of late tokens, which see most, first
     o.row1 = min(rows, o.row0 + tile_rows) - 1;
-    o.past = o.sq.length - o.sq.fresh;
+    o.past = o.sq.past;
     o.w = walk(p, o.past + o.row0 / p.group, o.past + o.row1 / p.group);
     o.chunks = min(p.chunks, max(1, (o.w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
     return o;
