@@ -522,10 +522,11 @@ CACHE_FP16, CACHE_E4M3 = 0, 1
 class KVCache:
     """A paged cache of keys and values as the library describes it (include/nestedfp.h has the storage).
 
-    KVCache(pages, page_tokens, kv_heads, head_dim, dtype=torch.float16 or torch.uint8 (E4M3 codes), device=...) makes the
+    KVCache(pages, page_tokens, kv_heads, head_dim, dtype=torch.float16 or torch.uint8 (E4M3 codes), device=the current GPU) makes the
     storage; KVCache(k=..., v=...) describes one that is there: contiguous [pages, kv_heads, page_tokens / 16, head_dim / E,
     16, E] keys and [pages, kv_heads, page_tokens / 16, 16 / E, head_dim, E] values, E = 8 (float16) or 16 (uint8).
-    k_scale, v_scale: float32 [kv_heads], of E4M3 caches (None: 1).  Keeps the device buffers alive."""
+    k_scale, v_scale: float32 [kv_heads], of E4M3 caches (None: 1).  Keeps the device buffers alive.
+    A cache in host memory can be looked at (keys, values); the calls refuse it."""
 
     def __init__(self, pages=0, page_tokens=0, kv_heads=0, head_dim=0, dtype=torch.float16, device=None, k=None, v=None,
                  k_scale=None, v_scale=None):
@@ -535,7 +536,7 @@ class KVCache:
             if dtype not in (torch.float16, torch.uint8):
                 raise ValueError("dtype must be float16 or uint8 (E4M3 codes)")
             e = 8 if dtype == torch.float16 else 16
-            head = (pages, kv_heads, page_tokens // 16)
+            head, device = (pages, kv_heads, page_tokens // 16), "cuda" if device is None else device
             k = torch.zeros(head + (head_dim // e, 16, e), dtype=dtype, device=device)
             v = torch.zeros(head + (16 // e, head_dim, e), dtype=dtype, device=device)
         else:
@@ -550,12 +551,15 @@ class KVCache:
         for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             if s is not None and (s.dtype != torch.float32 or s.shape != (kv_heads,) or not s.is_contiguous()):
                 raise ValueError("%s must be a contiguous float32 [kv_heads] tensor" % name)
+        if any(x is not None and x.device != k.device for x in (v, k_scale, v_scale)):
+            raise ValueError("keys, values and scales must be on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.page_tokens, self.kv_heads, self.head_dim = int(pages), int(page_tokens), int(kv_heads), int(head_dim)
         self._c = _CacheStruct(self.pages, self.page_tokens, self.kv_heads, self.head_dim,
                                CACHE_FP16 if k.dtype == torch.float16 else CACHE_E4M3, k.data_ptr(), v.data_ptr(),
                                _ptr(k_scale), _ptr(v_scale))
-        self._ref, self._at = ctypes.byref(self._c), ctypes.addressof(self._c)
+        # (_at: what the calls take; 0 for a cache that no kernel may touch)
+        self._ref, self._at = ctypes.byref(self._c), ctypes.addressof(self._c) if k.is_cuda else 0
         if pages and not lib().nestedfp_kv_cache_bytes(self._ref):
             raise ValueError("a cache has pages of 16, 32, 64, 128 or 256 tokens and heads of 64, 96, 128 or 256 dims")
 

@@ -66,6 +66,13 @@ float real(PyObject *o) {
 }
 void *address(PyObject *o) { return reinterpret_cast<void *>(whole(o)); }
 
+// the description of a cache, by its address in the binding's object; 0 stands for storage that is not on the GPU
+const nestedfp_kv_cache *cache_of(PyObject *o) {
+    const auto *cache = static_cast<const nestedfp_kv_cache *>(address(o));
+    if (cache == nullptr) refuse("cache", "on the GPU");
+    return cache;
+}
+
 Rows heads_of(PyObject *o, const char *name, int dim) {
     const Rows r = rows_of(o, name, at::kHalf, "float16 [tokens, heads * head_dim]");
     if (r.cols == 0 || r.cols % dim != 0) refuse(name, "float16 [tokens, heads * head_dim]");
@@ -109,7 +116,7 @@ PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // q, k, v, positions, slots, description of the cache, cos, sin, out, stream
 PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return call(n, 10, [&] {
-        const auto *cache = static_cast<const nestedfp_kv_cache *>(address(a[5]));
+        const auto *cache = cache_of(a[5]);
         const int dim = cache->head_dim;
         const Rows q = heads_of(a[0], "q", dim), k = heads_of(a[1], "k", dim), v = heads_of(a[2], "v", dim);
         if (k.rows != q.rows || v.rows != q.rows || k.cols != (int64_t)cache->kv_heads * dim || v.cols != k.cols)
@@ -136,7 +143,7 @@ PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // q, description of the cache, table, lens, starts, max_new, max_len, scale, window, sinks, out, workspace, stream
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return call(n, 13, [&] {
-        const auto *cache = static_cast<const nestedfp_kv_cache *>(address(a[1]));
+        const auto *cache = cache_of(a[1]);
         const int dim = cache->head_dim;
         const Rows q = heads_of(a[0], "q", dim), out = heads_of(a[10], "out", dim);
         if (out.rows != q.rows || out.cols != q.cols) refuse("out", "of the shape of q");
