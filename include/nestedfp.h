@@ -328,7 +328,7 @@ typedef struct {
     int32_t page_tokens, kv_heads, head_dim;
     int32_t type;               /* nestedfp_cache_type */
     void *k, *v;
-    const float *k_scale, *v_scale;     /* [kv_heads], E4M3 only */
+    const float *k_scale, *v_scale;     /* [kv_heads], E4M3 only; an FP16 cache that has them is an invalid argument */
 } nestedfp_kv_cache;
 
 size_t nestedfp_kv_cache_bytes(const nestedfp_kv_cache *cache_host);      /* of k, and of v; 0 for an invalid description */

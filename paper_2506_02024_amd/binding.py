@@ -549,6 +549,8 @@ class KVCache:
                 raise ValueError("v must be contiguous [pages, kv_heads, blocks, 16 / E, head_dim, E]")
             pages, kv_heads, page_tokens = head[0], head[1], head[2] * 16
         for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if s is not None and k.dtype != torch.uint8:
+                raise ValueError("%s goes with E4M3 codes; an FP16 cache holds the values themselves" % name)
             if s is not None and (s.dtype != torch.float32 or s.shape != (kv_heads,) or not s.is_contiguous()):
                 raise ValueError("%s must be a contiguous float32 [kv_heads] tensor" % name)
         if any(x is not None and x.device != k.device for x in (v, k_scale, v_scale)):

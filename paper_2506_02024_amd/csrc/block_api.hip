@@ -31,6 +31,7 @@ static int check_cache(const nestedfp_kv_cache *c) {
 // what the kernels need in memory
 static int check_storage(const nestedfp_kv_cache *c) {
     if (c->k == nullptr || c->v == nullptr) return kErrArg;
+    if (c->type == NESTEDFP_CACHE_FP16 && (c->k_scale != nullptr || c->v_scale != nullptr)) return kErrArg;      // (nothing multiplies by them)
     return on(c->k, 16) && on(c->v, 16) && on(c->k_scale, 4) && on(c->v_scale, 4) ? kOk : kErrShape;
 }
 

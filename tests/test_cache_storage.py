@@ -51,3 +51,21 @@ def test_only_the_cache_is_in_host_memory(nfp):
 def test_storage_is_made_on_the_gpu(nfp):
     cache = nfp.KVCache(2, 16, 1, 64)
     assert cache.k.is_cuda and cache.v.is_cuda and cache._at
+
+
+def test_scales_of_an_fp16_cache_are_refused(nfp):
+    import ctypes
+
+    for name in ("k_scale", "v_scale"):
+        with pytest.raises(ValueError, match="E4M3"):
+            nfp.KVCache(2, 16, 1, 64, device="cpu", **{name: torch.ones(1)})
+        assert getattr(nfp.KVCache(2, 16, 1, 64, torch.uint8, device="cpu", **{name: torch.ones(1)}), name) is not None
+    fake = 0x10000                                     # aligned, never dereferenced
+    for kind, status in ((nfp.CACHE_FP16, nfp.ERR_ARG), (nfp.CACHE_E4M3, nfp.ERR_WORKSPACE)):
+        for scales in ((fake, None), (None, fake)):
+            c = nfp._CacheStruct(8, 16, 2, 64, kind, fake, fake, *scales)
+            assert nfp.lib().nestedfp_paged_attention(fake, 4, 256, 4, ctypes.byref(c), fake, 10, 10, fake, 4, None, 1, 100000, 0.1, 0, 0, fake, 256,
+                                                      None, 0, None) == status
+            if kind == nfp.CACHE_FP16:
+                assert nfp.lib().nestedfp_rope_append(fake, 256, fake, 128, fake, 128, 3, 4, fake, fake, 10, 64, fake, fake, fake, 256,
+                                                      ctypes.byref(c), None) == nfp.ERR_ARG
