@@ -824,7 +824,7 @@ attention_tile_kernel(AttentionArgs p) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = -q[s];
     }
-    scale = fmaxf(scale, 1e-30f);                                // (zero: a masked score has to stay -Inf)
+    scale = scale < 1e-30f ? 1e-30f : scale;                     // (zero: a masked score has to stay -Inf; a NaN stays one)
     const int in_page = (1 << p.page_shift) - 1;
     // the row of S^T that this lane's operand of K holds is one of these tokens of a half: with it the lane's scores are those of the 8
     // tokens that its operand of V holds (8 h ... of each block)
