@@ -411,7 +411,7 @@ int nestedfp_probe_mfma(const void *operands, int fp8, int iters, uint32_t *sink
  * (not thread-safe; a call that runs while another thread changes a knob may size its
  * workspace for one launch shape and launch another).  knob names are listed in
  * nestedfp_tune_name(i), i = 0.. until NULL.  value < 0 restores the built-in choice.
- * Returns NESTEDFP_ERR_ARG for unknown knobs.
+ * Returns NESTEDFP_ERR_ARG for unknown knobs, and for values that name a kernel there is none of (attn_waves: 4 or 8).
  */
 int nestedfp_tune(const char *knob, int64_t value);
 const char *nestedfp_tune_name(int index);

@@ -720,7 +720,10 @@ int nestedfp_tune(const char *knob, int64_t value) {
     else if (!strcmp(knob, "tuned_table")) t.tuned_table = value;
     else if (!strcmp(knob, "quant_onepass")) t.quant_onepass = value;
     else if (!strcmp(knob, "attn_tiles")) t.attn_tiles = value;
-    else if (!strcmp(knob, "attn_waves")) t.attn_waves = value;
+    else if (!strcmp(knob, "attn_waves")) {
+        if (value > 0 && value != 4 && value != 8) return NESTEDFP_ERR_ARG;     // (there is no kernel for another number)
+        t.attn_waves = value;
+    }
     else if (!strcmp(knob, "attn_groups")) t.attn_groups = value;
     else if (!strcmp(knob, "attn_chunk")) t.attn_chunk = value;
     else return NESTEDFP_ERR_ARG;
