@@ -367,7 +367,8 @@ int nestedfp_rope_append(const uint16_t *Q, int64_t ldq, const uint16_t *K, int6
  * the last row of Q has no output, those before it keep their positions).
  * Scores, sums and accumulators are binary32, O is FP16 [tokens, heads * head_dim] (row stride ldo); strides are multiples of 8,
  * Q 16-byte and O 8-byte aligned.
- * The workspace follows the rules above (WORKSPACE); where a sequence is split over workgroups they leave their sums in it.
+ * The workspace follows the rules above (WORKSPACE); where a sequence is split over workgroups they leave their sums in it.  It is never
+ * larger than 256 MiB and 16 KiB, whatever the batch and the lengths (unless nestedfp_tune pins the parts' length).
  * The results do not depend on timing: the parts are joined in order.
  */
 size_t nestedfp_paged_attention_workspace_size(int64_t tokens, int64_t batch, int64_t heads,

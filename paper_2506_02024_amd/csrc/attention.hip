@@ -776,7 +776,8 @@ __device__ __forceinline__ TilePlace tile_place(const AttentionArgs &p, int tile
     o.row1 = min(rows, o.row0 + tile_rows) - 1;
     o.past = o.sq.past;
     o.w = walk(p, o.past + o.row0 / p.group, o.past + o.row1 / p.group);
-    o.chunks = min(p.chunks, max(1, (o.w.blocks + p.chunk_blocks - 1) / p.chunk_blocks));
+    // (the workspace has room for the parts of the first split_tiles alone)
+    o.chunks = tile / p.kv_heads < p.split_tiles ? min(p.chunks, max(1, (o.w.blocks + p.chunk_blocks - 1) / p.chunk_blocks)) : 1;
     return o;
 }
 
@@ -1223,12 +1224,14 @@ static void plan_launch(AttentionLaunch &a, const AttentionShape &s, int64_t til
     a.partial_bytes = a.chunks > 1 ? (size_t)a.tiles * (size_t)a.chunks * (size_t)a.part_rows * (size_t)(s.D + 2) * sizeof(float) : 0;
 }
 
+constexpr size_t kMostPartBytes = (size_t)256 << 20;   // parts of the tile kernel; a full chip's are 68 MB at 256 dims
+
 AttentionPlan attention_plan(const AttentionShape &s) {
     AttentionPlan a;
     const int64_t rows = s.max_new * s.group, stream_rows = s.D > 128 ? 16 : 32;      // (two tiles of 256 dims do not fit the registers)
     a.few = 0;
     a.scan = false;
-    a.stream.tiles = a.tile.tiles = 0;
+    a.stream.tiles = a.tile.tiles = a.stream.split_tiles = a.tile.split_tiles = 0;
     a.stream.partial_bytes = a.tile.partial_bytes = 0;
     const bool many = tuning().attn_tiles >= 0 ? tuning().attn_tiles > 0 : rows > stream_rows;
     if (many) {
@@ -1255,6 +1258,15 @@ AttentionPlan attention_plan(const AttentionShape &s) {
         a.tile.tiles = most * s.kv_heads;
         a.tile.part_rows = tile_rows;
         plan_launch(a.tile, s, tile_rows, likely * s.kv_heads, s.D > 128 ? 8 : 16, a.waves == 8 || s.D > 128 ? 256 : 512, false);
+        // Where every sequence may have a tile that it does not fill there can be many times the likely tiles: room for the parts of all of
+        // them, up to a bound (it would be 1.7 GB for 1600 tokens in 1000 sequences at 256 dims).  Tiles behind it are whole; so many fill the
+        // chip as they are.  Room for twice the likely ones and 8 more instead: 85 sequences of 9 tokens before 512 tokens after
+        // 16384, whose tiles are the last, 540 us instead of 385 (102 MB instead of 224).
+        const size_t each = (size_t)(s.kv_heads * a.tile.chunks * tile_rows * (s.D + 2)) * sizeof(float);
+        const size_t split = std::min((size_t)most, kMostPartBytes / each);
+        if (split == 0) a.tile.chunks = 1;
+        a.tile.split_tiles = (int64_t)split;
+        a.tile.partial_bytes = a.tile.chunks > 1 ? split * each : 0;
     }
     if (!many || a.few > 0) {
         const int64_t most = many ? a.few / s.group * s.group : rows;
@@ -1284,6 +1296,7 @@ static bool shape_of(const AttentionLaunch &l, AttentionArgs &a, dim3 &grid) {
     a.part_rows = (int)l.part_rows;
     a.chunk_blocks = (int)l.chunk_blocks;
     a.chunks = (int)l.chunks;
+    a.split_tiles = (int)l.split_tiles;
     grid = dim3((unsigned)groups);
     return true;
 }

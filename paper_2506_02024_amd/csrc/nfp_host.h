@@ -241,10 +241,11 @@ struct AttentionArgs {
     int32_t tokens, batch, per, max_new, columns;      // per: new tokens of every sequence where there are no starts
     int32_t kv_heads, group, pages, page_shift, window, sinks;
     int32_t row_tiles, part_rows, chunk_blocks, chunks, few;
+    int32_t split_tiles;                               // tile kernel: row tiles before this one may be split
     bool scan, fixed;                                  // workgroups work out who does what; in stretches of chunk_blocks
 };
 struct AttentionShape { int64_t tokens, batch, kv_heads, group, D, max_new, max_len, window, sinks;  bool fp8, ragged; };
-struct AttentionLaunch { int64_t row_tiles, part_rows, chunk_blocks, chunks, tiles;  size_t partial_bytes; };
+struct AttentionLaunch { int64_t row_tiles, part_rows, chunk_blocks, chunks, tiles, split_tiles;  size_t partial_bytes; };
 // few > 0: sequences of up to `few` rows go to the streaming kernel, the others to the tile kernel
 struct AttentionPlan { AttentionLaunch stream, tile;  int64_t few, rt, waves;  bool scan;  size_t partial_bytes; };
 AttentionPlan attention_plan(const AttentionShape &s);
