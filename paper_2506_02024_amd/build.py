@@ -57,9 +57,10 @@ def _marshal_command():
             "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
-def build_library(verbose=False):
-    """Compiles every source to an object of its own (in parallel, under _build/) and links them; beside it the
-    compiled part of the binding."""
+def build_library(verbose=False, binding=True):
+    """Compiles every source to an object of its own (in parallel, under _build/) and links them; beside it, unless `binding` is
+    false, the compiled part of the Python binding.  That one needs Python's and torch's headers and a host compiler, which the library
+    does not: where it fails the library is built all the same, and the error comes afterwards."""
     from concurrent.futures import ThreadPoolExecutor
 
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -69,14 +70,18 @@ def build_library(verbose=False):
     objs = [os.path.join(objdir, os.path.basename(s)[:-4] + ".o") for s in srcs]
     cmds = [[hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-c", s, "-o", o]
             for s, o in zip(srcs, objs)]
-    cmds.append(_marshal_command())
-    jobs = min(len(cmds), int(os.environ.get("MAX_JOBS", "0")) or os.cpu_count() or 1)
+    jobs = min(len(cmds) + bool(binding), int(os.environ.get("MAX_JOBS", "0")) or os.cpu_count() or 1)
     with ThreadPoolExecutor(max_workers=jobs) as pool:
+        marshal = pool.submit(lambda: _run(_marshal_command(), verbose)) if binding else None
         list(pool.map(lambda c: _run(c, verbose), cmds))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs, verbose)
+    if marshal is not None and marshal.exception() is not None:
+        raise RuntimeError("the library is built (%s), the compiled part of the Python binding is not" % LIB) from marshal.exception()
     return LIB
 
 
 if __name__ == "__main__":
-    build_library(verbose=True)
+    import sys
+
+    build_library(verbose=True, binding="--no-binding" not in sys.argv[1:])
     print("built", LIB)
