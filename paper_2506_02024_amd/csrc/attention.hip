@@ -255,19 +255,6 @@ __device__ __forceinline__ int sum_to_lane(int v) {
     v = plus_before<0x142, 0xa>(v);                    // the last lane of the row before
     return plus_before<0x143, 0xc>(v);                 // lane 31
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float plus_before(float v) {
-    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
-}
-__device__ __forceinline__ float sum_of_lanes(float v) {
-    v = plus_before<0x111, 0xf>(v);
-    v = plus_before<0x112, 0xf>(v);
-    v = plus_before<0x114, 0xf>(v);
-    v = plus_before<0x118, 0xf>(v);
-    v = plus_before<0x142, 0xa>(v);
-    v = plus_before<0x143, 0xc>(v);
-    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
-}
 struct Schedule {
     int begin[kScan / 64];                             // of sequence 64 i + lane in the row of all blocks
     int all, share;                                    // blocks, and of them a workgroup's
