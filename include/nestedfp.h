@@ -360,13 +360,14 @@ int nestedfp_rope_append(const uint16_t *Q, int64_t ldq, const uint16_t *K, int6
  *   max_new, max_len   no sequence has more new tokens, or more tokens, than this.  They size the launch: a new token past max_new
  *                      gets no output (those before it get theirs, at their own positions); a sequence longer than max_len costs time, its
  *                      result is the same
- *   window, sinks      a new token at position pos sees t <= pos and, with window > 0, of these only t > pos - window and t < sinks
+ *   window, sinks      a new token at position pos sees t <= pos, with window > 0 of these only those after pos - window and those before sinks
  * A new token that sees nothing (its sequence's length is smaller than its new tokens) gets zeros.  Pages that no new token sees are
  * not read, nor are their entries in the table; values that no new token sees may hold anything.  An entry outside the
  * cache where a token is seen gives NaN; lengths and starts outside their arrays are cut off (a new token past
  * the last row of Q has no output, those before it keep their positions).
- * Scores, sums and accumulators are binary32, O is FP16 [tokens, heads * head_dim] (row stride ldo); strides are multiples of 8,
- * Q 16-byte and O 8-byte aligned.
+ * Scores, sums and accumulators are binary32; where a sequence has more than 32 rows (new tokens times query heads of a key/value
+ * head; 16 at 256 dims) the probabilities that multiply the values are rounded to FP16, 2^-11 of each at most.
+ * O is FP16 [tokens, heads * head_dim] (row stride ldo); strides are multiples of 8, Q 16-byte and O 8-byte aligned.
  * The workspace follows the rules above (WORKSPACE); where a sequence is split over workgroups they leave their sums in it.  It is never
  * larger than 256 MiB and 16 KiB, whatever the batch and the lengths (unless nestedfp_tune pins the parts' length).
  * The results do not depend on timing: the parts are joined in order.

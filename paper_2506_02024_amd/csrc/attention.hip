@@ -313,7 +313,7 @@ __device__ __forceinline__ int place_of(const Schedule &plan, int x, int batch, 
 // P is carried as two FP16 terms (its FP16 rounding and the rest): the second product costs nothing here, and the
 // result then has the precision of the 32-bit sums.
 // Measured (128 dims, 8 key/value heads; a read-only stream reaches 7.15 TB/s): 768 equal tiles of 1600 tokens 96 us (6.6 TB/s), one token over
-// 131072 84 us (6.4), 32 sequences of 500 ... 8192 tokens 67 us (5.5), 48 of 1000 ... 20000 in E4M3 113 us (5.6), one of 613 8.6 us.  Beside
+// 131072 84 us (6.4), 32 sequences of 500 ... 8192 tokens 67 us (5.5), 48 of 1000 ... 20000 in E4M3 113 us (5.6), one of 613 8.9 us.  Beside
 // the bytes a call costs about 9 us: launch, lengths, page numbers and first keys one after the other, at the end sums, ticket
 // and join.
 // Tried and dropped: the next step's loads under way during the work on one (two steps of registers, 113 -> 122 us on the 48 sequences);
@@ -686,11 +686,16 @@ attention_stream_kernel(AttentionArgs p) {
 // values of TK tokens at a time go through two buffers of LDS, which all waves read, in the storage's own order: a wave's operand reads
 // are contiguous, nothing is transposed.  E4M3 codes become FP16 on their way into LDS, once for all rows.
 // A row's probabilities are taken relative to a maximum that follows the true one only when that is 2^kLag larger, so that
-// the sums are rarely rescaled; P is rounded to FP16 (2^-12 of a probability on average, as much as the output's own rounding) and its
-// sum is that of the rounded values.  32 rows per wave: a wave's operand reads from LDS then take as long as its products.
-// Measured: a prompt of 8192 tokens (32 query heads, 128 dims; 16, 256 dims alike) 590-600 us, 915-935 TFLOP/s; a large matrix product of the
-// vendor's library reaches 1336 on this card, the matrix pipe alone 1580 under the power limit.  What is left are the exponentials: 512 of a wave's 2000
-// issue cycles per step of 64 tokens, beside 400 of other vector work and 1024 of the pipe.
+// the sums are rarely rescaled.  P is rounded to FP16, as much as the output's own rounding, and its sum is that of the rounded values.  The
+// output is then 2.5e-4 to 2.9e-4 off (2-norm, against 64 bits) where the rounding of the output alone is 2.0e-4.  With P as two terms, as in the
+// streaming kernel, it is 2.0e-4, and a prompt of 8192 takes 786 us instead of 583, one of 2048 at 256 dims 110 / 90, 512 tokens after
+// 8192 116 / 89, two chunks of 600 beside decoding sequences 204 / 168, 777 tokens of 64 dims 18.1 / 17.1: half as many products
+// again and the vector work that makes the second term, which the streaming kernel has for nothing.
+// 32 rows per wave: a wave's operand reads from LDS then take as long as its products.
+// Measured: a prompt of 8192 tokens (32 query heads, 128 dims; 16, 256 dims alike) 583-600 us, 915-945 TFLOP/s; a large matrix product of the
+// vendor's library reaches 1336 on this card, the matrix pipe alone 1580 under the power limit.  By the counters a step of 64 tokens takes 2240
+// cycles of a SIMD for each of its two waves: the matrix pipe is busy for 1024 of them (46 %), vector instructions issue for 917 (41 %; 160 beside the
+// 32 products, 32 exponentials among them), so that the two hardly overlap.
 // Tried and dropped: scores one step ahead of their use (692 us), with an order of instructions given (643, 660); halves of the waves
 // taking turns at the pipe with two barriers per step (688, with raised priority 677).
 constexpr float kLag = 8.0f;
@@ -1336,6 +1341,8 @@ int launch_attention(const AttentionShape &s, const AttentionPlan &plan, Attenti
         // (the lengths are bounded by the table alone, and the blocks of all tiles are counted in 31 bits)
         a.scan = plan.scan && plan.stream.tiles * (((int64_t)a.columns << a.page_shift) + 16) < (int64_t)1 << 30;
         a.fixed = tuning().attn_chunk > 0;
+        // 256 workgroups up to 128 tiles, 512 above (microseconds with 256 / 512: one sequence of 8192 15.4 / 21.7, of 131072 84.3 / 90.5, 8 of 4096
+        // 26.7 / 27.8, 12 with a window of 4096, 120 tiles, 50.9 / 52.9): of 512 more share a tile, and meet in its join
         if (a.scan) grid = dim3((unsigned)std::min<int64_t>(grid.x, tuning().attn_groups > 0 ? tuning().attn_groups : plan.stream.tiles <= 128 ? 256 : 512));
 #define NFP_STREAM(D, FP8) launch_stream<D, FP8>(plan.rt, a, grid, stream)
         NFP_FOR_D(NFP_STREAM)

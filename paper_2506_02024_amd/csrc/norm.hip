@@ -3,8 +3,8 @@
 // HBM-bound: 2 + 2 bytes read and 2 + 2 (FP16) or 2 + 1 (codes) written per element.  A row stays in the registers of one
 // workgroup from its only read to its last write; the two statistics (sum of squares, largest magnitude) each cost
 // one exchange between its waves.  As many lanes as the row has chunks of 8 values, so that a few rows take one load's latency.
-// Measured: 8192 rows of 4096 to codes 42.6 us (5.5 TB/s; a large copy reaches 4.9), 48 of 5120 to both 4.2 us, one of 1040 2.2 us
-// (of which an empty kernel takes 1.5).
+// Measured: 8192 rows of 4096 to codes 42.6 us (5.5 TB/s; a large copy reaches 4.9), 48 of 5120 to both 4.2 us, one of 1040 2.0 us
+// (of which an empty kernel takes 1.5).  The counters of the large case read 134 and write 101 MB: nothing twice.
 #include "nfp_device.h"
 #include "nfp_host.h"
 
