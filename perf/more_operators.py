@@ -130,6 +130,12 @@ def _normal(g, shape, sigma=1.0):
     return torch.empty(shape, dtype=torch.float16, device=DEVICE).normal_(0.0, sigma, generator=g)
 
 
+def _scales(x):
+    """Largest magnitude of every row over 448, one division (by a number, torch multiplies by its reciprocal); 1 for a row of zeros."""
+    amax = x.abs().amax(1)
+    return torch.where(amax == 0, torch.ones_like(amax), amax / torch.full_like(amax, 448.0))
+
+
 def prepare(case, seed):
     g = torch.Generator(device=DEVICE)
     g.manual_seed(seed)
@@ -143,7 +149,7 @@ def prepare(case, seed):
         s["residual"] = _normal(g, (m, out)) if case["residual"] else None
         if case["codes"]:                              # (what the norm in front of the linear left)
             x = s["x"].float()
-            s["scales"] = (x.abs().amax(1) / 448.0).contiguous()
+            s["scales"] = _scales(x)
             s["codes"] = (x / s["scales"][:, None]).clamp(-448.0, 448.0).to(torch.float8_e4m3fn).view(torch.uint8)
     else:
         k, e, top = case["hidden"], case["experts"], case["top_k"]
@@ -250,7 +256,7 @@ def _run_fused(s):
         x = s["codes"].view(torch.float8_e4m3fn).float() * s["scales"][:, None]
     else:
         x = s["x"].float()
-        scale = x.abs().amax(1, keepdim=True) / 448.0
+        scale = _scales(x)[:, None]
         x = (x / scale).clamp(-448.0, 448.0).to(torch.float8_e4m3fn).float() * scale
     z = x @ _weight(s, "w").T
     if s["bias"] is not None:
@@ -333,7 +339,7 @@ def exact(case, seed):
         x = s["x"].to(wide)
         if case["mode"] == "fp8":                      # (codes and scales are part of the definition, in 32 bits)
             amax = s["x"].abs().amax(1).float()
-            scale = torch.where(amax == 0, torch.ones_like(amax), amax / 448.0)
+            scale = torch.where(amax == 0, torch.ones_like(amax), torch.div(amax, torch.tensor([448.0], device=DEVICE)))
             codes = (s["x"].float() / scale[:, None]).clamp(-448.0, 448.0).to(torch.float8_e4m3fn)
             x = codes.to(wide) * scale.to(wide)[:, None]
         z = torch.matmul(x, weight(s["w"]).t().contiguous())
