@@ -287,6 +287,92 @@ int nestedfp_linear(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_la
                     void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * A linear with an epilogue: bias, activation and residual are applied to the FP32 sums before these are rounded, which saves a pass
+ * over the outputs for each of them and a rounding for all but the last.
+ *   z = X * W^T + bias                       (the linear of the layer in `mode`, as nestedfp_linear; FP8 mode: the scaled sums)
+ *   Y = fp16(act(z) + residual)              gated == 0
+ *   Y[m,f] = fp16(act(z[m,2f]) * z[m,2f+1] + residual[m,f])     gated == 1: the layer's rows are gate and up rows in turn, N is even,
+ *                                            and Y and residual have N / 2 columns
+ *   act(z) = z, max(z, 0), z / (1 + exp(-z)) or z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; an Inf or a NaN stays in its outputs.
+ * bias is FP16 [N] (in the order of the layer's rows), residual FP16 with row stride ldr (any; at most 2^31); either may be NULL, and residual may be Y
+ * (ldr == ldy then).  8-byte aligned ones with N % 4 == 0 and ldr % 4 == 0 are loaded fastest.  The description lives in HOST memory.
+ * The workspace is that of nestedfp_linear (nestedfp_linear_workspace_size).  ldy as for the GEMM calls, of the N or N / 2 columns.
+ * The _prequantized form takes E4M3 activations as nestedfp_gemm_fp8_prequantized does (Xq dense [M,K]; e.g. those of nestedfp_add_rms_norm)
+ * and multiplies them by the upper plane; an exception layer, which has none, is NESTEDFP_ERR_RANGE.
+ */
+typedef enum {
+    NESTEDFP_ACT_NONE = 0,
+    NESTEDFP_ACT_RELU = 1,
+    NESTEDFP_ACT_SILU = 2,
+    NESTEDFP_ACT_GELU = 3       /* the form with a tangent */
+} nestedfp_activation;
+
+typedef struct {
+    const uint16_t *bias;
+    const uint16_t *residual;
+    int64_t ldr;
+    int32_t activation;         /* nestedfp_activation */
+    int32_t gated;
+} nestedfp_epilogue;
+
+int nestedfp_linear_fused(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_layer *layer_host, int mode,
+                          const float *act_scale, const nestedfp_epilogue *epilogue_host, uint16_t *Y, int64_t ldy,
+                          void *workspace, size_t workspace_bytes, void *stream);
+int nestedfp_linear_fused_prequantized(const uint8_t *Xq, const float *scales, int64_t M, const nestedfp_layer *layer_host,
+                                       const nestedfp_epilogue *epilogue_host, uint16_t *Y, int64_t ldy,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A mixture of experts: the router, and the experts of a few tokens.
+ *
+ * moe_route: for each of M tokens (X [M,K], row stride ldx) the top_k of `experts` experts.
+ *   logit[e] = sum_k X[m,k] R[e,k]            R is FP16 [experts,K], row stride ldr; in binary64
+ *   score    = softmax(logit) over all experts, or 1 / (1 + exp(-logit))     (scoring; in binary64)
+ *   choice   = score + bias[e]                (bias: float [experts] or NULL, without which the logits are compared)
+ *   ids[m]     the top_k largest choices in falling order, the lowest index first of equal ones, int32 [M,top_k]
+ *   weights[m] score of each (/ their sum if renormalize) * factor, float [M,top_k], rounded once
+ * A NaN is chosen after all numbers; the ids of a token are different experts whatever its activations hold.  1 <= top_k <= 32, top_k <= experts
+ * <= 512; K is a multiple of 16, strides are multiples of 8 and at most 2^21, X and R 16-byte aligned.  The workspace follows the rules above
+ * (WORKSPACE): it holds logits, 32 MiB and 16 KiB at most.
+ */
+typedef enum {
+    NESTEDFP_SCORE_SOFTMAX = 0,
+    NESTEDFP_SCORE_SIGMOID = 1
+} nestedfp_scoring;
+
+size_t nestedfp_moe_route_workspace_size(int64_t M, int64_t experts, int64_t K);
+int nestedfp_moe_route(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const uint16_t *R, int64_t experts, int64_t ldr,
+                       int64_t top_k, int scoring, int renormalize, float factor, const float *bias,
+                       int32_t *ids, float *weights, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * moe: Y[m] = fp16(residual[m] + sum_j weights[m,j] * down_e (act(gate_e x_m) * up_e x_m)),  e = ids[m,j],  for M tokens, 1 ... 64 (more are
+ * NESTEDFP_ERR_SHAPE: their experts' products are large enough for linears of their own).
+ *   experts: a description in HOST memory.  `up` is the stacked matrix [experts * 2 ffn, hidden], an expert's gate and up rows in turn (gate row f
+ *     at 2 f, up row f at 2 f + 1), `down` [experts * hidden, ffn]; either as the row-major planes that nestedfp_decompose writes of it
+ *     or, with is_exception, as dense FP16.  hidden and ffn are multiples of 16, experts <= 512, an expert's FP16 matrices below 2 GiB.
+ *   FP16 mode multiplies the exact FP16 weights, FP8 mode the upper planes' values (E4M3 times 2^-8; the lower planes are not read and may be
+ *     NULL); activations are FP16 in both modes.  An exception ignores the mode.
+ *   ids (int32) and weights (float) are dense [M,top_k], 1 <= top_k <= 32, and may come from anywhere: an id outside 0 ... experts - 1 adds nothing (experts of other
+ *     GPUs, tokens that are padding), one that a token names twice counts with the sum of its weights.
+ *   residual (FP16, row stride ldr, or NULL) and X may be Y.  Strides of X are multiples of 8, X and the weights 16-byte aligned.
+ * Sums are binary32.  The activated products lie in the workspace as two FP16 terms (2^-22 of each; above 65504 they are infinite, as a linear's outputs).
+ * The results do not depend on timing.  The workspace follows the rules above (WORKSPACE).
+ */
+typedef struct {
+    int64_t experts, hidden, ffn;
+    int32_t is_exception;
+    int32_t activation;         /* nestedfp_activation */
+    const void *up_upper, *up_lower;        /* planes; is_exception: FP16 in up_upper and down_upper */
+    const void *down_upper, *down_lower;
+} nestedfp_experts;
+
+size_t nestedfp_moe_workspace_size(int64_t M, const nestedfp_experts *experts_host, int64_t top_k);
+int nestedfp_moe(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_experts *experts_host, int mode,
+                 const int32_t *ids, const float *weights, int64_t top_k, const uint16_t *residual, int64_t ldr,
+                 uint16_t *Y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * What stands around the linears of a decoder layer: the norm in front of qkv and gate/up, and between qkv and o the
  * rotary positions, the key/value cache and the attention that reads it.
  *

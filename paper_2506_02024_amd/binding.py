@@ -110,6 +110,18 @@ def lib():
     L.nestedfp_paged_attention.restype = ci
     L.nestedfp_paged_attention.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, vp, i64, vp, i64, i64, f32, i64, i64, vp, i64,
                                            vp, sz, vp]
+    L.nestedfp_linear_fused.restype = ci
+    L.nestedfp_linear_fused.argtypes = [vp, i64, i64, vp, ci, vp, vp, vp, i64, vp, sz, vp]
+    L.nestedfp_linear_fused_prequantized.restype = ci
+    L.nestedfp_linear_fused_prequantized.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    L.nestedfp_moe_route_workspace_size.restype = sz
+    L.nestedfp_moe_route_workspace_size.argtypes = [i64, i64, i64]
+    L.nestedfp_moe_route.restype = ci
+    L.nestedfp_moe_route.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, ci, ci, f32, vp, vp, vp, vp, sz, vp]
+    L.nestedfp_moe_workspace_size.restype = sz
+    L.nestedfp_moe_workspace_size.argtypes = [i64, vp, i64]
+    L.nestedfp_moe.restype = ci
+    L.nestedfp_moe.argtypes = [vp, i64, i64, vp, ci, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     L.nestedfp_tune.restype = ci
     L.nestedfp_tune.argtypes = [c.c_char_p, i64]
     L.nestedfp_tune_name.restype = c.c_char_p
@@ -130,7 +142,7 @@ def _marshalled():
         from . import _marshal as m
 
         m.bind(*(ctypes.cast(getattr(L, "nestedfp_" + name), ctypes.c_void_p).value
-                 for name in ("add_rms_norm", "rope_append", "paged_attention")))
+                 for name in ("add_rms_norm", "rope_append", "paged_attention", "linear_fused", "linear_fused_prequantized", "moe_route", "moe")))
         _marshal = m
     return _marshal
 
@@ -472,7 +484,7 @@ class Layer:
 
     def _describe(self, c):
         # what linear() needs of it, taken out once (two field reads and a reference cost 0.3 us)
-        self._c, self._ref, self._dims = c, ctypes.byref(c), (int(c.N), int(c.K))
+        self._c, self._ref, self._dims, self._at = c, ctypes.byref(c), (int(c.N), int(c.K)), ctypes.addressof(c)
 
     c = property(lambda self: self._c, _describe)              # the struct that the library reads
     shape = property(lambda self: self._dims)
@@ -494,6 +506,107 @@ def linear(X, layer, mode, act_scale=None, out=None, workspace=None):
     st = lib().nestedfp_linear(_ptr(X), M, ldx, layer._ref, int(mode), _ptr(act_scale),
                                _ptr(out), ldy, _ptr(workspace), workspace.numel(), _stream())
     _check(st, "nestedfp_linear")
+    return out
+
+
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)         # ACT_GELU: the form with a tangent
+
+
+def interleave_gate_up(w):
+    """Gate rows before up rows ([2 ffn, ..]) -> gate and up rows in turn, as linear_fused(gated=True) wants a layer's weights and its bias."""
+    return w.unflatten(0, (2, w.shape[0] // 2)).transpose(0, 1).flatten(0, 1).contiguous()
+
+
+def linear_fused_workspace_size(M, layer, mode):
+    return int(lib().nestedfp_linear_workspace_size(int(M), layer._ref, int(mode)))
+
+
+def linear_fused(X, layer, mode, bias=None, activation=ACT_NONE, gated=False, residual=None, act_scale=None, scales=None, out=None,
+                 workspace=None):
+    """A linear with an epilogue, rounded once: act(X @ W^T + bias) + residual for a Layer in the given mode or, gated, the products of the
+    activated gate rows and the up rows (+ residual), for a layer whose rows are gate and up rows in turn (interleave_gate_up).
+
+    X: float16 [M,K], or E4M3 codes (uint8 [M,K], contiguous) with their scales (float32 [M]), for which the mode is FP8.  bias: float16
+    [N]; residual: float16 [M, N or N / 2], may be out.  Exception layers run in FP16 and take no codes."""
+    N = layer._dims[0]
+    if out is None:
+        out = torch.empty((X.shape[0], N // 2 if gated else N), dtype=torch.float16, device=X.device)
+    if workspace is None:
+        workspace = _workspace(lib().nestedfp_linear_workspace_size(X.shape[0], layer._ref, MODE_FP8 if scales is not None else int(mode)), X.device)
+    st = (_marshal or _marshalled()).linear_fused(X, scales, layer._at, mode, act_scale, bias, activation, gated, residual, out, workspace, _stream())
+    if st:
+        raise NestedFPError(st, "nestedfp_linear_fused")
+    return out
+
+
+class _ExpertsStruct(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int64), ("hidden", ctypes.c_int64), ("ffn", ctypes.c_int64), ("is_exception", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("up_upper", ctypes.c_void_p), ("up_lower", ctypes.c_void_p), ("down_upper", ctypes.c_void_p),
+                ("down_lower", ctypes.c_void_p)]
+
+
+class Experts:
+    """The experts of a layer as the library describes them: row-major planes of gate and up ([experts, 2 ffn, hidden], gate rows first; laid out
+    anew here) and of down ([experts, hidden, ffn]), or the FP16 weights themselves if any |w| > 1.75.  Keeps the device buffers alive."""
+
+    def __init__(self, gate_up, down, activation=ACT_SILU):
+        if gate_up.dim() != 3 or down.dim() != 3 or gate_up.dtype != torch.float16 or down.dtype != torch.float16:
+            raise ValueError("gate_up must be float16 [experts, 2 ffn, hidden] and down [experts, hidden, ffn]")
+        experts, hidden, ffn = down.shape
+        if tuple(gate_up.shape) != (experts, 2 * ffn, hidden):
+            raise ValueError("gate_up must be [experts, 2 ffn, hidden] where down is [experts, hidden, ffn]")
+        turned = gate_up.unflatten(1, (2, ffn)).transpose(1, 2).reshape(experts * 2 * ffn, hidden)
+        flat = down.reshape(experts * hidden, ffn)
+        up, down = Layer(turned), Layer(flat)
+        self.is_exception = up.is_exception or down.is_exception
+        self._keep = (turned, flat) if self.is_exception else (up, down)
+        parts = (turned, None, flat, None) if self.is_exception else (up.upper, up.lower, down.upper, down.lower)
+        self.count, self.hidden, self.ffn = int(experts), int(hidden), int(ffn)
+        self._c = _ExpertsStruct(experts, hidden, ffn, int(self.is_exception), int(activation), *(_ptr(t) for t in parts))
+        self._ref, self._at = ctypes.byref(self._c), ctypes.addressof(self._c)
+
+
+def moe_route_workspace_size(M, experts, K):
+    return int(lib().nestedfp_moe_route_workspace_size(int(M), int(experts), int(K)))
+
+
+def moe_route(X, router, top_k, scoring="softmax", renormalize=True, bias=None, factor=1.0, ids=None, weights=None, workspace=None):
+    """The top_k experts of every row of X (float16 [M,K]) by the router's weights (float16 [experts,K]): (ids int32 [M,top_k] in falling order of the
+    choice, weights float32 [M,top_k]).  scoring: "softmax" or "sigmoid"; bias: float32 [experts], added to the scores for the choice alone;
+    renormalize: weights are divided by their sum; factor multiplies them."""
+    if scoring not in ("softmax", "sigmoid"):
+        raise ValueError('scoring must be "softmax" or "sigmoid"')
+    M, K = X.shape
+    if ids is None:
+        ids = torch.empty((M, top_k), dtype=torch.int32, device=X.device)
+    if weights is None:
+        weights = torch.empty((M, top_k), dtype=torch.float32, device=X.device)
+    if workspace is None:
+        workspace = _workspace(moe_route_workspace_size(M, router.shape[0], K), X.device)
+    st = (_marshal or _marshalled()).moe_route(X, router, top_k, int(scoring == "sigmoid"), renormalize, factor, bias, ids, weights, workspace, _stream())
+    if st:
+        raise NestedFPError(st, "nestedfp_moe_route")
+    return ids, weights
+
+
+MOE_MOST_TOKENS = 64
+
+
+def moe_workspace_size(M, experts, top_k, mode=None):
+    """Bytes of workspace for moe (the same in both modes)."""
+    return int(lib().nestedfp_moe_workspace_size(int(M), experts._ref, int(top_k)))
+
+
+def moe(X, experts, ids, weights, mode, residual=None, out=None, workspace=None):
+    """residual + the weighted sum of the Experts that ids (int32 [M,top_k]) names for each row of X (float16 [M, hidden], at most 64 rows), with weights
+    (float32 [M,top_k]).  Ids outside the experts add nothing.  out may be residual or X."""
+    if out is None:
+        out = torch.empty(X.shape, dtype=torch.float16, device=X.device)
+    if workspace is None:
+        workspace = _workspace(moe_workspace_size(X.shape[0], experts, ids.shape[1]), X.device)
+    st = (_marshal or _marshalled()).moe(X, experts._at, mode, ids, weights, residual, out, workspace, _stream())
+    if st:
+        raise NestedFPError(st, "nestedfp_moe")
     return out
 
 

@@ -1,4 +1,4 @@
-// Marshalling of the calls that stand between a layer's linears (norm, cache write, attention): torch tensors to the arguments of
+// Marshalling of the calls that stand between a layer's linears (norm, cache write, attention), of linears with an epilogue and of mixtures of experts: torch tensors to the arguments of
 // the C ABI, with the checks of the Python binding.  No arithmetic.  In Python these checks cost more than a small kernel takes: 5
 // to 6 us of host time per call of 15 to 21 arguments, of them 1.2 in ctypes; here about 0.5.
 #include <Python.h>
@@ -13,6 +13,10 @@ namespace {
 decltype(&nestedfp_add_rms_norm) add_rms_norm_fn;
 decltype(&nestedfp_rope_append) rope_append_fn;
 decltype(&nestedfp_paged_attention) paged_attention_fn;
+decltype(&nestedfp_linear_fused) linear_fused_fn;
+decltype(&nestedfp_linear_fused_prequantized) linear_fused_prequantized_fn;
+decltype(&nestedfp_moe_route) moe_route_fn;
+decltype(&nestedfp_moe) moe_fn;
 
 // A wrong argument: its Python error is set.
 struct Refused {};
@@ -158,12 +162,82 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// addresses of the three entry points in the library that the binding has loaded
+// X or codes, scales, description of the layer, mode, act_scale, bias, activation, gated, residual, out, workspace, stream
+PyObject *linear_fused(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return call(n, 12, [&] {
+        const auto *layer = static_cast<const nestedfp_layer *>(address(a[2]));
+        nestedfp_epilogue e = nestedfp_epilogue();
+        e.activation = (int32_t)whole(a[6]);
+        e.gated = PyObject_IsTrue(a[7]) == 1;
+        const bool codes = a[1] != Py_None;
+        const char *what = codes ? "contiguous uint8 [M,K] codes, K as the layer's" : "float16 [M,K] with unit inner stride, K as the layer's";
+        const Rows x = rows_of(a[0], "X", codes ? at::kByte : at::kHalf, what);
+        if (x.cols != layer->K || (codes && x.ld != x.cols)) refuse("X", what);
+        if (e.gated && layer->N % 2 != 0) refuse("a gated layer's rows", "gate and up rows in turn");
+        Rows shape;
+        shape.rows = x.rows;
+        shape.cols = e.gated ? layer->N / 2 : layer->N;
+        const Rows residual = like(a[8], "residual", shape), out = like(a[9], "out", shape);
+        if (out.at == nullptr && shape.rows * shape.cols > 0) refuse("out", "float16 [M, outputs]");
+        e.bias = a[5] == Py_None ? nullptr : (const uint16_t *)dense(a[5], "bias", at::kHalf, layer->N, "a contiguous float16 [N] tensor");
+        e.residual = (const uint16_t *)residual.at;
+        e.ldr = residual.ld;
+        const at::Tensor &workspace = tensor(a[10], "workspace");
+        if (codes)
+            return linear_fused_prequantized_fn((const uint8_t *)x.at, (const float *)dense(a[1], "scales", at::kFloat, x.rows, "a contiguous float32 [M] tensor"),
+                                                x.rows, layer, &e, (uint16_t *)out.at, out.ld, workspace.data_ptr(), workspace.nbytes(), address(a[11]));
+        const float *scale = a[4] == Py_None ? nullptr : (const float *)dense(a[4], "act_scale", at::kFloat, 1, "a float32 tensor of one value");
+        return linear_fused_fn((const uint16_t *)x.at, x.rows, x.ld, layer, (int)whole(a[3]), scale, &e, (uint16_t *)out.at, out.ld,
+                               workspace.data_ptr(), workspace.nbytes(), address(a[11]));
+    });
+}
+
+// X, router, top_k, scoring, renormalize, factor, bias, ids, weights, workspace, stream
+PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return call(n, 11, [&] {
+        const Rows x = rows_of(a[0], "X", at::kHalf, "float16 [M,K] with unit inner stride");
+        const Rows r = rows_of(a[1], "router", at::kHalf, "float16 [experts,K] with unit inner stride");
+        if (r.cols != x.cols) refuse("router", "float16 [experts,K], K as that of X");
+        const int64_t top_k = whole(a[2]);
+        const char *what = "a contiguous [M,top_k] tensor, ids int32 and weights float32";
+        const Rows shape = rows_of(a[7], "ids", at::kInt, what), shape_w = rows_of(a[8], "weights", at::kFloat, what);
+        if (shape.rows != x.rows || shape.cols != top_k || shape_w.rows != x.rows || shape_w.cols != top_k) refuse("ids and weights", what);
+        void *ids = dense(a[7], "ids", at::kInt, x.rows * top_k, what), *weights = dense(a[8], "weights", at::kFloat, x.rows * top_k, what);
+        const void *bias = a[6] == Py_None ? nullptr : dense(a[6], "bias", at::kFloat, r.rows, "a contiguous float32 [experts] tensor");
+        const at::Tensor &workspace = tensor(a[9], "workspace");
+        return moe_route_fn((const uint16_t *)x.at, x.rows, x.cols, x.ld, (const uint16_t *)r.at, r.rows, r.ld, top_k, (int)whole(a[3]),
+                            PyObject_IsTrue(a[4]) == 1, real(a[5]), (const float *)bias, (int32_t *)ids, (float *)weights, workspace.data_ptr(),
+                            workspace.nbytes(), address(a[10]));
+    });
+}
+
+// X, description of the experts, mode, ids, weights, residual, out, workspace, stream
+PyObject *moe(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return call(n, 9, [&] {
+        const auto *experts = static_cast<const nestedfp_experts *>(address(a[1]));
+        const Rows x = rows_of(a[0], "X", at::kHalf, "float16 [M, hidden] with unit inner stride");
+        if (x.cols != experts->hidden) refuse("X", "float16 [M, hidden] of the experts");
+        const char *what = "contiguous [M,top_k] tensors, ids int32 and weights float32";
+        const Rows ids = rows_of(a[3], "ids", at::kInt, what), weights = rows_of(a[4], "weights", at::kFloat, what);
+        if (ids.rows != x.rows || weights.rows != x.rows || ids.cols != weights.cols || ids.ld != ids.cols || weights.ld != weights.cols)
+            refuse("ids and weights", what);
+        const Rows residual = like(a[5], "residual", x), out = like(a[6], "out", x);
+        const at::Tensor &workspace = tensor(a[7], "workspace");
+        return moe_fn((const uint16_t *)x.at, x.rows, x.ld, experts, (int)whole(a[2]), (const int32_t *)ids.at, (const float *)weights.at, ids.cols,
+                      (const uint16_t *)residual.at, residual.ld, (uint16_t *)out.at, out.ld, workspace.data_ptr(), workspace.nbytes(), address(a[8]));
+    });
+}
+
+// addresses of the entry points in the library that the binding has loaded
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return call(n, 3, [&] {
+    return call(n, 7, [&] {
         add_rms_norm_fn = reinterpret_cast<decltype(add_rms_norm_fn)>(address(a[0]));
         rope_append_fn = reinterpret_cast<decltype(rope_append_fn)>(address(a[1]));
         paged_attention_fn = reinterpret_cast<decltype(paged_attention_fn)>(address(a[2]));
+        linear_fused_fn = reinterpret_cast<decltype(linear_fused_fn)>(address(a[3]));
+        linear_fused_prequantized_fn = reinterpret_cast<decltype(linear_fused_prequantized_fn)>(address(a[4]));
+        moe_route_fn = reinterpret_cast<decltype(moe_route_fn)>(address(a[5]));
+        moe_fn = reinterpret_cast<decltype(moe_fn)>(address(a[6]));
         return 0;
     });
 }
@@ -173,6 +247,9 @@ PyMethodDef methods[] = {{"bind", fast(bind), METH_FASTCALL, nullptr},
                          {"add_rms_norm", fast(add_rms_norm), METH_FASTCALL, nullptr},
                          {"rope_append", fast(rope_append), METH_FASTCALL, nullptr},
                          {"paged_attention", fast(paged_attention), METH_FASTCALL, nullptr},
+                         {"linear_fused", fast(linear_fused), METH_FASTCALL, nullptr},
+                         {"moe_route", fast(moe_route), METH_FASTCALL, nullptr},
+                         {"moe", fast(moe), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -119,6 +119,8 @@ static int check_out(const uint16_t *Y, int64_t N, int64_t ldy) {
     return kOk;
 }
 
+static int64_t outputs_of(const Epilogue &epi, int64_t N) { return epi.kind == kEpiGated ? N / 2 : N; }
+
 static bool valid_mode(int mode) { return mode == NESTEDFP_MODE_FP16 || mode == NESTEDFP_MODE_FP8; }
 static bool valid_layout(int layout) { return layout == NESTEDFP_LAYOUT_ROWMAJOR || layout == NESTEDFP_LAYOUT_PACKED; }
 
@@ -126,22 +128,23 @@ static bool valid_layout(int layout) { return layout == NESTEDFP_LAYOUT_ROWMAJOR
 // itself (decode batches whose K fits one workgroup pass); returns -1 if it does not.
 static int fp8_gemm_fused(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const float *act_scale,
                           const uint8_t *Wq, int64_t N, int w_kind, float w_scale, uint16_t *Y, int64_t ldy,
-                          hipStream_t stream) {
+                          hipStream_t stream, const Epilogue &epi = Epilogue()) {
     if (!route_small(w_kind, M, N, K, K) || !small_gemm_fuses_quant(M, N, K)) return -1;
     GemmArgs a;
     memset(&a, 0, sizeof(a));
     a.X = X;  a.ldx = ldx;  a.static_scale = act_scale;  a.w_scale = w_scale;
     a.W0 = Wq;  a.W1 = nullptr;  a.ldw = K;
-    a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;
+    a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;  a.epi = epi;
     return launch_small_gemm(w_kind == kE4M3 ? kE4M3Quant : kE4M3QuantRow, a, stream);
 }
 
 static int fp8_gemm(const uint8_t *Xq, int64_t ldx, const float *scales, int64_t M, int64_t K, const uint8_t *Wq,
                     int64_t N, int w_kind, float w_scale, uint16_t *Y, int64_t ldy, const Workspace &ws,
-                    hipStream_t stream, bool bounded = false) {
+                    hipStream_t stream, bool bounded = false, const Epilogue &epi = Epilogue()) {
     GemmArgs a;
     memset(&a, 0, sizeof(a));
     a.bounded = bounded;
+    a.epi = epi;
     a.X = Xq;  a.ldx = ldx;  a.scales = scales;  a.w_scale = w_scale;
     a.W0 = Wq;  a.W1 = nullptr;  a.ldw = K;
     a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;
@@ -319,7 +322,8 @@ static size_t gemm_workspace_size(int64_t M, int64_t N, int64_t K, int mode) {
 
 static int gemm_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const uint8_t *upper,
                      const uint8_t *lower, int64_t N, int layout, int mode, const float *act_scale, uint16_t *Y,
-                     int64_t ldy, void *workspace, size_t workspace_bytes, void *stream, bool bounded = false) {
+                     int64_t ldy, void *workspace, size_t workspace_bytes, void *stream, bool bounded = false,
+                     const Epilogue &epi = Epilogue()) {
     if (!valid_mode(mode) || !valid_layout(layout)) return NESTEDFP_ERR_ARG;
     int st = check_dims(M, N, K);
     if (st != kOk) return st;
@@ -328,7 +332,7 @@ static int gemm_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const
     if (mode == NESTEDFP_MODE_FP16 && lower == nullptr) return NESTEDFP_ERR_ARG;
     st = check_mat(X, M, K, ldx, 8);
     if (st != kOk) return st;
-    st = check_out(Y, N, ldy);
+    st = check_out(Y, outputs_of(epi, N), ldy);
     if (st != kOk) return st;
     if (!aligned(upper, 16) || (mode == NESTEDFP_MODE_FP16 && !aligned(lower, 16))) return NESTEDFP_ERR_SHAPE;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -340,6 +344,7 @@ static int gemm_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const
         GemmArgs a;
         memset(&a, 0, sizeof(a));
         a.bounded = bounded;
+        a.epi = epi;
         a.X = X;  a.ldx = ldx;  a.W0 = upper;  a.W1 = lower;  a.ldw = K;
         a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;
         a.partials = ws.partials;  a.partial_bytes = ws.partial_bytes;  a.counters = ws.counters;
@@ -348,16 +353,16 @@ static int gemm_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const
     const int kind = packed ? kE4M3 : kE4M3Row;
     if (!carve(workspace, workspace_bytes, kind, M, N, K, true, ws, bounded)) return NESTEDFP_ERR_WORKSPACE;
     // Sec. 4.1: the upper plane read as E4M3 is the weight times 2^8
-    st = fp8_gemm_fused(X, M, K, ldx, act_scale, upper, N, kind, 0.00390625f, Y, ldy, s);
+    st = fp8_gemm_fused(X, M, K, ldx, act_scale, upper, N, kind, 0.00390625f, Y, ldy, s, epi);
     if (st >= 0) return st;
     st = launch_quantize_act(X, M, K, ldx, act_scale, ws.xq, ws.xq_ld, ws.scales, s);
     if (st != kOk) return st;
-    return fp8_gemm(ws.xq, ws.xq_ld, ws.scales, M, K, upper, N, kind, 0.00390625f, Y, ldy, ws, s, bounded);
+    return fp8_gemm(ws.xq, ws.xq_ld, ws.scales, M, K, upper, N, kind, 0.00390625f, Y, ldy, ws, s, bounded, epi);
 }
 
 static int plain_fp16_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, const void *W, int64_t N,
                            int64_t ldw, bool packed, uint16_t *Y, int64_t ldy, void *workspace,
-                           size_t workspace_bytes, void *stream) {
+                           size_t workspace_bytes, void *stream, const Epilogue &epi = Epilogue()) {
     int st = check_dims(M, N, K);
     if (st != kOk) return st;
     if (M == 0 || N == 0) return NESTEDFP_OK;
@@ -365,7 +370,7 @@ static int plain_fp16_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx,
     if (st != kOk) return st;
     st = packed ? (W == nullptr ? kErrArg : (aligned(W, 16) ? kOk : kErrShape)) : check_mat(W, N, K, ldw, 8);
     if (st != kOk) return st;
-    st = check_out(Y, N, ldy);
+    st = check_out(Y, outputs_of(epi, N), ldy);
     if (st != kOk) return st;
     const int kind = packed ? kPlainF16Packed : kPlainF16;
     Workspace ws;
@@ -373,7 +378,7 @@ static int plain_fp16_impl(const uint16_t *X, int64_t M, int64_t K, int64_t ldx,
     GemmArgs a;
     memset(&a, 0, sizeof(a));
     a.X = X;  a.ldx = ldx;  a.W0 = W;  a.W1 = nullptr;  a.ldw = packed ? K : ldw;
-    a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;
+    a.M = M;  a.N = N;  a.K = K;  a.Y = Y;  a.ldy = ldy;  a.epi = epi;
     a.partials = ws.partials;  a.partial_bytes = ws.partial_bytes;  a.counters = ws.counters;
     return run_gemm(kind, a, static_cast<hipStream_t>(stream));
 }
@@ -665,6 +670,62 @@ int nestedfp_linear(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_la
         return nestedfp_plain_gemm_fp16(X, M, L.K, ldx, L.W, L.N, L.ldw, Y, ldy, workspace, workspace_bytes, stream);
     return gemm_impl(X, M, L.K, ldx, L.upper, L.lower, L.N, L.layout, mode, act_scale, Y, ldy, workspace,
                      workspace_bytes, stream);
+}
+
+// What the caller's description of an epilogue asks of the kernels, for a linear of N rows on M tokens.
+static int epilogue_of(const nestedfp_epilogue *e, int64_t M, int64_t N, Epilogue &epi) {
+    if (e == nullptr || e->activation < 0 || e->activation >= kNumActivations || (e->gated != 0 && e->gated != 1)) return kErrArg;
+    if (e->gated && (N & 1) != 0) return kErrShape;
+    epi.kind = e->gated ? kEpiGated : kEpiFull;
+    const int64_t outputs = outputs_of(epi, N);
+    if (!aligned(e->bias, 2) || !aligned(e->residual, 2)) return kErrShape;
+    if (M > 0 && e->residual != nullptr && (e->ldr < outputs || e->ldr > ((int64_t)1 << 31))) return kErrShape;
+    epi.act = e->activation;
+    epi.bias = e->bias;
+    epi.residual = e->residual;
+    epi.ldr = e->ldr;
+    const int64_t piece = e->gated ? 2 : 4;            // residuals that a lane loads at a time
+    epi.vec = (N & 3) == 0 && aligned(e->bias, 8) &&
+              (e->residual == nullptr || (e->ldr % piece == 0 && aligned(e->residual, 2 * piece))) ? 1 : 0;
+    return kOk;
+}
+static_assert((int)NESTEDFP_ACT_GELU == (int)kActGelu && (int)NESTEDFP_ACT_SILU == (int)kActSilu && (int)NESTEDFP_ACT_RELU == (int)kActRelu, "one numbering");
+
+int nestedfp_linear_fused(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_layer *layer_host, int mode,
+                          const float *act_scale, const nestedfp_epilogue *epilogue_host, uint16_t *Y, int64_t ldy,
+                          void *workspace, size_t workspace_bytes, void *stream) {
+    if (layer_host == nullptr || !valid_mode(mode)) return NESTEDFP_ERR_ARG;
+    const nestedfp_layer &L = *layer_host;
+    Epilogue epi = Epilogue();
+    const int st = epilogue_of(epilogue_host, M, L.N, epi);
+    if (st != kOk) return st;
+    if (L.is_exception)
+        return plain_fp16_impl(X, M, L.K, ldx, L.W, L.N, L.ldw, false, Y, ldy, workspace, workspace_bytes, stream, epi);
+    return gemm_impl(X, M, L.K, ldx, L.upper, L.lower, L.N, L.layout, mode, act_scale, Y, ldy, workspace,
+                     workspace_bytes, stream, false, epi);
+}
+
+int nestedfp_linear_fused_prequantized(const uint8_t *Xq, const float *scales, int64_t M, const nestedfp_layer *layer_host,
+                                       const nestedfp_epilogue *epilogue_host, uint16_t *Y, int64_t ldy,
+                                       void *workspace, size_t workspace_bytes, void *stream) {
+    if (layer_host == nullptr) return NESTEDFP_ERR_ARG;
+    const nestedfp_layer &L = *layer_host;
+    if (L.is_exception) return NESTEDFP_ERR_RANGE;     // its FP16 weights have no E4M3 operand
+    if (!valid_layout(L.layout)) return NESTEDFP_ERR_ARG;
+    Epilogue epi = Epilogue();
+    int st = epilogue_of(epilogue_host, M, L.N, epi);
+    if (st != kOk) return st;
+    st = check_dims(M, L.N, L.K);
+    if (st != kOk) return st;
+    if (M == 0 || L.N == 0) return NESTEDFP_OK;
+    if (Xq == nullptr || scales == nullptr || L.upper == nullptr) return NESTEDFP_ERR_ARG;
+    st = check_out(Y, outputs_of(epi, L.N), ldy);
+    if (st != kOk) return st;
+    if (!aligned(Xq, 16) || !aligned(L.upper, 16) || !aligned(scales, 4)) return NESTEDFP_ERR_SHAPE;
+    const int kind = L.layout == NESTEDFP_LAYOUT_PACKED ? kE4M3 : kE4M3Row;
+    Workspace ws;
+    if (!carve(workspace, workspace_bytes, kind, M, L.N, L.K, false, ws)) return NESTEDFP_ERR_WORKSPACE;
+    return fp8_gemm(Xq, L.K, scales, M, L.K, L.upper, L.N, kind, 0.00390625f, Y, ldy, ws, static_cast<hipStream_t>(stream), false, epi);
 }
 
 int nestedfp_select_mode(int64_t tokens, int64_t threshold) {

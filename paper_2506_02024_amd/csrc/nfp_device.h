@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "nfp_host.h"
+
 namespace nfp {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -220,6 +222,65 @@ __device__ __forceinline__ uint32_t float2_to_half2_bits(float a, float b) {
     cvt.f[0] = (_Float16)a;
     cvt.f[1] = (_Float16)b;
     return cvt.u;
+}
+
+// ---- Epilogue of a linear (see Epilogue) -------------------------------------------------
+// SiLU is z sigma(z) and the GELU with a tangent z sigma(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi), since 1 + tanh u = 2 sigma(2 u):
+// both are z / (1 + 2^u) with u = z (k1 + k3 z^2).  2^u overflows to infinity for large negative z, whose reciprocal is the
+// zero that is wanted.  Exponential and reciprocal are the hardware's, 1 ulp each; the rounding of u adds up to |u| 2^-24
+// to the relative error of 2^u, of which 2^-17 is left where the result is still a normal FP16 number (|u| < 2^7).
+__device__ __forceinline__ float activate(float z, int act) {
+    if (act == kActRelu) return z < 0.0f ? 0.0f : z;
+    if (act == kActNone) return z;
+    const float k1 = act == kActGelu ? -2.302208198f : -1.442695041f;      // -2 c log2(e), -log2(e)
+    const float k = act == kActGelu ? __builtin_fmaf(-0.1029432397f, z * z, k1) : k1;
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * k));
+}
+
+// up to four consecutive halves; vec: all four are there and aligned to 8 bytes
+__device__ __forceinline__ floatx4 four_halves(const uint16_t *src, bool vec, int count) {
+    if (vec) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(src);
+        return floatx4{half_bits_to_float(w.x & 0xffffu), half_bits_to_float(w.x >> 16), half_bits_to_float(w.y & 0xffffu),
+                       half_bits_to_float(w.y >> 16)};
+    }
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (q < count) v[q] = half_bits_to_float(src[q]);
+    return v;
+}
+
+// The epilogue on the sums of token m and weight rows n .. n + 3 (n a multiple of 4); `bias` are those rows' biases.  The outputs: four, or two gated
+// ones, columns n / 2 and n / 2 + 1, in the first two.
+template <int EPI>
+__device__ __forceinline__ floatx4 epilogue4(floatx4 z, const floatx4 &bias, const Epilogue &e, int m, int n, int N) {
+    z.x += bias.x;  z.y += bias.y;  z.z += bias.z;  z.w += bias.w;
+    if constexpr (EPI == kEpiGated) {
+        floatx4 y = {activate(z.x, e.act) * z.y, activate(z.z, e.act) * z.w, 0.f, 0.f};
+        if (e.residual) {
+            const uint16_t *r = e.residual + (int64_t)m * e.ldr + (n >> 1);
+            if (e.vec) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(r);
+                y.x += half_bits_to_float(w & 0xffffu);
+                y.y += half_bits_to_float(w >> 16);
+            } else {
+                y.x += half_bits_to_float(r[0]);
+                if (n + 2 < N) y.y += half_bits_to_float(r[1]);
+            }
+        }
+        return y;
+    } else {
+        floatx4 y = {activate(z.x, e.act), activate(z.y, e.act), activate(z.z, e.act), activate(z.w, e.act)};
+        if (e.residual) {
+            const floatx4 r = four_halves(e.residual + (int64_t)m * e.ldr + n, e.vec, N - n);
+            y.x += r.x;  y.y += r.y;  y.z += r.z;  y.w += r.w;
+        }
+        return y;
+    }
+}
+__device__ __forceinline__ floatx4 bias4(const Epilogue &e, int n, int N) {
+    return e.bias ? four_halves(e.bias + n, e.vec, N - n) : floatx4{0.f, 0.f, 0.f, 0.f};
 }
 
 }  // namespace nfp

@@ -44,6 +44,19 @@ inline int64_t weight_array_bytes(int kind, int64_t N, int64_t K, int64_t ldw) {
     return N * K;
 }
 
+// What a linear does to its sums before they are rounded: z = sum + bias, y = act(z) + residual, or, gated, for the pairs of
+// weight rows 2 f and 2 f + 1, y_f = act(z_2f) * z_2f+1 + residual.  All in binary32, one rounding at the end.
+enum EpilogueKind { kEpiNone = 0, kEpiFull = 1, kEpiGated = 2 };
+enum Activation { kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kNumActivations = 4 };
+struct Epilogue {
+    int32_t kind;           // EpilogueKind: which kernels are launched; the rest says nothing with kEpiNone
+    int32_t act;            // Activation
+    int32_t vec;            // 1: four values of bias and of residual (two of the residual, gated) are loaded at a time
+    const uint16_t *bias;   // [N] or NULL
+    const uint16_t *residual;       // [M, outputs] or NULL; may be Y
+    int64_t ldr;
+};
+
 struct GemmArgs {
     // activations: fp16 X (kPlainF16 / kNestedF16) or E4M3 Xq with per-row scales (kE4M3)
     const void *X;        // uint16_t* or uint8_t*
@@ -61,6 +74,7 @@ struct GemmArgs {
     float *partials;      // split-K scratch (may be NULL if split == 1)
     size_t partial_bytes;
     uint32_t *counters;   // kMaxCounters arrival counters, all zero between calls (NULL: reduce in a second launch)
+    Epilogue epi;
     bool bounded;         // K splits of more than 64 tokens that fit the fixed scratch only (see nestedfp_gemm_static)
 };
 
@@ -193,7 +207,7 @@ constexpr bool padded_split_fits(int split, int64_t M, int64_t N, int64_t K, boo
 }
 
 int launch_splitk_reduce(const float *partials, int S, int64_t M, int64_t N, const float *scales,
-                         float w_scale, uint16_t *Y, int64_t ldy, hipStream_t stream);
+                         float w_scale, uint16_t *Y, int64_t ldy, const Epilogue &epi, hipStream_t stream);
 
 bool large_gemm_supports(int kind, int64_t K, int64_t ldx, int64_t ldw);
 int launch_probe_stream_read(const void *src, size_t bytes, uint32_t *sink, hipStream_t stream);
@@ -250,6 +264,41 @@ struct AttentionLaunch { int64_t row_tiles, part_rows, chunk_blocks, chunks, til
 struct AttentionPlan { AttentionLaunch stream, tile;  int64_t few, rt, waves;  bool scan;  size_t partial_bytes; };
 AttentionPlan attention_plan(const AttentionShape &s);
 int launch_attention(const AttentionShape &s, const AttentionPlan &plan, AttentionArgs a, hipStream_t stream);
+
+// mixture of experts
+struct RouteArgs {
+    const uint16_t *X, *R;
+    int64_t ldx, ldr, M, K;
+    int32_t experts, top_k, sigmoid, renormalize;
+    int32_t slices, tile0;                             // slices of K; the first token tile of the launch
+    float factor;
+    const float *bias;                                 // [experts] or NULL
+    double *logits;                                    // [slice][token of the launch][experts]
+    uint32_t *counters;                                // one per token tile, zero between launches
+    int32_t *ids;
+    float *weights;
+};
+size_t route_logit_bytes(int64_t M, int64_t experts, int64_t K);
+int launch_route(RouteArgs a, hipStream_t stream);
+
+struct ExpertArgs {
+    const uint16_t *X;
+    int64_t ldx, M, K, ffn;                            // K: hidden
+    const uint8_t *up0, *up1, *down0, *down1;          // upper and lower planes, or FP16 weights in the first of each
+    const int32_t *ids;
+    const float *weights;
+    const uint16_t *residual;
+    int64_t ldr;
+    uint16_t *Y;
+    int64_t ldy;
+    uint16_t *H;                                       // activated products between the launches
+    int32_t experts, top_k, act;
+    int32_t vec;                                       // 1: residuals are loaded four at a time, 2: outputs are stored so
+    int32_t passes, rotate, gather;
+};
+size_t experts_product_bytes(int64_t M, int64_t top_k, int64_t ffn);
+bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);
+int launch_experts_layer(int kind, ExpertArgs a, hipStream_t stream);
 
 bool use_small_gemm(int64_t M);
 bool route_small(int kind, int64_t M, int64_t N, int64_t K, int64_t ldw);     // which of the two families a problem runs on

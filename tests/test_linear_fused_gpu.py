@@ -1,0 +1,188 @@
+"""Linears with bias, activation, gate and residual in their epilogue, against 64 bits."""
+import itertools
+
+import pytest
+import torch
+
+import feed_forward_helpers as ff
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nfp():
+    from paper_2506_02024_amd import binding
+
+    return binding
+
+
+@pytest.fixture
+def tuned(nfp):
+    """Sets knobs for a test and takes them back."""
+    used = []
+
+    def tune(**knobs):
+        for name, value in knobs.items():
+            used.append(name)
+            nfp.tune(name, value)
+
+    yield tune
+    for name in used:
+        nfp.tune(name, -1)
+
+
+def check(nfp, M, N, K, mode, act=0, gated=False, bias=True, residual=True, packed=False, exception=False, seed=0, pad=0, what=""):
+    g = ff.generator(seed)
+    w = ff.normal(g, N, K, sigma=0.03)
+    if exception:
+        w[N // 2, K // 3] = 2.5
+    x, out = ff.normal(g, M, K), N // 2 if gated else N
+    b = ff.normal(g, N, sigma=0.5) if bias else None
+    r = ff.normal(g, M, out + pad)[:, :out] if residual else None
+    layer = nfp.Layer(w, packed=packed)
+    assert layer.is_exception == exception
+    fp8 = mode == nfp.MODE_FP8 and not exception
+    y = torch.full((M, out + pad), 7.0, dtype=torch.float16, device="cuda:0")
+    nfp.linear_fused(x, layer, mode, bias=b, activation=act, gated=gated, residual=r, out=y[:, :out])
+    ref, tol = ff.linear_ref(x, w, fp8, b, act, gated, r)
+    ff.assert_within(y[:, :out], ref, tol, what or str((M, N, K, mode, act, gated)))
+    assert (y[:, out:] == 7.0).all()
+    return x, layer, b, r, y[:, :out]
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("M,N,K", [(1, 2, 16), (1, 130, 1040), (3, 64, 272), (16, 514, 2048), (17, 96, 528), (40, 258, 1024), (64, 1024, 144),
+                                   (65, 320, 512), (130, 510, 640), (300, 770, 256)])
+def test_every_activation(nfp, M, N, K, mode):
+    for act, gated in itertools.product(range(4), (False, True)):
+        check(nfp, M, N, K, mode, act, gated, seed=act, what="act %d gated %d" % (act, gated))
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("packed,exception", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("M", [1, 33, 200])
+def test_storages_and_missing_parts(nfp, M, packed, exception, mode):
+    for bias, residual, gated in itertools.product((False, True), (False, True), (False, True)):
+        check(nfp, M, 260, 320, mode, 2, gated, bias, residual, packed, exception, seed=3)
+
+
+@pytest.mark.parametrize("M", [1, 20, 100, 300])
+@pytest.mark.parametrize("N,gated,pad", [(7, False, 0), (129, False, 3), (1031, False, 1), (262, True, 0), (262, True, 5), (1026, True, 1), (516, False, 12)])
+def test_rows_that_start_anywhere(nfp, M, N, gated, pad):
+    for mode in (0, 1):
+        check(nfp, M, N, 256, mode, 3, gated, seed=N, pad=pad)
+
+
+# every tile shape and height, split and not; the streaming kernel's splits with and without a launch of their own
+TILES = [dict(large_bm=64, large_bn=128), dict(large_bm=128, large_bn=128), dict(large_bm=128, large_bn=128, large_deep=1),
+         dict(large_bm=128, large_bn=256), dict(large_bm=128, large_bn=256, large_deep=1), dict(large_bm=256, large_bn=128),
+         dict(large_bm=256, large_bn=256)] + [dict(large_bm=256, large_bn=n, large_height=h) for n in (128, 256) for h in (160, 192, 224)]
+
+
+@pytest.mark.parametrize("knobs", TILES, ids=lambda k: "-".join("%s%d" % (n[6:], v) for n, v in k.items()))
+@pytest.mark.parametrize("split", [1, 2])
+def test_tile_shapes(nfp, tuned, knobs, split):
+    tuned(small_max_m=0, large_split=split, **knobs)
+    for rows in (0, 1):
+        tuned(large_rows=rows)
+        for mode, gated, packed, exception in ((0, False, False, False), (0, True, False, False), (0, True, True, False), (1, True, False, False),
+                                               (1, False, True, False), (0, True, False, True), (0, False, False, True)):
+            check(nfp, 300, 776 if gated else 517, 1024 + 64, mode, 2, gated, packed=packed, exception=exception, seed=1,
+                  what=str((rows, mode, gated, packed, exception)))
+
+
+@pytest.mark.parametrize("fused", [0, 1])
+@pytest.mark.parametrize("M", [1, 16, 30, 64])
+def test_streaming_splits(nfp, tuned, M, fused):
+    tuned(small_max_m=64, small_split=3, fused_reduce=fused)
+    for mode, gated, N in ((0, True, 98), (0, False, 101), (1, True, 100), (1, False, 64)):
+        check(nfp, M, N, 2048, mode, 2, gated, seed=2)
+
+
+def test_nothing_but_the_linear(nfp):
+    """Without bias, activation and residual the outputs are those of linear(), bit for bit."""
+    g = ff.generator(5)
+    for M, N, K in ((1, 512, 1024), (16, 1000, 2048), (48, 640, 512), (300, 512, 768)):
+        x, layer = ff.normal(g, M, K), nfp.Layer(ff.normal(g, N, K, sigma=0.02))
+        for mode in (0, 1):
+            assert torch.equal(nfp.linear_fused(x, layer, mode), nfp.linear(x, layer, mode))
+
+
+@pytest.mark.parametrize("M", [1, 16, 50, 200])
+def test_codes(nfp, M):
+    """E4M3 activations in: the codes of quantize_act give what the float16 activations give; codes of a norm against 64 bits."""
+    g = ff.generator(M)
+    x, w = ff.normal(g, M, 528), ff.normal(g, 260, 528, sigma=0.03)
+    r = ff.normal(g, M, 130)
+    for packed in (False, True):
+        layer = nfp.Layer(w, packed=packed)
+        codes, scales = nfp.quantize_act(x)
+        y = nfp.linear_fused(codes, layer, nfp.MODE_FP8, activation=nfp.ACT_SILU, gated=True, residual=r, scales=scales)
+        ref, tol = ff.linear_ref(x, w, True, None, 2, True, r)
+        ff.assert_within(y, ref, tol)
+
+
+@pytest.mark.parametrize("M", [1, 16, 64, 200, 300])
+def test_residual_in_place(nfp, M):
+    g = ff.generator(M)
+    for mode, gated, N in ((0, False, 512), (1, True, 512), (0, True, 130), (1, False, 131)):
+        x, layer, out = ff.normal(g, M, 2048), nfp.Layer(ff.normal(g, N, 2048, sigma=0.02)), N // 2 if gated else N
+        r = ff.normal(g, M, out)
+        apart = nfp.linear_fused(x, layer, mode, activation=nfp.ACT_GELU, gated=gated, residual=r)
+        nfp.linear_fused(x, layer, mode, activation=nfp.ACT_GELU, gated=gated, residual=r, out=r)
+        assert torch.equal(r, apart)
+
+
+def test_inf_and_nan_stay_in_their_outputs(nfp):
+    g = ff.generator(9)
+    for M in (5, 100):
+        x, w, b = ff.normal(g, M, 256), ff.normal(g, 256, 256, sigma=0.03), ff.normal(g, 256)
+        r = ff.normal(g, M, 256)
+        layer = nfp.Layer(w)
+        clean = nfp.linear_fused(x, layer, 0, bias=b, activation=nfp.ACT_SILU, residual=r)
+        b2, r2 = b.clone(), r.clone()
+        b2[7], r2[1, 9], r2[2, 20] = float("nan"), float("inf"), float("nan")
+        y = nfp.linear_fused(x, layer, 0, bias=b2, activation=nfp.ACT_SILU, residual=r2)
+        assert y[:, 7].isnan().all() and y[1, 9] == float("inf") and y[2, 20].isnan()
+        ok = torch.ones_like(y, dtype=torch.bool)
+        ok[:, 7], ok[1, 9], ok[2, 20] = False, False, False
+        assert torch.equal(y[ok], clean[ok])
+        # large sums: the exponential overflows, the result does not
+        b3 = torch.full_like(b, -30000.0)
+        b3[::2] = 30000.0
+        for act in (nfp.ACT_SILU, nfp.ACT_GELU, nfp.ACT_RELU):
+            y = nfp.linear_fused(x, layer, 0, bias=b3, activation=act)
+            assert (y[:, 1::2] == 0).all() and (y[:, ::2] > 29000).all() and y.isfinite().all()
+
+
+def test_empty_and_graph(nfp):
+    g = ff.generator(11)
+    layer = nfp.Layer(ff.normal(g, 256, 512, sigma=0.02))
+    assert nfp.linear_fused(ff.normal(g, 0, 512), layer, 0, activation=nfp.ACT_SILU, gated=True).shape == (0, 128)
+    x, r = ff.normal(g, 16, 512), ff.normal(g, 16, 128)
+    ws, out = nfp.new_workspace(nfp.linear_fused_workspace_size(16, layer, nfp.MODE_FP8), "cuda:0"), torch.empty_like(r)
+    call = lambda: nfp.linear_fused(x, layer, nfp.MODE_FP8, activation=nfp.ACT_SILU, gated=True, residual=r, out=out, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(4):
+        x.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone()
+        call()
+        assert torch.equal(out, replayed)
+
+
+def test_another_stream(nfp):
+    g = ff.generator(12)
+    layer, x = nfp.Layer(ff.normal(g, 512, 1024, sigma=0.02)), ff.normal(g, 40, 1024)
+    y = nfp.linear_fused(x, layer, 0, activation=nfp.ACT_SILU, gated=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        z = nfp.linear_fused(x, layer, 0, activation=nfp.ACT_SILU, gated=True)
+    s.synchronize()
+    assert torch.equal(y, z)

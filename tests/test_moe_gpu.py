@@ -1,0 +1,173 @@
+"""The experts of a few tokens against 64 bits."""
+import pytest
+import torch
+
+import feed_forward_helpers as ff
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nfp():
+    from paper_2506_02024_amd import binding
+
+    return binding
+
+
+def make(M, E, H, F, top_k, seed=0, exception=False):
+    g = ff.generator(seed)
+    gate_up, down = ff.normal(g, E, 2 * F, H, sigma=0.05), ff.normal(g, E, H, F, sigma=0.05)
+    if exception:
+        down[E // 2, 3, 5] = 3.0
+    x, r = ff.normal(g, M, H), ff.normal(g, M, H)
+    ids = torch.rand((M, E), generator=g, device="cuda:0").topk(top_k, 1).indices.to(torch.int32)
+    weights = torch.rand((M, top_k), generator=g, device="cuda:0")
+    return x, gate_up, down, ids.contiguous(), weights, r
+
+
+@pytest.mark.parametrize("mode,exception", [(0, False), (1, False), (0, True), (1, True)])
+@pytest.mark.parametrize("M,E,H,F,top_k", [(1, 1, 16, 16, 1), (1, 8, 1040, 528, 2), (1, 40, 256, 48, 8), (3, 4, 128, 272, 2), (16, 10, 512, 128, 3), (17, 4, 144, 64, 2),
+                                           (30, 3, 272, 80, 2), (48, 24, 256, 96, 6), (64, 2, 256, 128, 2), (64, 60, 96, 32, 4), (33, 1, 64, 160, 1)])
+def test_shapes(nfp, M, E, H, F, top_k, mode, exception):
+    x, gate_up, down, ids, weights, r = make(M, E, H, F, top_k, seed=M + E, exception=exception)
+    experts = nfp.Experts(gate_up, down)
+    assert experts.is_exception == exception
+    for residual in (None, r):
+        y = nfp.moe(x, experts, ids, weights, mode, residual=residual)
+        ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, mode == 1 and not exception, 2, residual)
+        ff.assert_within(y, ref, tol, str(residual is not None))
+
+
+@pytest.mark.parametrize("M,H", [(5, 4096), (2, 4112), (1, 5120), (20, 2064), (40, 2304), (64, 1600)])
+def test_long_rows(nfp, M, H):
+    """Rows in one pass and in several, that start on lines and inside them, for every number of token tiles."""
+    E = 2 if M != 40 else 12
+    for mode, exception in ((0, False), (1, False), (0, True)):
+        x, gate_up, down, ids, weights, r = make(M, E, H, 64, 2, seed=H, exception=exception)
+        y = nfp.moe(x, nfp.Experts(gate_up, down), ids, weights, mode, residual=r)
+        ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, mode == 1, 2, r)
+        ff.assert_within(y, ref, tol, str((mode, exception)))
+
+
+@pytest.mark.parametrize("act", range(4))
+def test_activations(nfp, act):
+    x, gate_up, down, ids, weights, _ = make(6, 5, 96, 80, 2, seed=act)
+    y = nfp.moe(x, nfp.Experts(gate_up, down, act), ids, weights, 0)
+    ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, False, act)
+    ff.assert_within(y, ref, tol)
+
+
+@pytest.mark.parametrize("M", [1, 7, 40, 64])
+def test_ids_from_anywhere(nfp, M):
+    """Ids outside the experts add nothing, one named twice counts with both weights, a token may have none at all, all tokens may choose one
+    expert, and what lies in the workspace does not matter."""
+    x, gate_up, down, ids, weights, r = make(M, 12, 128, 96, 4, seed=M)
+    experts = nfp.Experts(gate_up, down)
+    cases = {}
+    cases["outside"] = ids.clone()
+    cases["outside"][:, 1] = -1
+    cases["outside"][::2, 2] = 12
+    cases["outside"][0, 3] = 2 ** 31 - 1
+    cases["twice"] = ids.clone()
+    cases["twice"][:, 2] = cases["twice"][:, 0]
+    cases["twice"][0, :] = 5
+    cases["none"] = torch.full_like(ids, -7)
+    cases["some have none"] = ids.clone()
+    cases["some have none"][M // 2:] = -1
+    cases["one expert"] = torch.full_like(ids, -1)
+    cases["one expert"][:, 1] = 11
+    cases["crowded"] = torch.randint(0, 2, ids.shape, generator=ff.generator(1), device="cuda:0", dtype=torch.int32)
+    ws = nfp.new_workspace(nfp.moe_workspace_size(M, experts, 4), "cuda:0")
+    for what, chosen in cases.items():
+        for residual in (None, r):
+            ws[nfp.WORKSPACE_COUNTER_BYTES:] = 0xff    # (NaN as float16)
+            y = nfp.moe(x, experts, chosen, weights, 0, residual=residual, workspace=ws)
+            ref, tol = ff.moe_ref(x, gate_up, down, chosen, weights, False, 2, residual)
+            ff.assert_within(y, ref, tol, what)
+    y = nfp.moe(x, experts, cases["none"], weights, 0, residual=r)
+    assert torch.equal(y, r)
+
+
+def test_nan_stays_with_its_token(nfp):
+    for M in (5, 40):
+        x, gate_up, down, ids, weights, r = make(M, 6, 128, 64, 2, seed=M)
+        experts = nfp.Experts(gate_up, down)
+        clean = nfp.moe(x, experts, ids, weights, 0, residual=r)
+        x2, w2 = x.clone(), weights.clone()
+        x2[1, 3], w2[2, 0], x2[4] = float("nan"), float("inf"), 60000.0
+        y = nfp.moe(x2, experts, ids, w2, 0, residual=r)
+        keep = torch.ones(M, dtype=torch.bool, device="cuda:0")
+        keep[[1, 2, 4]] = False
+        assert torch.equal(y[keep], clean[keep]) and y[1].isnan().all()
+
+
+def test_strides_and_places(nfp):
+    """Padded rows, outputs that start anywhere, results over the residual and over the activations."""
+    for M in (4, 50):
+        x, gate_up, down, ids, weights, r = make(M, 7, 256, 64, 3, seed=M)
+        experts = nfp.Experts(gate_up, down)
+        apart = nfp.moe(x, experts, ids, weights, 0, residual=r)
+        wide = torch.zeros((M, 256 + 24), dtype=torch.float16, device="cuda:0")
+        wide[:, :256] = x
+        out, rr = torch.full((M, 261), 3.0, dtype=torch.float16, device="cuda:0"), torch.zeros((M, 259), dtype=torch.float16, device="cuda:0")
+        rr[:, 2:258] = r
+        nfp.moe(wide[:, :256], experts, ids, weights, 0, residual=rr[:, 2:258], out=out[:, 1:257])
+        assert torch.equal(out[:, 1:257], apart) and (out[:, 0] == 3).all() and (out[:, 257:] == 3).all()
+        r2, x2 = r.clone(), x.clone()
+        assert torch.equal(nfp.moe(x, experts, ids, weights, 0, residual=r2, out=r2), apart)
+        assert torch.equal(nfp.moe(x2, experts, ids, weights, 0, residual=r, out=x2), apart)
+
+
+def test_many_experts(nfp):
+    """As many experts as there may be, choices of 32."""
+    x, gate_up, down, ids, weights, _ = make(64, 512, 32, 16, 32, seed=1)
+    experts = nfp.Experts(gate_up, down)
+    for M in (64, 20, 1):
+        y = nfp.moe(x[:M], experts, ids[:M], weights[:M], 0)
+        ref, tol = ff.moe_ref(x[:M], gate_up, down, ids[:M], weights[:M], False, 2)
+        ff.assert_within(y, ref, tol, str(M))
+
+
+def test_graph_of_router_and_experts(nfp):
+    """Router, experts with a shared one as their residual, in a graph that is replayed with new activations; a second workspace for a second graph."""
+    g = ff.generator(6)
+    H, F, E, k, M = 256, 128, 16, 4, 12
+    x, router = ff.normal(g, M, H), ff.normal(g, E, H, sigma=0.1)
+    gate_up, down = ff.normal(g, E, 2 * F, H, sigma=0.05), ff.normal(g, E, H, F, sigma=0.05)
+    shared_up, shared_down = ff.normal(g, 2 * F, H, sigma=0.05), ff.normal(g, H, F, sigma=0.05)
+    experts, up, dn = nfp.Experts(gate_up, down), nfp.Layer(nfp.interleave_gate_up(shared_up)), nfp.Layer(shared_down)
+
+    def layer(mode, ws):
+        ids, weights = nfp.moe_route(x, router, k, workspace=ws)
+        h = nfp.linear_fused(x, up, mode, activation=nfp.ACT_SILU, gated=True, workspace=ws)
+        y = nfp.linear_fused(h, dn, mode, residual=x, workspace=ws)
+        return ids, weights, nfp.moe(x, experts, ids, weights, mode, residual=y, out=y, workspace=ws)
+
+    graphs = []
+    for mode in (0, 1):
+        need = max(nfp.moe_route_workspace_size(M, E, H), nfp.moe_workspace_size(M, experts, k), nfp.linear_fused_workspace_size(M, up, mode),
+                   nfp.linear_fused_workspace_size(M, dn, mode))
+        ws = nfp.new_workspace(need, "cuda:0")
+        layer(mode, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = layer(mode, ws)
+        graphs.append((mode, ws, graph, out))
+    for _ in range(3):
+        x.normal_(generator=g)
+        for mode, ws, graph, out in graphs:
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in out]
+            for a, b in zip(got, layer(mode, nfp.new_workspace(ws.numel(), "cuda:0"))):
+                assert torch.equal(a, b)
+            ids, weights = ff.route_ref(x, router, k, False, True, None, 1.0)
+            assert torch.equal(got[0].cpu(), ids)
+            # the shared expert in two calls, whose products are rounded between them
+            h, dh = ff.linear_ref(x, nfp.interleave_gate_up(shared_up), mode == 1, None, 2, True)
+            if mode == 0:
+                y, dy = ff.linear_ref(h.half(), shared_down, False, None, 0, False, x)
+                dy = dy + dh @ shared_down.double().abs().t().contiguous() + (h - h.half().double()).abs() @ shared_down.double().abs().t().contiguous()
+                ref, tol = ff.moe_ref(x, gate_up, down, got[0], got[1], False, 2, y.half())
+                ff.assert_within(got[2], ref, tol + dy + (y - y.half().double()).abs())
