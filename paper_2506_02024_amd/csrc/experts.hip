@@ -1,6 +1,6 @@
-// A mixture of experts on a few tokens (1 ... 64), in two launches: gate and up products with the activation, down products with the
+// A mixture of experts on a few tokens (1 ... 64), in two launches of one kernel: gate and up products with the activation, down products with the
 // weighted sum.  Bound by the bytes of the experts that the tokens have chosen; everything here is arranged around streaming
-// those once.  Which experts these are the kernels find out themselves from the tokens' choices, which lie in device memory.
+// those once.  Which experts these are the first launch finds out itself from the tokens' choices, which lie in device memory.
 //
 // As in the streaming linears, weight rows are the MFMA's first operand (row-major, fetched in pieces of 16 rows x 128 bytes and
 // regrouped through 2 KB of LDS per wave) and tokens the second; activations are FP16 in both modes.  FP8 mode expands the upper
@@ -12,7 +12,6 @@
 
 namespace nfp {
 
-constexpr int kNone = 255;                             // a token that has not chosen the expert
 // The activated products between the two launches are kept as two FP16 terms, h = high + low: rounded to one, their error is as large as the
 // output's own rounding.
 constexpr int kTerms = 2;
@@ -65,77 +64,149 @@ __device__ __forceinline__ void operand(const WItem &w, u32x4 &lo, u32x4 &hi) {
     else { lo = w.a;  hi = w.b; }
 }
 
-// Who has chosen whom, worked out by every workgroup from the ids (a few thousand at most): the experts that any token has chosen, in rising order, and
-// for each the place of every token's choice, kNone without one.  A token that names an expert twice has one place, with the sum of both
-// weights.  Ids outside the experts are nobody's.
-struct Choices {
-    uint16_t *rank;                                    // [experts] place among the chosen ones
-    uint16_t *chosen;                                  // [chosen] the experts
-    uint32_t *units;                                   // [chosen + 1] running sum of the experts' work (up kernel)
-    int16_t *ids;                                      // [tokens * top_k]
-    float *weights;                                    // the same (down kernel)
-    uint8_t *place;                                    // [chosen][tokens_padded]
-    int count, padded;
-};
 constexpr int kMostExperts = 512, kMostTokens = 64, kMostTop = 32;
-static inline size_t choices_bytes(const ExpertArgs &a) {
-    const size_t chosen = (size_t)std::min<int64_t>(a.experts, a.M * a.top_k), padded = (size_t)((a.M + 15) & ~(int64_t)15), n = (size_t)(a.M * a.top_k);
-    return ((a.experts * 2 + 15) & ~(size_t)15) + ((chosen * 2 + 15) & ~(size_t)15) + ((chosen * 4 + 4 + 15) & ~(size_t)15) + ((n * 2 + 15) & ~(size_t)15) +
-           ((n * 4 + 15) & ~(size_t)15) + chosen * padded;
-}
 
-__device__ __forceinline__ Choices choices_of(const ExpertArgs &a, uint8_t *at, bool want_weights) {
-    const int n = (int)(a.M * a.top_k), chosen = min((int)a.experts, n);
-    const int t = threadIdx.x, threads = blockDim.x, lane = t & 63;
+// ---- who has chosen whom -----------------------------------------------------------------------------
+// The experts that any token has chosen, in rising order, and for each the choices that name it, as rows of the products between the launches (token *
+// top_k + place), in the tokens' order: workgroups that share a crowded expert have to agree on who is among its first sixteen.  A token that names
+// an expert twice counts once, with the sum of both weights.  Ids outside the experts are nobody's.
+// One wave of every workgroup of the first launch works this out (a chain of LDS accesses, which a wave's LDS serves in order, without barriers), the
+// first workgroup leaves it in the workspace, and the second launch copies it from there.
+struct ChoiceHead { uint32_t count, chunks;  uint32_t pad[2]; };      // experts chosen; work of all of them in chunks of 16 MT choices
+struct Choices {
+    ChoiceHead *head;
+    u32x4 *info;                                       // [chosen + 1]: expert, first choice | number << 16, chunks before it
+    u32x2 *entry;                                      // [tokens * top_k]: row | token << 16 of the choices, expert by expert
+    float *share;                                      // [row] weight
+    uint32_t *used;                                    // a bit per row: first choice of an expert there is
+    uint8_t *scratch;                                  // first launch
+};
+static __host__ __device__ __forceinline__ int round16(int bytes) { return (bytes + 15) & ~15; }
+static __host__ __device__ __forceinline__ int choice_most(int experts, int n) { return experts < n ? experts : n; }
+// bytes that both launches share; the first one's scratch (counts and ranks of the experts, ids, unsorted choices, sizes)
+static __host__ __device__ __forceinline__ int choices_shared(int experts, int n) {
+    return 16 + 16 * (choice_most(experts, n) + 1) + round16(8 * n) + round16(4 * n) + round16((n + 31) / 32 * 4);
+}
+static __host__ __device__ __forceinline__ int choices_scratch(int experts, int n) {
+    return round16(4 * experts) + 2 * round16(2 * n) + round16(4 * choice_most(experts, n));
+}
+__device__ __forceinline__ Choices choices_at(uint8_t *at, int experts, int n) {
     Choices c;
-    c.padded = ((int)a.M + 15) & ~15;
     auto take = [&](int bytes) {
         uint8_t *p = at;
-        at += (bytes + 15) & ~15;
+        at += round16(bytes);
         return p;
     };
-    c.rank = reinterpret_cast<uint16_t *>(take((int)a.experts * 2));
-    c.chosen = reinterpret_cast<uint16_t *>(take(chosen * 2));
-    c.units = reinterpret_cast<uint32_t *>(take(chosen * 4 + 4));
-    c.ids = reinterpret_cast<int16_t *>(take(n * 2));
-    c.weights = reinterpret_cast<float *>(take(n * 4));
-    c.place = at;
-    for (int i = t; i < a.experts; i += threads) c.rank[i] = 0;
-    for (int i = t; i < chosen * c.padded / 4; i += threads) reinterpret_cast<uint32_t *>(c.place)[i] = 0xffffffffu;
-    __syncthreads();
-    for (int i = t; i < n; i += threads) {
-        const int e = a.ids[i];
-        const bool ok = e >= 0 && e < a.experts;
-        c.ids[i] = (int16_t)(ok ? e : -1);
-        if (ok) c.rank[e] = 1;
-        if (want_weights) c.weights[i] = a.weights[i];
+    c.head = reinterpret_cast<ChoiceHead *>(take(16));
+    c.info = reinterpret_cast<u32x4 *>(take(16 * (choice_most(experts, n) + 1)));
+    c.entry = reinterpret_cast<u32x2 *>(take(8 * n));
+    c.share = reinterpret_cast<float *>(take(4 * n));
+    c.used = reinterpret_cast<uint32_t *>(take((n + 31) / 32 * 4));
+    c.scratch = at;
+    return c;
+}
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, int lane, uint32_t &all) {
+    uint32_t upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t before = __shfl_up(upto, d);
+        if (lane >= d) upto += before;
     }
-    __syncthreads();
-    // (every wave counts by itself; the first one writes)
+    all = __builtin_amdgcn_readlane(upto, 63);
+    return upto - v;
+}
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+__device__ __forceinline__ void find_choices(const ExpertArgs &a, const Choices &c, int lane, int columns, bool shares) {
+    const int experts = a.experts, top_k = a.top_k, n = (int)a.M * top_k;
+    uint8_t *at = c.scratch;
+    uint32_t *const of = reinterpret_cast<uint32_t *>(at);             // choices of an expert; then its place among the chosen ones
+    at += round16(4 * experts);
+    int16_t *const ids = reinterpret_cast<int16_t *>(at);
+    at += round16(2 * n);
+    uint16_t *const unsorted = reinterpret_cast<uint16_t *>(at);
+    at += round16(2 * n);
+    uint32_t *const size = reinterpret_cast<uint32_t *>(at);
+    auto ordered = [] { asm volatile("" ::: "memory"); };            // (in program order; the LDS keeps a wave's accesses so)
+    const int first_id = lane < n ? a.ids[lane] : -1;
+    const float first_share = shares && lane < n ? a.weights[lane] : 0.0f;
+    for (int e = lane; e < experts; e += 64) of[e] = 0;
+    for (int w = lane; w < (n + 31) / 32; w += 64) c.used[w] = 0;
+    ordered();
+    for (int i = lane; i < n; i += 64) {
+        const int e = i == lane ? first_id : a.ids[i];
+        const bool ok = e >= 0 && e < experts;
+        ids[i] = (int16_t)(ok ? e : -1);
+        unsorted[i] = 0xffff;
+        if (ok) atomicAdd(&of[e], 1u);
+        if (shares) c.share[i] = i == lane ? first_share : a.weights[i];
+    }
+    ordered();
     int count = 0;
-    for (int base = 0; base < a.experts; base += 64) {
-        const bool in = base + lane < a.experts && c.rank[min(base + lane, (int)a.experts - 1)] != 0;
-        const uint64_t mask = __ballot(in);
-        if (t < 64 && in) c.chosen[count + __popcll(mask & ((1ull << lane) - 1))] = (uint16_t)(base + lane);
+    uint32_t begin = 0;
+    for (int base = 0; base < experts; base += 64) {
+        const int e = base + lane;
+        const uint32_t own = e < experts ? of[e] : 0u;
+        const uint64_t mask = __ballot(own != 0);
+        if (mask == 0) continue;
+        uint32_t all;
+        const uint32_t before = sum_before(own, lane, all);
+        if (own != 0) {
+            const int r = count + lanes_before(mask);
+            c.info[r] = u32x4{(uint32_t)e, begin + before, 0u, 0u};
+            size[r] = 0;
+            of[e] = (uint32_t)r;
+        }
+        begin += all;
         count += __popcll(mask);
     }
-    c.count = count;
-    __syncthreads();
-    for (int i = t; i < count; i += threads) c.rank[c.chosen[i]] = (uint16_t)i;
-    __syncthreads();
-    if (t < a.M) {                                     // (at most 64 tokens: lanes of the first wave)
-        const int16_t *const mine = c.ids + t * a.top_k;
-        for (int j = (int)a.top_k - 1; j >= 0; --j)
-            if (mine[j] >= 0) c.place[c.rank[mine[j]] * c.padded + t] = (uint8_t)j;
-        if (want_weights)
-            for (int j = 1; j < a.top_k; ++j)
-                if (mine[j] >= 0) {
-                    const int first = c.place[c.rank[mine[j]] * c.padded + t];
-                    if (first != j) c.weights[t * a.top_k + first] += c.weights[t * a.top_k + j];
-                }
+    ordered();
+    for (int i = lane; i < n; i += 64) {
+        const int e = ids[i], m = i / top_k, j = i - m * top_k;
+        if (e < 0) continue;
+        const int16_t *const others = ids + m * top_k;
+        bool again = false;
+        for (int q = 0; q < j; ++q) again |= others[q] == e;
+        if (again) continue;
+        if (shares) {                                  // (a choice that repeats an earlier one keeps its weight: only first ones are written)
+            float w = c.share[i];
+            for (int q = j + 1; q < top_k; ++q)
+                if (others[q] == e) w += c.share[m * top_k + q];
+            c.share[i] = w;
+        }
+        const uint32_t r = of[e];
+        unsorted[c.info[r].y + atomicAdd(&size[r], 1u)] = (uint16_t)i;
+        atomicOr(&c.used[i >> 5], 1u << (i & 31));
     }
-    __syncthreads();
-    return c;
+    ordered();
+    for (int s = lane; s < n; s += 64) {
+        const int i = unsorted[s];
+        if (i == 0xffff) continue;
+        const uint32_t r = of[ids[i]];
+        const int start = (int)c.info[r].y, of_r = (int)size[r];
+        int place = start;
+        for (int q = 0; q < of_r; ++q) place += unsorted[start + q] < i;
+        c.entry[place] = u32x2{(uint32_t)i | (uint32_t)(i / top_k) << 16, 0u};
+    }
+    ordered();
+    uint32_t chunks = 0;
+    for (int base = 0; base < count; base += 64) {
+        const int r = base + lane;
+        const uint32_t of_r = r < count ? size[r] : 0u;
+        uint32_t all;
+        const uint32_t before = sum_before((of_r + columns - 1) / (uint32_t)columns, lane, all);
+        if (r < count) {
+            const u32x4 v = c.info[r];
+            c.info[r] = u32x4{v.x, v.y | of_r << 16, chunks + before, 0u};
+        }
+        chunks += all;
+    }
+    if (lane == 0) {
+        c.info[count] = u32x4{0u, 0u, chunks, 0u};
+        *c.head = ChoiceHead{(uint32_t)count, chunks, {0u, 0u}};
+    }
 }
 
 __device__ __forceinline__ void lds_barrier() {
@@ -145,139 +216,145 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// ---- gate and up products --------------------------------------------------------------------------
-// The weight rows of an expert are gate and up rows in turn, so that a lane's four sums of a 16-row tile are two gated pairs.  A unit of work is two
-// such tiles (16 columns of ffn) for one expert and up to 16 MT of its tokens; all units stand in one row, expert by expert, and every
-// workgroup takes an equal stretch.  Its waves share K (slices of SPW steps of 64 columns, in several passes where K is longer) and keep the
-// tokens of their slice in registers; tile t + 1 is loaded while tile t is multiplied, across units and experts; sums meet in
-// LDS, one barrier per unit.
-// Up to 16 tokens stand in the columns as they are (`gather` 0), and are loaded once.  Of more tokens the columns are those that have chosen
-// the expert, loaded anew with every expert, so that 48 tokens over many experts take the time of a few.
-// (with four token tiles the sums of one unit are all that the LDS has room for: a second barrier)
+// ---- the kernel ---------------------------------------------------------------------------------------
+// Rows of weights: gate and up rows in turn (first launch, !DOWN), so that a lane's four sums of a 16-row tile are two gated pairs; rows of the output (DOWN).
+// A unit of work is two such tiles of one expert for up to 16 MT of its choices.  All units stand in one row, expert by expert, and every
+// workgroup takes an equal stretch.  Its waves share K (slices of SPW steps of 64 columns, in several passes where K is longer) and keep
+// the columns' values of their slice in registers: tokens, or the products of the first launch in two terms.  Tile t + 1 is loaded while tile t is multiplied,
+// across units and experts; sums meet in LDS, one barrier per unit.
+// Columns are the choices of the expert, loaded anew with every expert, so that 48 tokens over many experts take the time of a few; in the first launch up
+// to 16 tokens stand in the columns as they are (`gather` 0) and are loaded once.
+// The second launch leaves the product of every choice in memory, 32 bits each.  At its end a workgroup counts its units per 32 output rows, past the caches; the one
+// that has the last of them adds up the rows' choices, token by token in their order, so that the result does not depend on timing.
+// (Tried for the second launch: a workgroup for 16 output rows that walks over all experts and needs no memory in between.  Each of its waves has to fetch
+// the products of every expert anew for 16 rows of weights: 16 tokens, 64 experts of 1408, FP8 mode 80 us; 48 tokens, 96 experts of 1520, FP16 mode 478 us.)
+// (with four column tiles the sums of one unit are all that the LDS has room for: a second barrier)
 template <int MT> constexpr int kSumRegions = MT == 4 ? 1 : 2;
-template <int KIND, int MT, int SPW, bool PASSES, int POL>
-__global__ void __launch_bounds__(MT == 1 && !PASSES ? 1024 : 512)
-experts_up_kernel(ExpertArgs a) {
+template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN>
+__global__ void __launch_bounds__(MT == 1 && !PASSES && !DOWN ? 1024 : 512)
+experts_kernel(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     constexpr int KSTEP = 64, EB = kind_elem_bytes(KIND), PIECES = row_pieces<KIND == kPlainF16 ? kPlainF16 : kNestedF16Row, SPW>();
+    constexpr int TERMS = DOWN ? kTerms : 1;
+    static_assert(PIECES > 0, "whole pieces");
+    constexpr int SUMS = kSumRegions<MT> * 2 * MT * 1024;      // bytes of sums per wave
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int g = lane >> 4, r16 = lane & 15;
-    constexpr int SUMS = kSumRegions<MT> * 2 * MT * 1024;      // bytes of sums per wave
+    const int g = lane >> 4, n = (int)a.M * a.top_k;
+    const int64_t K = DOWN ? a.ffn : a.K;
+    const int tiles = (int)((DOWN ? a.K : 2 * a.ffn) >> 4), per_expert = (tiles + 1) >> 1;
     floatx4 *const slots = reinterpret_cast<floatx4 *>(shared);                // [regions][2 tiles][wave][MT][64]
     const uint32_t own = (uint32_t)(waves * SUMS + wave * 2048);
-    uint8_t *const list = shared + waves * (SUMS + 2048) + wave * 64;          // the columns' tokens
-    const Choices c = choices_of(a, shared + waves * (SUMS + 2048 + 64), false);
-    const int per_expert = (int)(a.ffn >> 4);
-    // the running sum of the units: one chunk of columns for every 16 MT tokens
-    if (threadIdx.x < 64) {
-        uint32_t sum = 0;
-        for (int base = 0; base < c.count; base += 64) {
-            const int r = base + lane;
-            uint32_t tokens = c.padded;                // (places are below 128)
-            if (a.gather && r < c.count)
-                for (int q = 0; q < c.padded / 4; ++q) tokens -= __popc(reinterpret_cast<const uint32_t *>(c.place + r * c.padded)[q] & 0x80808080u);
-            uint32_t mine = r < c.count ? (a.gather ? (tokens + 16 * MT - 1) / (16 * MT) : 1u) * (uint32_t)per_expert : 0u;
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t before = __shfl_up(mine, d);
-                if (lane >= d) mine += before;
-            }
-            if (r < c.count) c.units[r + 1] = sum + mine;
-            sum += __shfl(mine, 63);
-        }
-        if (lane == 0) c.units[0] = 0;
-    }
-    __syncthreads();
-    const uint32_t total = c.units[c.count];
-    const uint32_t first = (uint32_t)((uint64_t)total * blockIdx.x / gridDim.x), end = (uint32_t)((uint64_t)total * (blockIdx.x + 1) / gridDim.x);
-    if (first >= end) return;
-    // Where a unit lies: the expert's place among the chosen ones, the chunk of its tokens, the columns of ffn.
-    struct At { int r, chunk, f; };
-    At at = {0, 0, 0};
-    for (int base = 0; base < c.count; base += 64)
-        at.r += __popcll(__ballot(base + lane < c.count && c.units[min(base + lane, c.count - 1) + 1] <= first));
-    at.r = __builtin_amdgcn_readfirstlane(at.r);
-    {
-        const uint32_t inside = first - c.units[at.r];
-        at.chunk = __builtin_amdgcn_readfirstlane(inside / (uint32_t)per_expert);
-        at.f = __builtin_amdgcn_readfirstlane((int)(inside - (uint32_t)at.chunk * (uint32_t)per_expert));
-    }
-    auto step = [&](At &x) {
-        if (++x.f < per_expert) return;
-        x.f = 0;
-        ++x.chunk;
-        const uint32_t of = __builtin_amdgcn_readfirstlane(c.units[x.r + 1] - c.units[x.r]);
-        if ((uint32_t)x.chunk * (uint32_t)per_expert >= of) { x.chunk = 0;  ++x.r; }
-    };
+    uint16_t *const list = reinterpret_cast<uint16_t *>(shared + waves * (SUMS + 2048) + wave * 32);       // the columns' rows
+    const Choices c = choices_at(shared + waves * (SUMS + 2048 + 32), a.experts, n);
 
-    const uint32_t row_bytes = (uint32_t)a.K * EB;
-    const int64_t expert_bytes = 2 * a.ffn * (int64_t)row_bytes;
+    const uint32_t row_bytes = (uint32_t)K * EB;
+    const int64_t expert_bytes = tiles * 16 * (int64_t)row_bytes;
+    const uint8_t *const w0 = DOWN ? a.down0 : a.up0, *const w1 = DOWN ? a.down1 : a.up1;
     // (rows of a multiple of 4 KB put the 16 rows of a slice on the same memory channels: the slices are rotated from workgroup to workgroup)
     const int ks = a.rotate ? (int)((wave + (blockIdx.x >> 3) * 5u) % (unsigned)waves) : wave;
     const Regroup<true> rx(shared, own, lane);
     const Regroup<KIND == kPlainF16> rw(shared, own, lane);
-    u32x4 xa[SPW][MT], xb[SPW][MT];
-    int row[MT];                                       // the column's row of the products between the launches, or -1
-    uint32_t x_a[MT], x_b[MT];                         // where the activations lie that the lane loads: rows 0 .. 7, 8 .. 15 of the columns
-    const __amdgpu_buffer_rsrc_t rsx = weight_rsrc(reinterpret_cast<const uint8_t *>(a.X), (uint32_t)(((a.M - 1) * a.ldx + a.K) * 2));
-    auto x_at = [&](int token, int l) { return token >= 0 ? (uint32_t)token * (uint32_t)(2 * a.ldx) + (l & 7) * 16u : kDead; };
-    int k_slice = 0;
+    u32x4 xa[SPW][MT][TERMS], xb[SPW][MT][TERMS];
+    int row[MT];                                       // the column's choice, or -1
+    uint32_t x_a[MT], x_b[MT];                         // where the values lie that the lane loads: columns 0 .. 7, 8 .. 15
+    const uint32_t x_row = DOWN ? (uint32_t)(kTerms * 2 * a.ffn) : (uint32_t)(2 * a.ldx);
+    const __amdgpu_buffer_rsrc_t rsx = DOWN ? weight_rsrc(reinterpret_cast<const uint8_t *>(a.H), (uint32_t)n * x_row)
+                                            : weight_rsrc(reinterpret_cast<const uint8_t *>(a.X), (uint32_t)(((a.M - 1) * a.ldx + a.K) * 2));
+    auto x_at = [&](int which, int l) { return which >= 0 ? (uint32_t)which * x_row + (l & 7) * 16u : kDead; };
     auto k_of = [&](int pass) { return (pass * waves + ks) * (SPW * KSTEP); };
-
-    auto columns = [&](const At &x) {
-        const uint8_t *const place = c.place + x.r * c.padded;
-        int l = lane;                                  // (what follows from the lane is worked out anew: kept across the loop it costs registers that are spilled)
-        asm volatile("" : "+v"(l));
-        const int col = l & 15;
-        if (!a.gather) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int m = 16 * i + col, p = m < a.M ? place[m] : kNone;
-                row[i] = p == kNone ? -1 : m * (int)a.top_k + p;
-            }
-            return;
-        }
-        const bool in = l < a.M && place[min(l, (int)a.M - 1)] != kNone;
-        const uint64_t mask = __ballot(in);
-        const int n = __popcll(mask);
-        if (in) list[__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = (uint8_t)l;
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int at0 = 16 * (x.chunk * MT + i);
-            auto token = [&](int q) { return q < n ? (int)list[min(q, 63)] : -1; };
-            const int m = token(at0 + col);
-            row[i] = m < 0 ? -1 : m * (int)a.top_k + place[m];
-            x_a[i] = x_at(token(at0 + (l >> 3)), l);
-            x_b[i] = x_at(token(at0 + 8 + (l >> 3)), l);
-        }
-        asm volatile("" ::: "memory");
-    };
-    auto load_tokens = [&](int pass) {
+    auto request = [&](int pass) {
         const int k0 = k_of(pass);
 #pragma unroll
         for (int s = 0; s < SPW; ++s)
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const bool in = k0 + s * KSTEP + (lane & 7) * 8 < a.K;
-                xa[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rsx, (in ? x_a[i] + 2u * k0 : kDead) + 2 * KSTEP * s, 0, 0);
-                xb[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rsx, (in ? x_b[i] + 2u * k0 : kDead) + 2 * KSTEP * s, 0, 0);
+                const bool in = k0 + s * KSTEP + (lane & 7) * 8 < K;
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) {
+                    xa[s][i][t] = __builtin_amdgcn_raw_buffer_load_b128(rsx, (in ? x_a[i] + 2u * k0 + (uint32_t)(t * 2 * K) : kDead) + 2 * KSTEP * s, 0, 0);
+                    xb[s][i][t] = __builtin_amdgcn_raw_buffer_load_b128(rsx, (in ? x_b[i] + 2u * k0 + (uint32_t)(t * 2 * K) : kDead) + 2 * KSTEP * s, 0, 0);
+                }
             }
+    };
+    auto regroup = [&] {
 #pragma unroll
         for (int s = 0; s < SPW; ++s)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) rx.run(xa[s][i], xb[s][i]);
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) rx.run(xa[s][i][t], xb[s][i][t]);
+    };
+
+    const bool in_place = !DOWN && !a.gather;          // the tokens in their places (MT is 1)
+    if (in_place) {
+        x_a[0] = x_at((lane >> 3) < a.M ? lane >> 3 : -1, lane);
+        x_b[0] = x_at(8 + (lane >> 3) < a.M ? 8 + (lane >> 3) : -1, lane);
+        request(0);
+    }
+    if constexpr (DOWN) {
+        const u32x4 *const from = reinterpret_cast<const u32x4 *>(a.choices);
+        for (int i = threadIdx.x; i < choices_shared(a.experts, n) / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(c.head)[i] = from[i];
+    } else if (wave == 0) {
+        find_choices(a, c, lane, 16 * MT, blockIdx.x == 0);
+    }
+    lds_barrier();
+    if (!DOWN && blockIdx.x == 0) {
+        u32x4 *const to = reinterpret_cast<u32x4 *>(a.choices);
+        for (int i = threadIdx.x; i < choices_shared(a.experts, n) / 16; i += blockDim.x) to[i] = reinterpret_cast<const u32x4 *>(c.head)[i];
+    }
+    const int count = __builtin_amdgcn_readfirstlane(c.head->count);
+    const uint32_t chunks = __builtin_amdgcn_readfirstlane(c.head->chunks), total = chunks * (uint32_t)per_expert;
+    const uint32_t first = (uint32_t)((uint64_t)total * blockIdx.x / gridDim.x), end = (uint32_t)((uint64_t)total * (blockIdx.x + 1) / gridDim.x);
+
+    // Where a unit lies: the expert's place among the chosen ones, the chunk of its choices, the two tiles; the expert.
+    struct At { int r, chunk, f, expert; };
+    At at = {0, 0, 0, 0};
+    auto scalar = [](uint32_t v) { return (int)__builtin_amdgcn_readfirstlane(v); };
+    auto step = [&](At &x) {
+        if (++x.f < per_expert) return;
+        x.f = 0;
+        ++x.chunk;
+        if (x.chunk == scalar(c.info[x.r + 1].z - c.info[x.r].z)) { x.chunk = 0;  ++x.r; }
+        x.expert = x.r < count ? scalar(c.info[x.r].x) : 0;
+    };
+    auto columns = [&](const At &x) {
+        int l = lane;                                  // (what follows from the lane is worked out anew: kept across the loop it costs registers that are spilled)
+        asm volatile("" : "+v"(l));
+        const int col = l & 15;
+        const uint32_t places = c.info[x.r].y;
+        const int start = (int)(places & 0xffffu), size = (int)(places >> 16);
+        if (in_place) {
+            if (l < 16) list[l] = 0xffff;
+            asm volatile("" ::: "memory");
+            if (l < size) {
+                const uint32_t e = c.entry[start + l].x;
+                list[e >> 16] = (uint16_t)e;
+            }
+            asm volatile("" ::: "memory");
+            row[0] = list[col] == 0xffff ? -1 : (int)list[col];
+            asm volatile("" ::: "memory");
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int at0 = 16 * (x.chunk * MT + i);
+            auto of = [&](int q) { return q < size ? (DOWN ? (int)(c.entry[start + q].x & 0xffffu) : (int)(c.entry[start + q].x >> 16)) : -1; };
+            row[i] = at0 + col < size ? (int)(c.entry[start + at0 + col].x & 0xffffu) : -1;
+            x_a[i] = x_at(of(at0 + (l >> 3)), l);
+            x_b[i] = x_at(of(at0 + 8 + (l >> 3)), l);
+        }
     };
     auto fetch = [&](WItem (&w)[SPW], const At &x, int tile, int pass, bool live) {
-        const int64_t base = live ? (int64_t)c.chosen[x.r] * expert_bytes : 0;
-        const int64_t off = ((int64_t)__builtin_amdgcn_readfirstlane((int)(base >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
-        const __amdgpu_buffer_rsrc_t r0 = weight_rsrc(a.up0 + off, (uint32_t)expert_bytes);
-        const __amdgpu_buffer_rsrc_t r1 = weight_rsrc(KIND == kNestedF16Row ? a.up1 + off : a.up0 + off, (uint32_t)expert_bytes);
+        live = live && 2 * x.f + tile < tiles;
+        const int64_t off = (int64_t)x.expert * expert_bytes;
+        const __amdgpu_buffer_rsrc_t r0 = weight_rsrc(w0 + off, (uint32_t)expert_bytes);
+        const __amdgpu_buffer_rsrc_t r1 = weight_rsrc(KIND == kNestedF16Row ? w1 + off : w0 + off, (uint32_t)expert_bytes);
         const int kb = k_of(pass) * EB + (lane & 7) * 16;
         const uint32_t lo = live ? (uint32_t)((2 * x.f + tile) * 16 + (lane >> 3)) * row_bytes + (uint32_t)kb : kDead;
         bool kv[SPW];
 #pragma unroll
-        for (int q = 0; q < SPW; ++q) kv[q] = q < PIECES && kb + 128 * q < a.K * EB;
+        for (int q = 0; q < SPW; ++q) kv[q] = q < PIECES && kb + 128 * q < K * EB;
         load_pieces<KIND, SPW, POL>(w, r0, r1, lo, lo + 8u * row_bytes, kv);
     };
     int region = 0;
@@ -292,268 +369,227 @@ experts_up_kernel(ExpertArgs a) {
             u32x4 w_lo, w_hi;
             operand<KIND>(w[s], w_lo, w_hi);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_lo), as_half8(xa[s][i]), sum[i], 0, 0, 0);
-                sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_hi), as_half8(xb[s][i]), sum[i], 0, 0, 0);
-            }
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) {
+                    sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_lo), as_half8(xa[s][i][t]), sum[i], 0, 0, 0);
+                    sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_hi), as_half8(xb[s][i][t]), sum[i], 0, 0, 0);
+                }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) slot[i * 64] = sum[i];
     };
+    // products of the choices: written through, read back past the caches (every XCD has an L2 of its own)
+    constexpr int kThrough = 1 | 16;                   // sc0 | sc1
+    const __amdgpu_buffer_rsrc_t rsp = weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)((int64_t)n * a.K * 4));
 
-    if (!a.gather) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            x_a[i] = x_at(16 * i + (lane >> 3) < a.M ? 16 * i + (lane >> 3) : -1, lane);
-            x_b[i] = x_at(16 * i + 8 + (lane >> 3) < a.M ? 16 * i + 8 + (lane >> 3) : -1, lane);
-        }
-    }
-    WItem buf0[SPW], buf1[SPW];
-    const int passes = PASSES ? a.passes : 1;
-    columns(at);
-    fetch(buf0, at, 0, 0, true);
-    load_tokens(0);
-    for (uint32_t u = first; u < end; ++u) {
-        At next = at;
-        step(next);
-        for (int pass = 0; pass < passes; ++pass) {
-            if (PASSES && (pass > 0 || u > first)) load_tokens(pass);
-            fetch(buf1, at, 1, pass, true);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(buf0, 0, pass);
-            __builtin_amdgcn_sched_barrier(0);
-            if (pass + 1 < passes) fetch(buf0, at, 0, pass + 1, true);
-            else fetch(buf0, next, 0, 0, u + 1 < end);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(buf1, 1, pass);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        lds_barrier();
-        // The waves take turns with the sums.  (They are written again two units later, behind the next barrier.)
-        for (int item = 0; item < 2 * MT; ++item) {
-            if ((int)((u * (2 * MT) + item) % (unsigned)waves) != wave) continue;
-            const int t = item / MT, i = item - t * MT;
-            floatx4 sum = slots[(((region * 2 + t) * waves) * MT + i) * 64 + lane];
+    if (first < end) {
+        const uint32_t chunk0 = first / (uint32_t)per_expert;
+        for (int base = 0; base < count; base += 64)
+            at.r += __popcll(__ballot(base + lane < count && c.info[min(base + lane, count - 1) + 1].z <= chunk0));
+        at.r = scalar((uint32_t)at.r);
+        at.chunk = scalar(chunk0 - c.info[at.r].z);
+        at.f = scalar(first - chunk0 * (uint32_t)per_expert);
+        at.expert = scalar(c.info[at.r].x);
+        WItem buf0[SPW], buf1[SPW];
+        const int passes = PASSES ? a.passes : 1;
+        fetch(buf0, at, 0, 0, true);
+        columns(at);
+        if (!in_place) request(0);
+        regroup();
+        for (uint32_t u = first; u < end; ++u) {
+            At next = at;
+            step(next);
+            for (int pass = 0; pass < passes; ++pass) {
+                if (PASSES && (pass > 0 || u > first)) {
+                    request(pass);
+                    regroup();
+                }
+                fetch(buf1, at, 1, pass, true);
+                __builtin_amdgcn_sched_barrier(0);
+                consume(buf0, 0, pass);
+                __builtin_amdgcn_sched_barrier(0);
+                if (pass + 1 < passes) fetch(buf0, at, 0, pass + 1, true);
+                else fetch(buf0, next, 0, 0, u + 1 < end);
+                __builtin_amdgcn_sched_barrier(0);
+                consume(buf1, 1, pass);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            lds_barrier();
+            // The waves take turns with the sums.  (They are written again two units later, behind the next barrier.)
+            for (int item = 0; item < 2 * MT; ++item) {
+                if ((int)((u * (2 * MT) + item) % (unsigned)waves) != wave) continue;
+                const int t = item / MT, i = item - t * MT;
+                floatx4 sum = slots[(((region * 2 + t) * waves) * MT + i) * 64 + lane];
 #pragma unroll 4
-            for (int w = 1; w < waves; ++w) {
-                const floatx4 v = slots[(((region * 2 + t) * waves + w) * MT + i) * 64 + lane];
-                sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
-            }
-            int to = row[0];
+                for (int w = 1; w < waves; ++w) {
+                    const floatx4 v = slots[(((region * 2 + t) * waves + w) * MT + i) * 64 + lane];
+                    sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
+                }
+                int to = row[0];
 #pragma unroll
-            for (int q = 1; q < MT; ++q) to = i == q ? row[q] : to;
-            if (to < 0) continue;
-            const float h0 = activate(sum.x, a.act) * sum.y, h1 = activate(sum.z, a.act) * sum.w;
-            const int f = 16 * at.f + 8 * t + 2 * g;
-            uint16_t *const dst = a.H + (int64_t)to * kTerms * a.ffn + f;
-            const uint32_t high = float2_to_half2_bits(h0, h1);
-            *reinterpret_cast<uint32_t *>(dst) = high;
-            if constexpr (kTerms == 2) {
-                // (an infinite first term has no rest)
-                const float l0 = h0 - half_bits_to_float(high & 0xffffu), l1 = h1 - half_bits_to_float(high >> 16);
-                *reinterpret_cast<uint32_t *>(dst + a.ffn) =
-                    float2_to_half2_bits((high & 0x7fffu) == 0x7c00u ? 0.0f : l0, (high & 0x7fff0000u) == 0x7c000000u ? 0.0f : l1);
+                for (int q = 1; q < MT; ++q) to = i == q ? row[q] : to;
+                if (to < 0 || 2 * at.f + t >= tiles) continue;
+                if constexpr (DOWN) {
+                    const uint32_t off = (uint32_t)(((int64_t)to * a.K + 32 * at.f + 16 * t + 4 * g) * 4);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(sum.x), __float_as_uint(sum.y), __float_as_uint(sum.z), __float_as_uint(sum.w)},
+                                                           rsp, off, 0, kThrough);
+                } else {
+                    const float h0 = activate(sum.x, a.act) * sum.y, h1 = activate(sum.z, a.act) * sum.w;
+                    const int f = 16 * at.f + 8 * t + 2 * g;
+                    uint16_t *const dst = a.H + (int64_t)to * kTerms * a.ffn + f;
+                    const uint32_t high = float2_to_half2_bits(h0, h1);
+                    *reinterpret_cast<uint32_t *>(dst) = high;
+                    if constexpr (kTerms == 2) {
+                        // (an infinite first term has no rest)
+                        const float l0 = h0 - half_bits_to_float(high & 0xffffu), l1 = h1 - half_bits_to_float(high >> 16);
+                        *reinterpret_cast<uint32_t *>(dst + a.ffn) =
+                            float2_to_half2_bits((high & 0x7fffu) == 0x7c00u ? 0.0f : l0, (high & 0x7fff0000u) == 0x7c000000u ? 0.0f : l1);
+                    }
+                }
             }
+            if constexpr (kSumRegions<MT> == 2) region ^= 1;
+            else lds_barrier();
+            if (u + 1 < end && (next.r != at.r || next.chunk != at.chunk)) {
+                columns(next);
+                if (!PASSES && !in_place) {
+                    request(0);
+                    regroup();
+                }
+            }
+            at = next;
         }
-        if constexpr (kSumRegions<MT> == 2) region ^= 1;
-        else lds_barrier();
-        if (u + 1 < end && (next.r != at.r || next.chunk != at.chunk)) {
-            columns(next);
-            if (!PASSES && a.gather) load_tokens(0);
-        }
-        at = next;
     }
-}
+    if constexpr (!DOWN) return;
 
-// ---- down products ---------------------------------------------------------------------------------
-// A workgroup owns 16 rows of the output for all tokens and walks over all chosen experts, so that the sum over a token's experts stays in its
-// registers: no second pass, no order that depends on timing.  Work is cut into items of 128 columns of one expert; wave w takes items
-// w, w + 8, ...; weights are loaded DEPTH items ahead, the activated products (from L2) where they are used.  Columns are the tokens as they are; a
-// token tile that has not chosen the expert is skipped.
-template <int KIND, int MT, int POL>
-__global__ void __launch_bounds__(512)
-experts_down_kernel(ExpertArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
-    constexpr int EB = kind_elem_bytes(KIND), DEPTH = KIND == kE4M3Row ? 4 : 3, PIECES = KIND == kPlainF16 ? 2 : 1;
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int g = lane >> 4, r16 = lane & 15;
-    floatx4 *const slots = reinterpret_cast<floatx4 *>(shared);                // [wave][MT][64]
-    const uint32_t own = (uint32_t)(waves * MT * 1024 + wave * 2048);
-    const Choices c = choices_of(a, shared + waves * (MT * 1024 + 2048), true);
-    const Regroup<KIND == kPlainF16> rw(shared, own, lane);
-    const uint32_t row_bytes = (uint32_t)a.ffn * EB;
-    const int64_t expert_bytes = a.K * (int64_t)row_bytes;
-    const int per_expert = (int)((a.ffn + 127) >> 7);
-    struct At { int r, q; };
-    auto forward = [&](At &x, int by) {
-        x.q += by;
-        while (x.q >= per_expert) { x.q -= per_expert;  ++x.r; }
-    };
-    WItem buf[DEPTH][2];
-    auto fetch = [&](WItem (&w)[2], const At &x) {
-        const bool live = x.r < c.count;
-        const int64_t base = live ? (int64_t)c.chosen[x.r] * expert_bytes : 0;
-        const int64_t off = ((int64_t)__builtin_amdgcn_readfirstlane((int)(base >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
-        const __amdgpu_buffer_rsrc_t r0 = weight_rsrc(a.down0 + off, (uint32_t)expert_bytes);
-        const __amdgpu_buffer_rsrc_t r1 = weight_rsrc(KIND == kNestedF16Row ? a.down1 + off : a.down0 + off, (uint32_t)expert_bytes);
-        const int kb = x.q * 128 * EB + (lane & 7) * 16;
-        const uint32_t lo = live ? (uint32_t)(blockIdx.x * 16 + (lane >> 3)) * row_bytes + (uint32_t)kb : kDead;
-        bool kv[2];
+    // ---- the weighted sums -----------------------------------------------------------------------------
+    // (nobody has chosen anything: the rows are shared out)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this lane's products have reached memory
+    __syncthreads();
+    uint32_t *const done = reinterpret_cast<uint32_t *>(c.scratch);            // how many blocks of 32 rows this workgroup adds up, and which
+    if (threadIdx.x == 0) done[0] = 0;
+    __syncthreads();
+    if (total == 0) {
+        for (int f = blockIdx.x + gridDim.x * threadIdx.x; f < per_expert; f += gridDim.x * blockDim.x) done[1 + atomicAdd(&done[0], 1u)] = (uint32_t)f;
+    } else {
+        for (uint32_t u = first + threadIdx.x; u < end; u += blockDim.x) {
+            const uint32_t f = u % (uint32_t)per_expert;
+            if (__hip_atomic_fetch_add(&a.counters[f], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != chunks - 1) continue;
+            __hip_atomic_store(&a.counters[f], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            done[1 + atomicAdd(&done[0], 1u)] = f;
+        }
+    }
+    __syncthreads();
+    const int blocks = (int)done[0], per_block = (int)a.M * 8;
+    for (int i = threadIdx.x; i < blocks * per_block; i += blockDim.x) {
+        const int b = i / per_block, q = i - b * per_block, m = q >> 3, col = 32 * (int)done[1 + b] + 4 * (q & 7);
+        if (col >= a.K) continue;
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int j0 = 0; j0 < a.top_k; j0 += 4) {      // (four loads under way at a time)
+            u32x4 v[4];
+            float share[4];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) kv[q] = q < PIECES && kb + 128 * q < a.ffn * EB;
-        load_pieces<KIND, 2, POL>(w, r0, r1, lo, lo + 8u * row_bytes, kv);
-    };
-    floatx4 total[MT];
+            for (int j = 0; j < 4; ++j) {
+                const int r = m * a.top_k + j0 + j;
+                const bool in = j0 + j < a.top_k && (c.used[r >> 5] >> (r & 31) & 1u) != 0;
+                share[j] = in ? c.share[r] : 0.0f;
+                v[j] = __builtin_amdgcn_raw_buffer_load_b128(rsp, in ? (uint32_t)(((int64_t)r * a.K + col) * 4) : 0xfffffff0u, 0, kThrough);
+            }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) total[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto consume = [&](WItem (&w)[2], const At &x) {
-        regroup_pieces<KIND, 2>(w, rw);
-        u32x4 w_lo[2], w_hi[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) operand<KIND>(w[s], w_lo[s], w_hi[s]);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = 16 * i + r16;
-            const int p = m < a.M ? c.place[x.r * c.padded + m] : kNone;
-            if (!__any(p != kNone)) continue;
-            const int at = m * (int)a.top_k + p;
-            floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-            const uint16_t *const src = a.H + (int64_t)at * kTerms * a.ffn + x.q * 128 + 16 * g;
-            u32x4 h[kTerms][2][2];
-#pragma unroll
-            for (int term = 0; term < kTerms; ++term)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const bool ok = p != kNone && x.q * 128 + 64 * s + 16 * g < a.ffn;
-                    const u32x4 zero = {0u, 0u, 0u, 0u};
-                    h[term][s][0] = ok ? *reinterpret_cast<const u32x4 *>(src + term * a.ffn + 64 * s) : zero;
-                    h[term][s][1] = ok ? *reinterpret_cast<const u32x4 *>(src + term * a.ffn + 64 * s + 8) : zero;
-                }
-#pragma unroll
-            for (int term = kTerms - 1; term >= 0; --term)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_lo[s]), as_half8(h[term][s][0]), sum, 0, 0, 0);
-                    sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_hi[s]), as_half8(h[term][s][1]), sum, 0, 0, 0);
-                }
-            if (p != kNone) {
-                const float weight = c.weights[at];
-                total[i].x = __builtin_fmaf(weight, sum.x, total[i].x);
-                total[i].y = __builtin_fmaf(weight, sum.y, total[i].y);
-                total[i].z = __builtin_fmaf(weight, sum.z, total[i].z);
-                total[i].w = __builtin_fmaf(weight, sum.w, total[i].w);
+            for (int j = 0; j < 4; ++j) {
+                sum.x = __builtin_fmaf(share[j], __uint_as_float(v[j].x), sum.x);
+                sum.y = __builtin_fmaf(share[j], __uint_as_float(v[j].y), sum.y);
+                sum.z = __builtin_fmaf(share[j], __uint_as_float(v[j].z), sum.z);
+                sum.w = __builtin_fmaf(share[j], __uint_as_float(v[j].w), sum.w);
             }
         }
-    };
-    At at = {0, 0}, ahead = {0, 0};
-    forward(at, wave);
-    ahead = at;
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-        fetch(buf[d], ahead);
-        forward(ahead, waves);
-    }
-    while (at.r < c.count) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            if (at.r < c.count) consume(buf[d], at);
-            __builtin_amdgcn_sched_barrier(0);
-            fetch(buf[d], ahead);
-            __builtin_amdgcn_sched_barrier(0);
-            forward(at, waves);
-            forward(ahead, waves);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) slots[(wave * MT + i) * 64 + lane] = total[i];
-    __syncthreads();
-    for (int i = wave; i < MT; i += waves) {
-        floatx4 sum = slots[i * 64 + lane];
-        for (int w = 1; w < waves; ++w) {
-            const floatx4 v = slots[(w * MT + i) * 64 + lane];
-            sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
-        }
-        const int m = 16 * i + r16, n = blockIdx.x * 16 + 4 * g;
-        if (m >= a.M) continue;
         if (a.residual) {
-            const floatx4 r = four_halves(a.residual + (int64_t)m * a.ldr + n, a.vec & 1, 4);
-            sum.x += r.x;  sum.y += r.y;  sum.z += r.z;  sum.w += r.w;
+            const floatx4 v = four_halves(a.residual + (int64_t)m * a.ldr + col, a.vec & 1, 4);
+            sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
         }
         u32x2 o;
         o.x = float2_to_half2_bits(sum.x, sum.y);
         o.y = float2_to_half2_bits(sum.z, sum.w);
-        uint16_t *const dst = a.Y + (int64_t)m * a.ldy + n;
+        uint16_t *const dst = a.Y + (int64_t)m * a.ldy + col;
         if (a.vec & 2) *reinterpret_cast<u32x2 *>(dst) = o;
         else
 #pragma unroll
-            for (int q = 0; q < 4; ++q) dst[q] = (uint16_t)((q < 2 ? o.x : o.y) >> (16 * (q & 1)));
+            for (int p = 0; p < 4; ++p) dst[p] = (uint16_t)((p < 2 ? o.x : o.y) >> (16 * (p & 1)));
     }
 }
 
 // ---- host --------------------------------------------------------------------------------------------
-size_t experts_product_bytes(int64_t M, int64_t top_k, int64_t ffn) { return (size_t)(M * top_k) * kTerms * (size_t)ffn * 2; }
-
-bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k) {
-    // an expert's matrix is addressed with 31 bits
-    return experts <= kMostExperts && M <= kMostTokens && top_k <= kMostTop && 2 * ffn * hidden * 2 + 64 * std::max(hidden, ffn) < ((int64_t)1 << 31);
+// The workspace behind its counters: the choices, the activated products, the products of the choices.
+static size_t choices_bytes(int64_t experts, int64_t n) { return round256((size_t)choices_shared((int)experts, (int)n)); }
+static size_t activated_bytes(int64_t n, int64_t ffn) { return round256((size_t)n * kTerms * (size_t)ffn * 2); }
+size_t experts_workspace_bytes(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k) {
+    return choices_bytes(experts, M * top_k) + activated_bytes(M * top_k, ffn) + (size_t)(M * top_k) * (size_t)hidden * 4;
 }
 
-template <typename Kernel>
-static int launch_experts(Kernel kern, std::atomic<bool> &ready, unsigned grid, unsigned threads, size_t lds, const ExpertArgs &a, hipStream_t stream) {
-    if (lds > 160 * 1024) return kErrShape;
+bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k) {
+    // an expert's matrix and the products between the launches are addressed with 31 bits, and every 32 output rows have a counter
+    constexpr int64_t limit = (int64_t)1 << 31;
+    if (experts > kMostExperts || M > kMostTokens || top_k > kMostTop || hidden > 32 * kMaxCounters) return false;
+    return 2 * ffn * hidden * 2 + 64 * std::max(hidden, ffn) < limit && (int64_t)activated_bytes(M * top_k, ffn) + 4096 < limit &&
+           M * top_k * hidden * 4 + 4096 < limit;
+}
+
+template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN>
+static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) {
+    auto kern = experts_kernel<KIND, MT, SPW, PASSES, POL, DOWN>;
+    static std::atomic<bool> ready{false};
     if (!ready.load(std::memory_order_acquire)) {
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         ready.store(true, std::memory_order_release);
     }
-    kern<<<grid, threads, lds, stream>>>(a);
+    const int n = (int)(a.M * a.top_k);
+    // (behind the choices what finding them takes, or a list of blocks of 32 rows)
+    const size_t lds = (size_t)waves * (kSumRegions<MT> * 2 * MT * 1024 + 2048 + 32) + choices_shared(a.experts, n) +
+                       (DOWN ? (size_t)round16((int)(a.K / 32 + 2) * 4) : choices_scratch(a.experts, n));
+    if (lds > 160 * 1024) return kErrShape;
+    const int64_t units = choice_most(a.experts, n) * ((DOWN ? a.K / 16 + 1 : 2 * a.ffn / 16) / 2);
+    const int per_cu = std::max(1, std::min((MT == 1 && !DOWN ? 16 : 8) / waves, (int)(160 * 1024 / lds)));
+    kern<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(units, 256 * per_cu)), (unsigned)waves * 64, lds, stream>>>(a);
     return hip_ok(hipGetLastError());
 }
 
-template <int KIND, int MT, int SPW, int POL>
-static int launch_up(ExpertArgs a, hipStream_t stream) {
-    const int slices = (int)((a.K + SPW * 64 - 1) / (SPW * 64));
-    const int most = MT == 1 && slices <= 16 ? 16 : 8;         // waves, as the registers allow
+template <int KIND, int MT, int SPW, int POL, bool DOWN>
+static int launch_slices(ExpertArgs a, hipStream_t stream) {
+    const int64_t K = DOWN ? a.ffn : a.K;
+    const int slices = (int)((K + SPW * 64 - 1) / (SPW * 64));
+    const int most = MT == 1 && !DOWN && slices <= 16 ? 16 : 8;        // waves, as the registers allow
     a.passes = (slices + most - 1) / most;
+    a.rotate = (K * kind_elem_bytes(KIND)) % 4096 == 0 ? 1 : 0;
     const int waves = (slices + a.passes - 1) / a.passes;
-    a.rotate = (a.K * kind_elem_bytes(KIND)) % 4096 == 0 ? 1 : 0;
-    const size_t lds = (size_t)waves * (kSumRegions<MT> * 2 * MT * 1024 + 2048 + 64) + choices_bytes(a);
-    const int64_t units = std::min<int64_t>(a.experts, a.M * a.top_k) * (a.ffn / 16);
-    const int64_t fit = 256 * std::max<int64_t>(1, std::min<int64_t>(16 / waves, (int64_t)(160 * 1024 / lds)));
-    static std::atomic<bool> ready{false};
-    static std::atomic<bool> ready_passes{false};
-    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(units, fit));
-    return a.passes > 1 ? launch_experts(experts_up_kernel<KIND, MT, SPW, true, POL>, ready_passes, grid, (unsigned)waves * 64, lds, a, stream)
-                        : launch_experts(experts_up_kernel<KIND, MT, SPW, false, POL>, ready, grid, (unsigned)waves * 64, lds, a, stream);
-}
-template <int KIND, int MT, int POL>
-static int launch_down(const ExpertArgs &a, hipStream_t stream) {
-    static std::atomic<bool> ready{false};
-    return launch_experts(experts_down_kernel<KIND, MT, POL>, ready, (unsigned)(a.K / 16), 512, 8 * (MT * 1024 + 2048) + choices_bytes(a), a, stream);
+    return a.passes > 1 ? launch_experts_t<KIND, MT, SPW, true, POL, DOWN>(a, waves, stream) : launch_experts_t<KIND, MT, SPW, false, POL, DOWN>(a, waves, stream);
 }
 
-template <int KIND, int POL>
-static int launch_kind(const ExpertArgs &a, bool up, hipStream_t stream) {
-    if (!up) return a.M <= 16 ? launch_down<KIND, 1, POL>(a, stream) : (a.M <= 32 ? launch_down<KIND, 2, POL>(a, stream) : launch_down<KIND, 4, POL>(a, stream));
-    if (a.M <= 16 || 2 * a.M * a.top_k <= 16 * a.experts) return launch_up<KIND, 1, 4, POL>(a, stream);
-    return a.M <= 32 || a.M * a.top_k <= 16 * a.experts ? launch_up<KIND, 2, 4, POL>(a, stream) : launch_up<KIND, 4, 2, POL>(a, stream);
+template <int KIND, int POL, bool DOWN>
+static int launch_columns(const ExpertArgs &a, hipStream_t stream) {
+    // both launches alike: the chunks of an expert's choices are counted once
+    if (a.M <= 16 || 2 * a.M * a.top_k <= 16 * a.experts) return launch_slices<KIND, 1, 4, POL, DOWN>(a, stream);
+    return a.M <= 32 || a.M * a.top_k <= 16 * a.experts ? launch_slices<KIND, 2, 4, POL, DOWN>(a, stream) : launch_slices<KIND, 4, 2, POL, DOWN>(a, stream);
+}
+
+template <int KIND, bool DOWN>
+static int launch_lines(const ExpertArgs &a, hipStream_t stream) {
+    const int64_t row = (DOWN ? a.ffn : a.K) * kind_elem_bytes(KIND);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(DOWN ? a.down0 : a.up0) | reinterpret_cast<uintptr_t>(DOWN ? a.down1 : a.up1);
+    return (row & 127) == 0 && (at & 127) == 0 ? launch_columns<KIND, kStream, DOWN>(a, stream) : launch_columns<KIND, kCached, DOWN>(a, stream);
 }
 
 template <int KIND>
-static int launch_lines(const ExpertArgs &a, bool up, hipStream_t stream) {
-    const int64_t row = (up ? a.K : a.ffn) * kind_elem_bytes(KIND);
-    const uintptr_t at = reinterpret_cast<uintptr_t>(up ? a.up0 : a.down0) | reinterpret_cast<uintptr_t>(up ? a.up1 : a.down1);
-    return (row & 127) == 0 && (at & 127) == 0 ? launch_kind<KIND, kStream>(a, up, stream) : launch_kind<KIND, kCached>(a, up, stream);
+static int launch_both(const ExpertArgs &a, hipStream_t stream) {
+    const int st = launch_lines<KIND, false>(a, stream);
+    return st != kOk ? st : launch_lines<KIND, true>(a, stream);
 }
 
-int launch_experts_layer(int kind, ExpertArgs a, hipStream_t stream) {
+int launch_experts_layer(int kind, ExpertArgs a, uint8_t *room, hipStream_t stream) {
+    a.choices = room;
+    a.H = reinterpret_cast<uint16_t *>(room + choices_bytes(a.experts, a.M * a.top_k));
+    a.products = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.H) + activated_bytes(a.M * a.top_k, a.ffn));
     a.gather = a.M > 16 ? 1 : 0;
-    for (const bool up : {true, false}) {
-        const int st = kind == kPlainF16 ? launch_lines<kPlainF16>(a, up, stream)
-                                         : (kind == kE4M3Row ? launch_lines<kE4M3Row>(a, up, stream) : launch_lines<kNestedF16Row>(a, up, stream));
-        if (st != kOk) return st;
-    }
-    return kOk;
+    return kind == kPlainF16 ? launch_both<kPlainF16>(a, stream) : (kind == kE4M3Row ? launch_both<kE4M3Row>(a, stream) : launch_both<kNestedF16Row>(a, stream));
 }
 
 }  // namespace nfp

@@ -62,7 +62,7 @@ int nestedfp_moe_route(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, con
 
 size_t nestedfp_moe_workspace_size(int64_t M, const nestedfp_experts *experts_host, int64_t top_k) {
     if (check_experts(experts_host, M, top_k) != kOk || M == 0) return 0;
-    return kCounterBytes + experts_product_bytes(M, top_k, experts_host->ffn);
+    return kCounterBytes + experts_workspace_bytes(experts_host->experts, experts_host->hidden, experts_host->ffn, M, top_k);
 }
 
 int nestedfp_moe(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_experts *experts_host, int mode, const int32_t *ids,
@@ -81,7 +81,7 @@ int nestedfp_moe(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_exper
     for (const void *w : {e.up_upper, e.down_upper, nested ? e.up_lower : e.up_upper, nested ? e.down_lower : e.down_upper})
         if (!at_multiple(w, 16)) return NESTEDFP_ERR_SHAPE;
     if (!at_multiple(ids, 4) || !at_multiple(weights, 4)) return NESTEDFP_ERR_SHAPE;
-    const size_t need = kCounterBytes + experts_product_bytes(M, top_k, e.ffn);
+    const size_t need = kCounterBytes + experts_workspace_bytes(e.experts, e.hidden, e.ffn, M, top_k);
     if (workspace == nullptr || workspace_bytes < need || !at_multiple(workspace, 16)) return NESTEDFP_ERR_WORKSPACE;
     ExpertArgs a;
     memset(&a, 0, sizeof(a));
@@ -91,10 +91,11 @@ int nestedfp_moe(const uint16_t *X, int64_t M, int64_t ldx, const nestedfp_exper
     a.down0 = static_cast<const uint8_t *>(e.down_upper);
     a.down1 = nested ? static_cast<const uint8_t *>(e.down_lower) : a.down0;
     a.ids = ids;  a.weights = weights;  a.residual = residual;  a.ldr = ldr;  a.Y = Y;  a.ldy = ldy;
-    a.H = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workspace) + kCounterBytes);
+    a.counters = static_cast<uint32_t *>(workspace);
     a.experts = (int32_t)e.experts;  a.top_k = (int32_t)top_k;  a.act = e.activation;
     a.vec = ((ldr & 3) == 0 && at_multiple(residual, 8) ? 1 : 0) | ((ldy & 3) == 0 && at_multiple(Y, 8) ? 2 : 0);
-    return launch_experts_layer(e.is_exception ? kPlainF16 : (nested ? kNestedF16Row : kE4M3Row), a, static_cast<hipStream_t>(stream));
+    return launch_experts_layer(e.is_exception ? kPlainF16 : (nested ? kNestedF16Row : kE4M3Row), a,
+                                static_cast<uint8_t *>(workspace) + kCounterBytes, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

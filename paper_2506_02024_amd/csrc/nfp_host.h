@@ -291,14 +291,17 @@ struct ExpertArgs {
     int64_t ldr;
     uint16_t *Y;
     int64_t ldy;
+    uint8_t *choices;                                  // who has chosen whom, left by the first launch
     uint16_t *H;                                       // activated products between the launches
+    float *products;                                   // [choice][hidden]
+    uint32_t *counters;                                // one per 32 output rows, zero between calls
     int32_t experts, top_k, act;
     int32_t vec;                                       // 1: residuals are loaded four at a time, 2: outputs are stored so
     int32_t passes, rotate, gather;
 };
-size_t experts_product_bytes(int64_t M, int64_t top_k, int64_t ffn);
+size_t experts_workspace_bytes(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);      // behind the counters
 bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);
-int launch_experts_layer(int kind, ExpertArgs a, hipStream_t stream);
+int launch_experts_layer(int kind, ExpertArgs a, uint8_t *room, hipStream_t stream);
 
 bool use_small_gemm(int64_t M);
 bool route_small(int kind, int64_t M, int64_t N, int64_t K, int64_t ldw);     // which of the two families a problem runs on
