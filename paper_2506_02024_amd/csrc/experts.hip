@@ -105,13 +105,18 @@ __device__ __forceinline__ Choices choices_at(uint8_t *at, int experts, int n) {
     c.scratch = at;
     return c;
 }
-__device__ __forceinline__ uint32_t sum_before(uint32_t v, int lane, uint32_t &all) {
-    uint32_t upto = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t before = __shfl_up(upto, d);
-        if (lane >= d) upto += before;
-    }
+// Sum over the lanes before this one, by DPP moves within rows of 16 and from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t add_from(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t &all) {
+    uint32_t upto = add_from<0x111, 0xf>(v);           // lane - 1
+    upto = add_from<0x112, 0xf>(upto);                 // lane - 2
+    upto = add_from<0x114, 0xf>(upto);
+    upto = add_from<0x118, 0xf>(upto);
+    upto = add_from<0x142, 0xa>(upto);                 // last lane of the row before, rows 1 and 3
+    upto = add_from<0x143, 0xc>(upto);                 // lane 31, rows 2 and 3
     all = __builtin_amdgcn_readlane(upto, 63);
     return upto - v;
 }
@@ -152,7 +157,7 @@ __device__ __forceinline__ void find_choices(const ExpertArgs &a, const Choices 
         const uint64_t mask = __ballot(own != 0);
         if (mask == 0) continue;
         uint32_t all;
-        const uint32_t before = sum_before(own, lane, all);
+        const uint32_t before = sum_before(own, all);
         if (own != 0) {
             const int r = count + lanes_before(mask);
             c.info[r] = u32x4{(uint32_t)e, begin + before, 0u, 0u};
@@ -196,7 +201,7 @@ __device__ __forceinline__ void find_choices(const ExpertArgs &a, const Choices 
         const int r = base + lane;
         const uint32_t of_r = r < count ? size[r] : 0u;
         uint32_t all;
-        const uint32_t before = sum_before((of_r + columns - 1) / (uint32_t)columns, lane, all);
+        const uint32_t before = sum_before((of_r + columns - 1) / (uint32_t)columns, all);
         if (r < count) {
             const u32x4 v = c.info[r];
             c.info[r] = u32x4{v.x, v.y | of_r << 16, chunks + before, 0u};
@@ -224,14 +229,16 @@ __device__ __forceinline__ void lds_barrier() {
 // across units and experts; sums meet in LDS, one barrier per unit.
 // Columns are the choices of the expert, loaded anew with every expert, so that 48 tokens over many experts take the time of a few; in the first launch up
 // to 16 tokens stand in the columns as they are (`gather` 0) and are loaded once.
-// The second launch leaves the product of every choice in memory, 32 bits each.  At its end a workgroup counts its units per 32 output rows, past the caches; the one
-// that has the last of them adds up the rows' choices, token by token in their order, so that the result does not depend on timing.
+// The second launch leaves the product of every choice in memory, 32 bits each.  A wave of every workgroup that streams nothing adds up its units' sums,
+// stores them past the caches and counts the units per 32 output rows a unit later, when they have arrived; where it has the last of them, it adds up the rows'
+// choices, token by token in their order, so that the result does not depend on timing.  (Counted by the workgroup at its end, the last workgroups
+// to end had all their rows to add up, 10 to 17 us.)
 // (Tried for the second launch: a workgroup for 16 output rows that walks over all experts and needs no memory in between.  Each of its waves has to fetch
 // the products of every expert anew for 16 rows of weights: 16 tokens, 64 experts of 1408, FP8 mode 80 us; 48 tokens, 96 experts of 1520, FP16 mode 478 us.)
 // (with four column tiles the sums of one unit are all that the LDS has room for: a second barrier)
 template <int MT> constexpr int kSumRegions = MT == 4 ? 1 : 2;
 template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN>
-__global__ void __launch_bounds__(MT == 1 && !PASSES && !DOWN ? 1024 : 512)
+__global__ void __launch_bounds__(MT == 1 && !PASSES ? (DOWN ? 576 : 1024) : 512)
 experts_kernel(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     constexpr int KSTEP = 64, EB = kind_elem_bytes(KIND), PIECES = row_pieces<KIND == kPlainF16 ? kPlainF16 : kNestedF16Row, SPW>();
@@ -239,7 +246,7 @@ experts_kernel(ExpertArgs a) {
     static_assert(PIECES > 0, "whole pieces");
     constexpr int SUMS = kSumRegions<MT> * 2 * MT * 1024;      // bytes of sums per wave
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (blockDim.x >> 6) - (DOWN ? 1 : 0);       // (waves that stream)
     const int g = lane >> 4, n = (int)a.M * a.top_k;
     const int64_t K = DOWN ? a.ffn : a.K;
     const int tiles = (int)((DOWN ? a.K : 2 * a.ffn) >> 4), per_expert = (tiles + 1) >> 1;
@@ -379,10 +386,15 @@ experts_kernel(ExpertArgs a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) slot[i * 64] = sum[i];
     };
-    // products of the choices: written through, read back past the caches (every XCD has an L2 of its own)
-    constexpr int kThrough = 1 | 16;                   // sc0 | sc1
-    const __amdgpu_buffer_rsrc_t rsp = weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)((int64_t)n * a.K * 4));
-
+    auto add_up = [&](int t, int i) {
+        floatx4 sum = slots[(((region * 2 + t) * waves) * MT + i) * 64 + lane];
+#pragma unroll 4
+        for (int w = 1; w < waves; ++w) {
+            const floatx4 v = slots[(((region * 2 + t) * waves + w) * MT + i) * 64 + lane];
+            sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
+        }
+        return sum;
+    };
     if (first < end) {
         const uint32_t chunk0 = first / (uint32_t)per_expert;
         for (int base = 0; base < count; base += 64)
@@ -391,6 +403,101 @@ experts_kernel(ExpertArgs a) {
         at.chunk = scalar(chunk0 - c.info[at.r].z);
         at.f = scalar(first - chunk0 * (uint32_t)per_expert);
         at.expert = scalar(c.info[at.r].x);
+    }
+    if constexpr (DOWN) {
+        if (wave == waves) {
+            // products of the choices: written through, read back past the caches (every XCD has an L2 of its own)
+            constexpr int kThrough = 1 | 16;           // sc0 | sc1
+            const __amdgpu_buffer_rsrc_t rsp = weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)((int64_t)n * a.K * 4));
+            auto join = [&](int f) {
+                for (int i = lane; i < a.M * 8; i += 64) {
+                    const int m = i >> 3, col = 32 * f + 4 * (i & 7);
+                    if (col >= a.K) continue;
+                    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+                    for (int j0 = 0; j0 < a.top_k; j0 += 8) {          // (eight loads under way at a time)
+                        u32x4 v[8];
+                        float share[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int r = m * a.top_k + j0 + j;
+                            const bool in = j0 + j < a.top_k && (c.used[r >> 5] >> (r & 31) & 1u) != 0;
+                            share[j] = in ? c.share[r] : 0.0f;
+                            v[j] = __builtin_amdgcn_raw_buffer_load_b128(rsp, in ? (uint32_t)(((int64_t)r * a.K + col) * 4) : 0xfffffff0u, 0, kThrough);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            sum.x = __builtin_fmaf(share[j], __uint_as_float(v[j].x), sum.x);
+                            sum.y = __builtin_fmaf(share[j], __uint_as_float(v[j].y), sum.y);
+                            sum.z = __builtin_fmaf(share[j], __uint_as_float(v[j].z), sum.z);
+                            sum.w = __builtin_fmaf(share[j], __uint_as_float(v[j].w), sum.w);
+                        }
+                    }
+                    if (a.residual) {
+                        const floatx4 v = four_halves(a.residual + (int64_t)m * a.ldr + col, a.vec & 1, 4);
+                        sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
+                    }
+                    u32x2 o;
+                    o.x = float2_to_half2_bits(sum.x, sum.y);
+                    o.y = float2_to_half2_bits(sum.z, sum.w);
+                    uint16_t *const dst = a.Y + (int64_t)m * a.ldy + col;
+                    if (a.vec & 2) *reinterpret_cast<u32x2 *>(dst) = o;
+                    else
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) dst[p] = (uint16_t)((p < 2 ? o.x : o.y) >> (16 * (p & 1)));
+                }
+            };
+            if (total == 0)                            // nobody has chosen anything: the rows are shared out
+                for (int f = blockIdx.x; f < per_expert; f += gridDim.x) join(f);
+            if (first >= end) return;
+            auto count_unit = [&](int f) {             // (behind a wait for the unit's products)
+                uint32_t before = 0;
+                if (lane == 0) before = __hip_atomic_fetch_add(&a.counters[f], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                return before;
+            };
+            auto finish = [&](int f, uint32_t before) {
+                if ((uint32_t)scalar(before) != chunks - 1) return;
+                if (lane == 0) __hip_atomic_store(&a.counters[f], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                join(f);
+            };
+            columns(at);
+            int f_before = -1;
+            for (uint32_t u = first; u < end; ++u) {
+                lds_barrier();
+                uint32_t before = 0;
+                if (f_before >= 0) {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the products of the unit before
+                    before = count_unit(f_before);
+                }
+                floatx4 sum[2][MT];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) sum[t][i] = add_up(t, i);
+                if constexpr (kSumRegions<MT> == 2) region ^= 1;
+                else lds_barrier();
+                if (f_before >= 0) finish(f_before, before);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        if (row[i] < 0 || 2 * at.f + t >= tiles) continue;
+                        const uint32_t off = (uint32_t)(((int64_t)row[i] * a.K + 32 * at.f + 16 * t + 4 * g) * 4);
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(sum[t][i].x), __float_as_uint(sum[t][i].y), __float_as_uint(sum[t][i].z),
+                                                                     __float_as_uint(sum[t][i].w)}, rsp, off, 0, kThrough);
+                    }
+                f_before = at.f;
+                At next = at;
+                step(next);
+                if (u + 1 < end && (next.r != at.r || next.chunk != at.chunk)) columns(next);
+                at = next;
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            finish(f_before, count_unit(f_before));
+            return;
+        }
+    }
+
+    if (first < end) {
         WItem buf0[SPW], buf1[SPW];
         const int passes = PASSES ? a.passes : 1;
         fetch(buf0, at, 0, 0, true);
@@ -417,24 +524,15 @@ experts_kernel(ExpertArgs a) {
             }
             lds_barrier();
             // The waves take turns with the sums.  (They are written again two units later, behind the next barrier.)
-            for (int item = 0; item < 2 * MT; ++item) {
-                if ((int)((u * (2 * MT) + item) % (unsigned)waves) != wave) continue;
-                const int t = item / MT, i = item - t * MT;
-                floatx4 sum = slots[(((region * 2 + t) * waves) * MT + i) * 64 + lane];
-#pragma unroll 4
-                for (int w = 1; w < waves; ++w) {
-                    const floatx4 v = slots[(((region * 2 + t) * waves + w) * MT + i) * 64 + lane];
-                    sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
-                }
-                int to = row[0];
+            if constexpr (!DOWN) {
+                for (int item = 0; item < 2 * MT; ++item) {
+                    if ((int)((u * (2 * MT) + item) % (unsigned)waves) != wave) continue;
+                    const int t = item / MT, i = item - t * MT;
+                    const floatx4 sum = add_up(t, i);
+                    int to = row[0];
 #pragma unroll
-                for (int q = 1; q < MT; ++q) to = i == q ? row[q] : to;
-                if (to < 0 || 2 * at.f + t >= tiles) continue;
-                if constexpr (DOWN) {
-                    const uint32_t off = (uint32_t)(((int64_t)to * a.K + 32 * at.f + 16 * t + 4 * g) * 4);
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(sum.x), __float_as_uint(sum.y), __float_as_uint(sum.z), __float_as_uint(sum.w)},
-                                                           rsp, off, 0, kThrough);
-                } else {
+                    for (int q = 1; q < MT; ++q) to = i == q ? row[q] : to;
+                    if (to < 0) continue;
                     const float h0 = activate(sum.x, a.act) * sum.y, h1 = activate(sum.z, a.act) * sum.w;
                     const int f = 16 * at.f + 8 * t + 2 * g;
                     uint16_t *const dst = a.H + (int64_t)to * kTerms * a.ffn + f;
@@ -459,62 +557,6 @@ experts_kernel(ExpertArgs a) {
             }
             at = next;
         }
-    }
-    if constexpr (!DOWN) return;
-
-    // ---- the weighted sums -----------------------------------------------------------------------------
-    // (nobody has chosen anything: the rows are shared out)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this lane's products have reached memory
-    __syncthreads();
-    uint32_t *const done = reinterpret_cast<uint32_t *>(c.scratch);            // how many blocks of 32 rows this workgroup adds up, and which
-    if (threadIdx.x == 0) done[0] = 0;
-    __syncthreads();
-    if (total == 0) {
-        for (int f = blockIdx.x + gridDim.x * threadIdx.x; f < per_expert; f += gridDim.x * blockDim.x) done[1 + atomicAdd(&done[0], 1u)] = (uint32_t)f;
-    } else {
-        for (uint32_t u = first + threadIdx.x; u < end; u += blockDim.x) {
-            const uint32_t f = u % (uint32_t)per_expert;
-            if (__hip_atomic_fetch_add(&a.counters[f], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != chunks - 1) continue;
-            __hip_atomic_store(&a.counters[f], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            done[1 + atomicAdd(&done[0], 1u)] = f;
-        }
-    }
-    __syncthreads();
-    const int blocks = (int)done[0], per_block = (int)a.M * 8;
-    for (int i = threadIdx.x; i < blocks * per_block; i += blockDim.x) {
-        const int b = i / per_block, q = i - b * per_block, m = q >> 3, col = 32 * (int)done[1 + b] + 4 * (q & 7);
-        if (col >= a.K) continue;
-        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int j0 = 0; j0 < a.top_k; j0 += 4) {      // (four loads under way at a time)
-            u32x4 v[4];
-            float share[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = m * a.top_k + j0 + j;
-                const bool in = j0 + j < a.top_k && (c.used[r >> 5] >> (r & 31) & 1u) != 0;
-                share[j] = in ? c.share[r] : 0.0f;
-                v[j] = __builtin_amdgcn_raw_buffer_load_b128(rsp, in ? (uint32_t)(((int64_t)r * a.K + col) * 4) : 0xfffffff0u, 0, kThrough);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sum.x = __builtin_fmaf(share[j], __uint_as_float(v[j].x), sum.x);
-                sum.y = __builtin_fmaf(share[j], __uint_as_float(v[j].y), sum.y);
-                sum.z = __builtin_fmaf(share[j], __uint_as_float(v[j].z), sum.z);
-                sum.w = __builtin_fmaf(share[j], __uint_as_float(v[j].w), sum.w);
-            }
-        }
-        if (a.residual) {
-            const floatx4 v = four_halves(a.residual + (int64_t)m * a.ldr + col, a.vec & 1, 4);
-            sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
-        }
-        u32x2 o;
-        o.x = float2_to_half2_bits(sum.x, sum.y);
-        o.y = float2_to_half2_bits(sum.z, sum.w);
-        uint16_t *const dst = a.Y + (int64_t)m * a.ldy + col;
-        if (a.vec & 2) *reinterpret_cast<u32x2 *>(dst) = o;
-        else
-#pragma unroll
-            for (int p = 0; p < 4; ++p) dst[p] = (uint16_t)((p < 2 ? o.x : o.y) >> (16 * (p & 1)));
     }
 }
 
@@ -543,13 +585,15 @@ static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) 
         ready.store(true, std::memory_order_release);
     }
     const int n = (int)(a.M * a.top_k);
-    // (behind the choices what finding them takes, or a list of blocks of 32 rows)
     const size_t lds = (size_t)waves * (kSumRegions<MT> * 2 * MT * 1024 + 2048 + 32) + choices_shared(a.experts, n) +
-                       (DOWN ? (size_t)round16((int)(a.K / 32 + 2) * 4) : choices_scratch(a.experts, n));
+                       (DOWN ? 0 : choices_scratch(a.experts, n));
     if (lds > 160 * 1024) return kErrShape;
     const int64_t units = choice_most(a.experts, n) * ((DOWN ? a.K / 16 + 1 : 2 * a.ffn / 16) / 2);
-    const int per_cu = std::max(1, std::min((MT == 1 && !DOWN ? 16 : 8) / waves, (int)(160 * 1024 / lds)));
-    kern<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(units, 256 * per_cu)), (unsigned)waves * 64, lds, stream>>>(a);
+    // waves that a CU holds, by registers
+    const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : (KIND == kE4M3Row ? 16 : 12)) : (PASSES ? 12 : 16));
+    const int all = waves + (DOWN ? 1 : 0);
+    const int per_cu = std::max(1, std::min(held / all, (int)(160 * 1024 / lds)));
+    kern<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(units, 256 * per_cu)), (unsigned)all * 64, lds, stream>>>(a);
     return hip_ok(hipGetLastError());
 }
 
@@ -557,7 +601,8 @@ template <int KIND, int MT, int SPW, int POL, bool DOWN>
 static int launch_slices(ExpertArgs a, hipStream_t stream) {
     const int64_t K = DOWN ? a.ffn : a.K;
     const int slices = (int)((K + SPW * 64 - 1) / (SPW * 64));
-    const int most = MT == 1 && !DOWN && slices <= 16 ? 16 : 8;        // waves, as the registers allow
+    const int one_pass = MT == 1 ? (DOWN ? 8 : 16) : (DOWN ? 7 : 8);   // waves that stream, as the registers allow
+    const int most = slices <= one_pass ? one_pass : (DOWN ? 7 : 8);
     a.passes = (slices + most - 1) / most;
     a.rotate = (K * kind_elem_bytes(KIND)) % 4096 == 0 ? 1 : 0;
     const int waves = (slices + a.passes - 1) / a.passes;
