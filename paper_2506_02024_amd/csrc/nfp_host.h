@@ -270,7 +270,8 @@ struct RouteArgs {
     const uint16_t *X, *R;
     int64_t ldx, ldr, M, K;
     int32_t experts, top_k, sigmoid, renormalize;
-    int32_t slices, tile0;                             // slices of K; the first token tile of the launch
+    int32_t slices;                                    // of K
+    int64_t token0;                                    // the first token of the launch
     float factor;
     const float *bias;                                 // [experts] or NULL
     double *logits;                                    // [slice][token of the launch][experts]

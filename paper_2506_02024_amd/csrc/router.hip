@@ -11,7 +11,7 @@
 namespace nfp {
 
 typedef double doublex4 __attribute__((ext_vector_type(4)));
-constexpr int kRouteWaves = 8;
+constexpr int kRouteWaves = 8, kMostSlices = 8;
 
 // Orders doubles as unsigned numbers: larger numbers above smaller ones, NaN below all, zero below NaN (for what has been taken or lies outside).
 __device__ __forceinline__ uint64_t sortable(double x) {
@@ -88,111 +88,158 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const double (&logit)
     }
 }
 
-// Workgroup (x, y, z): 16 experts, 16 tokens, one slice of K, which its eight waves share (each holds 8 consecutive columns of a row per lane and step: the sum
+// Workgroup (x, y, z): 16 T experts, 16 T tokens, one slice of K, which its eight waves share (each holds 8 consecutive columns of a row per lane and step: the sum
 // does not care which four columns a MFMA takes, so its step j takes the j-th of each lane's eight).  The logits go to memory past the caches; the
-// workgroup that takes the token tile's last ticket adds the slices in order and chooses, two tokens per wave.
-template <int VALUES>
+// workgroup that takes the token tile's last ticket adds the slices in order and chooses, a token per wave at a time.
+// T: 2 on large batches, where the conversions to 64 bits, half as many per product, take as long as the products (4000 tokens, 256 experts, 4096 columns: 255 us
+// with 1).
+template <int VALUES, int T>
 __global__ void __launch_bounds__(64 * kRouteWaves)
 route_kernel(RouteArgs a) {
     __shared__ doublex4 sums[kRouteWaves][64];
     __shared__ uint32_t ticket;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
     const int tile = blockIdx.y, slice = blockIdx.z;
-    const int64_t token0 = (int64_t)(a.tile0 + tile) * 16;
-    const int e0 = blockIdx.x * 16;
+    const int64_t token0 = (int64_t)a.token0 + tile * (16 * T);
+    const int e0 = blockIdx.x * (16 * T);
     const int steps = (int)((a.K + 31) >> 5), per = (steps + a.slices - 1) / a.slices;
     const int begin = slice * per, end = min(begin + per, steps);
-    const bool has_e = e0 + r16 < a.experts, has_m = token0 + r16 < a.M;
-    const uint16_t *const re = a.R + (int64_t)(e0 + r16) * a.ldr + 8 * g, *const xm = a.X + (token0 + r16) * a.ldx + 8 * g;
-    doublex4 acc = {0.0, 0.0, 0.0, 0.0};
-    auto load = [&](u32x4 &w, u32x4 &x, int s) {
+    const uint16_t *re[T], *xm[T];
+    bool has_e[T], has_m[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        has_e[t] = e0 + 16 * t + r16 < a.experts;
+        has_m[t] = token0 + 16 * t + r16 < a.M;
+        re[t] = a.R + (int64_t)(has_e[t] ? e0 + 16 * t + r16 : 0) * a.ldr + 8 * g;
+        xm[t] = a.X + (has_m[t] ? token0 + 16 * t + r16 : 0) * a.ldx + 8 * g;
+    }
+    doublex4 acc[T][T];
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j) acc[i][j] = doublex4{0.0, 0.0, 0.0, 0.0};
+    struct Step { u32x4 w[T], x[T]; };
+    auto load = [&](Step &v, int s) {
         const u32x4 zero = {0u, 0u, 0u, 0u};
         const bool in = s < end && 32 * s + 8 * g < a.K;
-        w = in && has_e ? *reinterpret_cast<const u32x4 *>(re + 32 * s) : zero;
-        x = in && has_m ? *reinterpret_cast<const u32x4 *>(xm + 32 * s) : zero;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            v.w[t] = in && has_e[t] ? *reinterpret_cast<const u32x4 *>(re[t] + 32 * s) : zero;
+            v.x[t] = in && has_m[t] ? *reinterpret_cast<const u32x4 *>(xm[t] + 32 * s) : zero;
+        }
     };
-    u32x4 w[2], x[2];
-    load(w[0], x[0], begin + wave);
-    load(w[1], x[1], begin + wave + kRouteWaves);
+    Step v[2];
+    load(v[0], begin + wave);
+    load(v[1], begin + wave + kRouteWaves);
     for (int s = begin + wave; s < end; s += 2 * kRouteWaves) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const u32x4 wn = w[b], xn = x[b];
-            load(w[b], x[b], s + (2 + b) * kRouteWaves);
+            const Step now = v[b];
+            load(v[b], s + (2 + b) * kRouteWaves);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t half = 16u * (j & 1);
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)half_bits_to_float((wn[j >> 1] >> half) & 0xffffu),
-                                                           (double)half_bits_to_float((xn[j >> 1] >> half) & 0xffffu), acc, 0, 0, 0);
+                double w[T], x[T];
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    w[t] = (double)half_bits_to_float((now.w[t][j >> 1] >> half) & 0xffffu);
+                    x[t] = (double)half_bits_to_float((now.x[t][j >> 1] >> half) & 0xffffu);
+                }
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+#pragma unroll
+                    for (int q = 0; q < T; ++q) acc[i][q] = __builtin_amdgcn_mfma_f64_16x16x4f64(w[i], x[q], acc[i][q], 0, 0, 0);
             }
         }
     }
-    sums[wave][lane] = acc;
-    __syncthreads();
-    // rows of the result: expert g + 4 v of lane group g, column: token r16
     constexpr int kThrough = 1 | 16;                   // sc0 | sc1: every XCD has an L2 of its own
-    const int tokens = (int)min((int64_t)gridDim.y * 16, a.M - (int64_t)a.tile0 * 16);          // of this launch
+    const int tokens = (int)min((int64_t)gridDim.y * (16 * T), a.M - a.token0);         // of this launch
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         a.logits, 0, (uint32_t)((int64_t)a.slices * tokens * a.experts * 8), 0x00020000);
-    if (threadIdx.x < 256) {
-        const int v = threadIdx.x >> 6, e = e0 + g + 4 * v, m = tile * 16 + r16;
-        double sum = sums[0][lane][v];
+    // the waves' sums, 16 x 16 at a time; rows of a block: expert g + 4 v of lane group g, column: token r16
 #pragma unroll
-        for (int q = 1; q < kRouteWaves; ++q) sum += sums[q][lane][v];
-        const uint64_t bits = (uint64_t)__double_as_longlong(sum);
-        if (e < a.experts && m < tokens)
-            __builtin_amdgcn_raw_buffer_store_b64(u32x2{(uint32_t)bits, (uint32_t)(bits >> 32)}, rs,
-                                                  (uint32_t)((((int64_t)slice * tokens + m) * a.experts + e) * 8), 0, kThrough);
-    }
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int q = 0; q < T; ++q) {
+            if (i + q > 0) __syncthreads();
+            sums[wave][lane] = acc[i][q];
+            __syncthreads();
+            if (threadIdx.x < 256) {
+                const int row = threadIdx.x >> 6, e = e0 + 16 * i + g + 4 * row, m = tile * (16 * T) + 16 * q + r16;
+                double sum = sums[0][lane][row];
+#pragma unroll
+                for (int w = 1; w < kRouteWaves; ++w) sum += sums[w][lane][row];
+                const uint64_t bits = (uint64_t)__double_as_longlong(sum);
+                if (e < a.experts && m < tokens)
+                    __builtin_amdgcn_raw_buffer_store_b64(u32x2{(uint32_t)bits, (uint32_t)(bits >> 32)}, rs,
+                                                          (uint32_t)((((int64_t)slice * tokens + m) * a.experts + e) * 8), 0, kThrough);
+            }
+        }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this lane's stores have reached memory
     __syncthreads();
     if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(&a.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (ticket != gridDim.x * gridDim.z - 1) return;
-    for (int q = wave; q < 16 && tile * 16 + q < tokens; q += kRouteWaves) {
-        const int m = tile * 16 + q;
+    if (threadIdx.x == 0) __hip_atomic_store(&a.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int q = wave; q < 16 * T && tile * (16 * T) + q < tokens; q += kRouteWaves) {
+        const int m = tile * (16 * T) + q;
         double logit[VALUES];
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) logit[v] = 0.0;
-        for (int s = 0; s < a.slices; ++s) {
-            u32x2 bits[VALUES];
+        for (int i = 0; i < VALUES; ++i) logit[i] = 0.0;
+        auto add = [&](auto count, int s0) {           // so many slices under way at a time
+            u32x2 bits[decltype(count)::value][VALUES];
 #pragma unroll
-            for (int v = 0; v < VALUES; ++v)
-                bits[v] = __builtin_amdgcn_raw_buffer_load_b64(
-                    rs, lane + 64 * v < a.experts ? (uint32_t)((((int64_t)s * tokens + m) * a.experts + lane + 64 * v) * 8) : 0xfffffff0u, 0, kThrough);
+            for (int s = 0; s < decltype(count)::value; ++s)
 #pragma unroll
-            for (int v = 0; v < VALUES; ++v) logit[v] += __longlong_as_double((long long)(((uint64_t)bits[v].y << 32) | bits[v].x));
-        }
-        choose<VALUES>(a, logit, (int64_t)a.tile0 * 16 + m, lane);
+                for (int i = 0; i < VALUES; ++i)
+                    bits[s][i] = __builtin_amdgcn_raw_buffer_load_b64(
+                        rs, s0 + s < a.slices && lane + 64 * i < a.experts ? (uint32_t)((((int64_t)(s0 + s) * tokens + m) * a.experts + lane + 64 * i) * 8) : 0xfffffff0u,
+                        0, kThrough);
+#pragma unroll
+            for (int s = 0; s < decltype(count)::value; ++s)
+#pragma unroll
+                for (int i = 0; i < VALUES; ++i)
+                    if (s0 + s < a.slices) logit[i] += __longlong_as_double((long long)(((uint64_t)bits[s][i].y << 32) | bits[s][i].x));
+        };
+        if (a.slices == 1) add(std::integral_constant<int, 1>{}, 0);
+        else add(std::integral_constant<int, kMostSlices>{}, 0);
+        choose<VALUES>(a, logit, (int64_t)a.token0 + m, lane);
     }
-    if (threadIdx.x == 0) __hip_atomic_store(&a.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Tokens of a launch: as many tiles as there are counters, and 32 MiB of logits (of 256 experts 16384 tokens, whose products take 0.4 ms).
 static int64_t route_tokens(int64_t M, int64_t experts) {
-    const int64_t most = std::min<int64_t>(16 * kMaxCounters, (((int64_t)1 << 22) / experts) & ~(int64_t)15);
+    const int64_t most = std::min<int64_t>(16 * kMaxCounters, (((int64_t)1 << 22) / experts) & ~(int64_t)31);
     return std::min(M, most);
 }
+static bool route_pairs(int64_t M, int64_t experts) { return ((M + 31) / 32) * ((experts + 31) / 32) >= 512; }       // two workgroups per CU
 // Slices of K: enough workgroups for the chip, at least a step of every wave's each.
 static int route_slices(int64_t M, int64_t experts, int64_t K) {
     const int64_t tiles = ((experts + 15) / 16) * ((M + 15) / 16), steps = (K + 31) / 32;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({16, 256 / tiles, steps / kRouteWaves}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kMostSlices, 256 / tiles, steps / kRouteWaves}));
 }
 size_t route_logit_bytes(int64_t M, int64_t experts, int64_t K) {
     const int64_t tokens = route_tokens(M, experts);
     return (size_t)route_slices(tokens, experts, K) * (size_t)tokens * (size_t)experts * 8;
 }
 
+template <int T>
+static void launch_route_t(const RouteArgs &a, int64_t tokens, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.experts + 16 * T - 1) / (16 * T)), (unsigned)((tokens + 16 * T - 1) / (16 * T)), (unsigned)a.slices);
+    if (a.experts <= 64) route_kernel<1, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else if (a.experts <= 128) route_kernel<2, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else if (a.experts <= 256) route_kernel<4, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else route_kernel<8, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+}
+
 int launch_route(RouteArgs a, hipStream_t stream) {
     const int64_t tokens = route_tokens(a.M, a.experts);
     a.slices = route_slices(tokens, a.experts, a.K);
     for (int64_t m = 0; m < a.M; m += tokens) {
-        a.tile0 = (int32_t)(m / 16);
-        const dim3 grid((unsigned)((a.experts + 15) / 16), (unsigned)((std::min(tokens, a.M - m) + 15) / 16), (unsigned)a.slices);
-        if (a.experts <= 64) route_kernel<1><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-        else if (a.experts <= 128) route_kernel<2><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-        else if (a.experts <= 256) route_kernel<4><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-        else route_kernel<8><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+        a.token0 = m;
+        const int64_t some = std::min(tokens, a.M - m);
+        if (a.slices == 1 && route_pairs(some, a.experts)) launch_route_t<2>(a, some, stream);
+        else launch_route_t<1>(a, some, stream);
         if (hipGetLastError() != hipSuccess) return kErrHip;
     }
     return kOk;
