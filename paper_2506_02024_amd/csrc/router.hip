@@ -19,81 +19,119 @@ __device__ __forceinline__ uint64_t sortable(double x) {
     const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);          // (-0 is 0)
     return b ^ ((b >> 63) != 0 ? ~0ull : 1ull << 63);
 }
-__device__ __forceinline__ double sum_of_wave(double v) {
+__device__ __forceinline__ double unsorted(uint64_t key) {
+    return key == 1 ? __longlong_as_double(0x7ff8000000000000ll) : __longlong_as_double((long long)(key ^ ((key >> 63) != 0 ? 1ull << 63 : ~0ull)));
+}
+// Largest value and sum of the lanes of a group, in all of them.
+template <int GROUP>
+__device__ __forceinline__ uint32_t max_of_group(uint32_t v) {
+    if (GROUP == 64) return max_of_wave(v);
+    v = max_of_16_lanes(v);
+    return GROUP == 32 ? max(v, (uint32_t)__shfl_xor((int)v, 16)) : v;
+}
+template <int GROUP>
+__device__ __forceinline__ double sum_of_group(double v) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    for (int d = 1; d < GROUP; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
 
-// One token's choice by one wave; lane l holds experts l, l + 64, ....  VALUES: of 64 experts each.
-template <int VALUES>
-__device__ __forceinline__ void choose(const RouteArgs &a, const double (&logit)[VALUES], int64_t token, int lane) {
-    double score[VALUES];
+// The choice of one token by a group of lanes; lane `sub` of the group holds experts sub, sub + GROUP, ....  Groups of a wave choose side by side (what is longest, the
+// search for the largest one top_k times, is the same work for one token as for four); `live`: the group has a token.  Scores of all experts are worked out only
+// where they matter: for a bias, or for the sum of a softmax that is not divided out again.
+template <int GROUP, int VALUES>
+__device__ __forceinline__ void choose(const RouteArgs &a, const double (&logit)[VALUES], int64_t token, int lane, bool live) {
+    const int sub = lane & (GROUP - 1);
     uint64_t key[VALUES];
-    if (a.sigmoid) {
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) score[v] = 1.0 / (1.0 + exp(-logit[v]));
-    } else {
-        uint64_t best = 0;
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) best = max(best, lane + 64 * v < a.experts ? sortable(logit[v]) : 0);
-        const uint32_t high = max_of_wave((uint32_t)(best >> 32)), low = max_of_wave((uint32_t)(best >> 32) == high ? (uint32_t)best : 0u);
-        const uint64_t b = ((uint64_t)high << 32) | low;
-        const double most = __longlong_as_double((long long)(b ^ ((b >> 63) != 0 ? 1ull << 63 : ~0ull)));       // (of NaN alone: some NaN)
-        double sum = 0.0;
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) {
-            score[v] = lane + 64 * v < a.experts ? exp(logit[v] - most) : 0.0;
-            sum += score[v];
-        }
-        sum = sum_of_wave(sum);
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) score[v] /= sum;
-    }
+    double score[VALUES];
+    double most = 0.0, sum = 1.0;
+    uint32_t strange = 0;                              // a NaN among the logits
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) {
-        const int e = lane + 64 * v;
-        key[v] = e < a.experts ? sortable(a.bias ? score[v] + (double)a.bias[e] : logit[v]) : 0;
+        key[v] = sub + GROUP * v < a.experts ? sortable(logit[v]) : 0;
+        strange |= key[v] == 1 ? 1u : 0u;
+        score[v] = 0.0;
     }
-    // the largest, top_k times; the lowest index of equal ones
-    double mine = 0.0;                                 // lane j: the score of the j-th choice
-    int id = 0;
+    if (!a.sigmoid) {
+        uint64_t best = key[0];
+#pragma unroll
+        for (int v = 1; v < VALUES; ++v) best = max(best, key[v]);
+        const uint32_t high = max_of_group<GROUP>((uint32_t)(best >> 32)), low = max_of_group<GROUP>((uint32_t)(best >> 32) == high ? (uint32_t)best : 0u);
+        most = unsorted(((uint64_t)high << 32) | low);
+        if (a.bias || !a.renormalize) {
+            sum = 0.0;
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) {
+                score[v] = sub + GROUP * v < a.experts ? exp(logit[v] - most) : 0.0;
+                sum += score[v];
+            }
+            sum = sum_of_group<GROUP>(sum);
+        }
+        if (max_of_group<GROUP>(strange)) sum = __longlong_as_double(0x7ff8000000000000ll);
+    }
+    auto of = [&](double l) { return a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - most) / sum; };
+    if (a.bias) {
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            const int e = sub + GROUP * v;
+            score[v] = a.sigmoid ? of(logit[v]) : score[v] / sum;
+            key[v] = e < a.experts ? sortable(score[v] + (double)a.bias[e]) : 0;
+        }
+    }
+    // the largest, top_k times; the lowest index of equal ones.  Lane j keeps the j-th (and the one GROUP further on)
+    constexpr int KEPT = GROUP < 32 ? 2 : 1;           // (top_k is 32 at most)
+    double mine[KEPT];
+    int id[KEPT];
+#pragma unroll
+    for (int q = 0; q < KEPT; ++q) { mine[q] = 0.0;  id[q] = 0; }
     for (int j = 0; j < a.top_k; ++j) {
         uint64_t best = key[0];
-        int at = lane;
+        int at = sub;
 #pragma unroll
         for (int v = 1; v < VALUES; ++v)
-            if (key[v] > best) { best = key[v];  at = lane + 64 * v; }
-        const uint32_t high = max_of_wave((uint32_t)(best >> 32));
+            if (key[v] > best) { best = key[v];  at = sub + GROUP * v; }
+        const uint32_t high = max_of_group<GROUP>((uint32_t)(best >> 32));
         const bool in = (uint32_t)(best >> 32) == high;
-        const uint32_t low = max_of_wave(in ? (uint32_t)best : 0u);
-        const uint32_t first = ~max_of_wave(in && (uint32_t)best == low ? ~(uint32_t)at : 0u);
-        const int owner = (int)(first & 63u), which = (int)(first >> 6);
-        double s = score[0];
+        const uint32_t low = max_of_group<GROUP>(in ? (uint32_t)best : 0u);
+        const int first = (int)~max_of_group<GROUP>(in && (uint32_t)best == low ? ~(uint32_t)at : 0u);
+        double value;
+        if (a.bias) {                                  // the score itself
+            double s = score[0];
 #pragma unroll
-        for (int v = 1; v < VALUES; ++v) s = which == v ? score[v] : s;
-        s = __shfl(s, owner);
+            for (int v = 1; v < VALUES; ++v) s = first == sub + GROUP * v ? score[v] : s;
+            value = __shfl(s, (lane & ~(GROUP - 1)) | (first & (GROUP - 1)));
+        } else {
+            value = unsorted(((uint64_t)high << 32) | low);
+        }
 #pragma unroll
         for (int v = 0; v < VALUES; ++v)
-            if (lane == owner && which == v) key[v] = 0;
-        if (lane == j) { mine = s;  id = (int)first; }
+            if (first == sub + GROUP * v) key[v] = 0;
+#pragma unroll
+        for (int q = 0; q < KEPT; ++q)
+            if (j == sub + GROUP * q) { mine[q] = value;  id[q] = first; }
     }
-    if (a.renormalize) {
-        const double sum = sum_of_wave(lane < a.top_k ? mine : 0.0);
-        mine /= sum;
+    double all = 0.0;
+#pragma unroll
+    for (int q = 0; q < KEPT; ++q) {
+        if (!a.bias) mine[q] = of(mine[q]);
+        all += sub + GROUP * q < a.top_k ? mine[q] : 0.0;
     }
-    if (lane < a.top_k) {
-        a.ids[token * a.top_k + lane] = id;
-        a.weights[token * a.top_k + lane] = (float)(mine * (double)a.factor);
+    if (a.renormalize) all = sum_of_group<GROUP>(all);
+#pragma unroll
+    for (int q = 0; q < KEPT; ++q) {
+        const int j = sub + GROUP * q;
+        if (!live || j >= a.top_k) continue;
+        a.ids[token * a.top_k + j] = id[q];
+        a.weights[token * a.top_k + j] = (float)((a.renormalize ? mine[q] / all : mine[q]) * (double)a.factor);
     }
 }
 
 // Workgroup (x, y, z): 16 T experts, 16 T tokens, one slice of K, which its eight waves share (each holds 8 consecutive columns of a row per lane and step: the sum
 // does not care which four columns a MFMA takes, so its step j takes the j-th of each lane's eight).  The logits go to memory past the caches; the
-// workgroup that takes the token tile's last ticket adds the slices in order and chooses, a token per wave at a time.
+// workgroup that takes the token tile's last ticket adds the slices in order and chooses, a token for every GROUP lanes.
 // T: 2 on large batches, where the conversions to 64 bits, half as many per product, take as long as the products (4000 tokens, 256 experts, 4096 columns: 255 us
 // with 1).
-template <int VALUES, int T>
+template <int GROUP, int VALUES, int T>
 __global__ void __launch_bounds__(64 * kRouteWaves)
 route_kernel(RouteArgs a) {
     __shared__ doublex4 sums[kRouteWaves][64];
@@ -181,8 +219,11 @@ route_kernel(RouteArgs a) {
     __syncthreads();
     if (ticket != gridDim.x * gridDim.z - 1) return;
     if (threadIdx.x == 0) __hip_atomic_store(&a.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int q = wave; q < 16 * T && tile * (16 * T) + q < tokens; q += kRouteWaves) {
-        const int m = tile * (16 * T) + q;
+    constexpr int AT_ONCE = 64 / GROUP;                // tokens of a wave
+    const int sub = lane & (GROUP - 1);
+    for (int q = wave * AT_ONCE; q < 16 * T && tile * (16 * T) + q < tokens; q += kRouteWaves * AT_ONCE) {
+        const int m = tile * (16 * T) + q + lane / GROUP;
+        const bool live = m < tokens;
         double logit[VALUES];
 #pragma unroll
         for (int i = 0; i < VALUES; ++i) logit[i] = 0.0;
@@ -193,17 +234,18 @@ route_kernel(RouteArgs a) {
 #pragma unroll
                 for (int i = 0; i < VALUES; ++i)
                     bits[s][i] = __builtin_amdgcn_raw_buffer_load_b64(
-                        rs, s0 + s < a.slices && lane + 64 * i < a.experts ? (uint32_t)((((int64_t)(s0 + s) * tokens + m) * a.experts + lane + 64 * i) * 8) : 0xfffffff0u,
-                        0, kThrough);
+                        rs, live && s0 + s < a.slices && sub + GROUP * i < a.experts
+                                ? (uint32_t)((((int64_t)(s0 + s) * tokens + m) * a.experts + sub + GROUP * i) * 8) : 0xfffffff0u, 0, kThrough);
 #pragma unroll
             for (int s = 0; s < decltype(count)::value; ++s)
 #pragma unroll
                 for (int i = 0; i < VALUES; ++i)
                     if (s0 + s < a.slices) logit[i] += __longlong_as_double((long long)(((uint64_t)bits[s][i].y << 32) | bits[s][i].x));
         };
-        if (a.slices == 1) add(std::integral_constant<int, 1>{}, 0);
-        else add(std::integral_constant<int, kMostSlices>{}, 0);
-        choose<VALUES>(a, logit, (int64_t)a.token0 + m, lane);
+        if (T > 1 || a.slices == 1) add(std::integral_constant<int, 1>{}, 0);
+        else
+            for (int s0 = 0; s0 < a.slices; s0 += 32 / VALUES) add(std::integral_constant<int, 32 / VALUES>{}, s0);
+        choose<GROUP, VALUES>(a, logit, (int64_t)a.token0 + m, lane, live);
     }
 }
 
@@ -223,13 +265,13 @@ size_t route_logit_bytes(int64_t M, int64_t experts, int64_t K) {
     return (size_t)route_slices(tokens, experts, K) * (size_t)tokens * (size_t)experts * 8;
 }
 
-template <int T>
+template <int T, int GROUP>
 static void launch_route_t(const RouteArgs &a, int64_t tokens, hipStream_t stream) {
     const dim3 grid((unsigned)((a.experts + 16 * T - 1) / (16 * T)), (unsigned)((tokens + 16 * T - 1) / (16 * T)), (unsigned)a.slices);
-    if (a.experts <= 64) route_kernel<1, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-    else if (a.experts <= 128) route_kernel<2, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-    else if (a.experts <= 256) route_kernel<4, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
-    else route_kernel<8, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    if (a.experts <= 64) route_kernel<GROUP, 64 / GROUP, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else if (a.experts <= 128) route_kernel<GROUP, 128 / GROUP, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else if (a.experts <= 256) route_kernel<GROUP, 256 / GROUP, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
+    else route_kernel<GROUP < 32 ? 32 : GROUP, GROUP < 64 ? 16 : 8, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
 }
 
 int launch_route(RouteArgs a, hipStream_t stream) {
@@ -238,8 +280,10 @@ int launch_route(RouteArgs a, hipStream_t stream) {
     for (int64_t m = 0; m < a.M; m += tokens) {
         a.token0 = m;
         const int64_t some = std::min(tokens, a.M - m);
-        if (a.slices == 1 && route_pairs(some, a.experts)) launch_route_t<2>(a, some, stream);
-        else launch_route_t<1>(a, some, stream);
+        // (a token per wave, two or four: as many waves as a tile has)
+        if (a.slices == 1 && route_pairs(some, a.experts)) launch_route_t<2, 16>(a, some, stream);
+        else if (some <= kRouteWaves) launch_route_t<1, 64>(a, some, stream);
+        else launch_route_t<1, 32>(a, some, stream);
         if (hipGetLastError() != hipSuccess) return kErrHip;
     }
     return kOk;
