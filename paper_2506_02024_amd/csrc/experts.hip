@@ -223,34 +223,38 @@ __device__ __forceinline__ void lds_barrier() {
 
 // ---- the kernel ---------------------------------------------------------------------------------------
 // Rows of weights: gate and up rows in turn (first launch, !DOWN), so that a lane's four sums of a 16-row tile are two gated pairs; rows of the output (DOWN).
-// A unit of work is two such tiles of one expert for up to 16 MT of its choices.  All units stand in one row, expert by expert, and every
+// A unit of work is two (or four) such tiles of one expert for up to 16 MT of its choices.  All units stand in one row, expert by expert, and every
 // workgroup takes an equal stretch.  Its waves share K (slices of SPW steps of 64 columns, in several passes where K is longer) and keep
 // the columns' values of their slice in registers: tokens, or the products of the first launch in two terms.  Tile t + 1 is loaded while tile t is multiplied,
 // across units and experts; sums meet in LDS, one barrier per unit.
 // Columns are the choices of the expert, loaded anew with every expert, so that 48 tokens over many experts take the time of a few; in the first launch up
 // to 16 tokens stand in the columns as they are (`gather` 0) and are loaded once.
 // The second launch leaves the product of every choice in memory, 32 bits each.  A wave of every workgroup that streams nothing adds up its units' sums,
-// stores them past the caches and counts the units per 32 output rows a unit later, when they have arrived; where it has the last of them, it adds up the rows'
+// stores them past the caches and counts the units per block of output rows a unit later, when they have arrived; where it has the last of them, it adds up the rows'
 // choices, token by token in their order, so that the result does not depend on timing.  (Counted by the workgroup at its end, the last workgroups
 // to end had all their rows to add up, 10 to 17 us.)
 // (Tried for the second launch: a workgroup for 16 output rows that walks over all experts and needs no memory in between.  Each of its waves has to fetch
 // the products of every expert anew for 16 rows of weights: 16 tokens, 64 experts of 1408, FP8 mode 80 us; 48 tokens, 96 experts of 1520, FP16 mode 478 us.)
-// (with four column tiles the sums of one unit are all that the LDS has room for: a second barrier)
-template <int MT> constexpr int kSumRegions = MT == 4 ? 1 : 2;
-template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN>
+// TILES: 4 where K takes several passes and there are units enough: the columns' values are loaded anew for every unit and pass, which two tiles pay
+// for badly (FP8 mode, 16 tokens, 64 experts of 4096: down products 231 us with two, 193 with four; but 4 tokens, 8 experts of 14336, 320 units of four for 256
+// workgroups: 113 and 128).
+// (with many sums those of one unit are all that the LDS has room for: a second barrier)
+constexpr int sum_regions(int MT, int TILES) { return MT * TILES > 4 ? 1 : 2; }
+template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN, int TILES>
 __global__ void __launch_bounds__(MT == 1 && !PASSES ? (DOWN ? 576 : 1024) : 512)
 experts_kernel(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     constexpr int KSTEP = 64, EB = kind_elem_bytes(KIND), PIECES = row_pieces<KIND == kPlainF16 ? kPlainF16 : kNestedF16Row, SPW>();
     constexpr int TERMS = DOWN ? kTerms : 1;
     static_assert(PIECES > 0, "whole pieces");
-    constexpr int SUMS = kSumRegions<MT> * 2 * MT * 1024;      // bytes of sums per wave
+    constexpr int REGIONS = sum_regions(MT, TILES);
+    constexpr int SUMS = REGIONS * TILES * MT * 1024;      // bytes of sums per wave
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (blockDim.x >> 6) - (DOWN ? 1 : 0);       // (waves that stream)
     const int g = lane >> 4, n = (int)a.M * a.top_k;
     const int64_t K = DOWN ? a.ffn : a.K;
-    const int tiles = (int)((DOWN ? a.K : 2 * a.ffn) >> 4), per_expert = (tiles + 1) >> 1;
-    floatx4 *const slots = reinterpret_cast<floatx4 *>(shared);                // [regions][2 tiles][wave][MT][64]
+    const int tiles = (int)((DOWN ? a.K : 2 * a.ffn) >> 4), per_expert = (tiles + TILES - 1) / TILES;
+    floatx4 *const slots = reinterpret_cast<floatx4 *>(shared);                // [regions][tiles][wave][MT][64]
     const uint32_t own = (uint32_t)(waves * SUMS + wave * 2048);
     uint16_t *const list = reinterpret_cast<uint16_t *>(shared + waves * (SUMS + 2048) + wave * 32);       // the columns' rows
     const Choices c = choices_at(shared + waves * (SUMS + 2048 + 32), a.experts, n);
@@ -353,12 +357,12 @@ experts_kernel(ExpertArgs a) {
         }
     };
     auto fetch = [&](WItem (&w)[SPW], const At &x, int tile, int pass, bool live) {
-        live = live && 2 * x.f + tile < tiles;
+        live = live && TILES * x.f + tile < tiles;
         const int64_t off = (int64_t)x.expert * expert_bytes;
         const __amdgpu_buffer_rsrc_t r0 = weight_rsrc(w0 + off, (uint32_t)expert_bytes);
         const __amdgpu_buffer_rsrc_t r1 = weight_rsrc(KIND == kNestedF16Row ? w1 + off : w0 + off, (uint32_t)expert_bytes);
         const int kb = k_of(pass) * EB + (lane & 7) * 16;
-        const uint32_t lo = live ? (uint32_t)((2 * x.f + tile) * 16 + (lane >> 3)) * row_bytes + (uint32_t)kb : kDead;
+        const uint32_t lo = live ? (uint32_t)((TILES * x.f + tile) * 16 + (lane >> 3)) * row_bytes + (uint32_t)kb : kDead;
         bool kv[SPW];
 #pragma unroll
         for (int q = 0; q < SPW; ++q) kv[q] = q < PIECES && kb + 128 * q < K * EB;
@@ -366,7 +370,7 @@ experts_kernel(ExpertArgs a) {
     };
     int region = 0;
     auto consume = [&](WItem (&w)[SPW], int tile, int pass) {
-        floatx4 *const slot = slots + ((region * 2 + tile) * waves + ks) * MT * 64 + lane;
+        floatx4 *const slot = slots + ((region * TILES + tile) * waves + ks) * MT * 64 + lane;
         floatx4 sum[MT];
         regroup_pieces<KIND, SPW>(w, rw);
 #pragma unroll
@@ -387,10 +391,10 @@ experts_kernel(ExpertArgs a) {
         for (int i = 0; i < MT; ++i) slot[i * 64] = sum[i];
     };
     auto add_up = [&](int t, int i) {
-        floatx4 sum = slots[(((region * 2 + t) * waves) * MT + i) * 64 + lane];
+        floatx4 sum = slots[(((region * TILES + t) * waves) * MT + i) * 64 + lane];
 #pragma unroll 4
         for (int w = 1; w < waves; ++w) {
-            const floatx4 v = slots[(((region * 2 + t) * waves + w) * MT + i) * 64 + lane];
+            const floatx4 v = slots[(((region * TILES + t) * waves + w) * MT + i) * 64 + lane];
             sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
         }
         return sum;
@@ -410,8 +414,8 @@ experts_kernel(ExpertArgs a) {
             constexpr int kThrough = 1 | 16;           // sc0 | sc1
             const __amdgpu_buffer_rsrc_t rsp = weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)((int64_t)n * a.K * 4));
             auto join = [&](int f) {
-                for (int i = lane; i < a.M * 8; i += 64) {
-                    const int m = i >> 3, col = 32 * f + 4 * (i & 7);
+                for (int i = lane; i < a.M * (4 * TILES); i += 64) {
+                    const int m = i / (4 * TILES), col = 16 * TILES * f + 4 * (i % (4 * TILES));
                     if (col >= a.K) continue;
                     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
                     for (int j0 = 0; j0 < a.top_k; j0 += 8) {          // (eight loads under way at a time)
@@ -468,20 +472,20 @@ experts_kernel(ExpertArgs a) {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the products of the unit before
                     before = count_unit(f_before);
                 }
-                floatx4 sum[2][MT];
+                floatx4 sum[TILES][MT];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < TILES; ++t)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) sum[t][i] = add_up(t, i);
-                if constexpr (kSumRegions<MT> == 2) region ^= 1;
+                if constexpr (REGIONS == 2) region ^= 1;
                 else lds_barrier();
                 if (f_before >= 0) finish(f_before, before);
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < TILES; ++t)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        if (row[i] < 0 || 2 * at.f + t >= tiles) continue;
-                        const uint32_t off = (uint32_t)(((int64_t)row[i] * a.K + 32 * at.f + 16 * t + 4 * g) * 4);
+                        if (row[i] < 0 || TILES * at.f + t >= tiles) continue;
+                        const uint32_t off = (uint32_t)(((int64_t)row[i] * a.K + 16 * (TILES * at.f + t) + 4 * g) * 4);
                         __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(sum[t][i].x), __float_as_uint(sum[t][i].y), __float_as_uint(sum[t][i].z),
                                                                      __float_as_uint(sum[t][i].w)}, rsp, off, 0, kThrough);
                     }
@@ -512,29 +516,33 @@ experts_kernel(ExpertArgs a) {
                     request(pass);
                     regroup();
                 }
-                fetch(buf1, at, 1, pass, true);
-                __builtin_amdgcn_sched_barrier(0);
-                consume(buf0, 0, pass);
-                __builtin_amdgcn_sched_barrier(0);
-                if (pass + 1 < passes) fetch(buf0, at, 0, pass + 1, true);
-                else fetch(buf0, next, 0, 0, u + 1 < end);
-                __builtin_amdgcn_sched_barrier(0);
-                consume(buf1, 1, pass);
-                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < TILES; t += 2) {
+                    fetch(buf1, at, t + 1, pass, true);
+                    __builtin_amdgcn_sched_barrier(0);
+                    consume(buf0, t, pass);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (t + 2 < TILES) fetch(buf0, at, t + 2, pass, true);
+                    else if (pass + 1 < passes) fetch(buf0, at, 0, pass + 1, true);
+                    else fetch(buf0, next, 0, 0, u + 1 < end);
+                    __builtin_amdgcn_sched_barrier(0);
+                    consume(buf1, t + 1, pass);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             lds_barrier();
             // The waves take turns with the sums.  (They are written again two units later, behind the next barrier.)
             if constexpr (!DOWN) {
-                for (int item = 0; item < 2 * MT; ++item) {
-                    if ((int)((u * (2 * MT) + item) % (unsigned)waves) != wave) continue;
+                for (int item = 0; item < TILES * MT; ++item) {
+                    if ((int)((u * (TILES * MT) + item) % (unsigned)waves) != wave) continue;
                     const int t = item / MT, i = item - t * MT;
                     const floatx4 sum = add_up(t, i);
                     int to = row[0];
 #pragma unroll
                     for (int q = 1; q < MT; ++q) to = i == q ? row[q] : to;
-                    if (to < 0) continue;
+                    if (to < 0 || TILES * at.f + t >= tiles) continue;
                     const float h0 = activate(sum.x, a.act) * sum.y, h1 = activate(sum.z, a.act) * sum.w;
-                    const int f = 16 * at.f + 8 * t + 2 * g;
+                    const int f = 8 * (TILES * at.f + t) + 2 * g;
                     uint16_t *const dst = a.H + (int64_t)to * kTerms * a.ffn + f;
                     const uint32_t high = float2_to_half2_bits(h0, h1);
                     *reinterpret_cast<uint32_t *>(dst) = high;
@@ -546,7 +554,7 @@ experts_kernel(ExpertArgs a) {
                     }
                 }
             }
-            if constexpr (kSumRegions<MT> == 2) region ^= 1;
+            if constexpr (REGIONS == 2) region ^= 1;
             else lds_barrier();
             if (u + 1 < end && (next.r != at.r || next.chunk != at.chunk)) {
                 columns(next);
@@ -576,19 +584,19 @@ bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, 
            M * top_k * hidden * 4 + 4096 < limit;
 }
 
-template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN>
+template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN, int TILES>
 static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) {
-    auto kern = experts_kernel<KIND, MT, SPW, PASSES, POL, DOWN>;
+    auto kern = experts_kernel<KIND, MT, SPW, PASSES, POL, DOWN, TILES>;
     static std::atomic<bool> ready{false};
     if (!ready.load(std::memory_order_acquire)) {
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         ready.store(true, std::memory_order_release);
     }
     const int n = (int)(a.M * a.top_k);
-    const size_t lds = (size_t)waves * (kSumRegions<MT> * 2 * MT * 1024 + 2048 + 32) + choices_shared(a.experts, n) +
+    const size_t lds = (size_t)waves * (sum_regions(MT, TILES) * TILES * MT * 1024 + 2048 + 32) + choices_shared(a.experts, n) +
                        (DOWN ? 0 : choices_scratch(a.experts, n));
     if (lds > 160 * 1024) return kErrShape;
-    const int64_t units = choice_most(a.experts, n) * ((DOWN ? a.K / 16 + 1 : 2 * a.ffn / 16) / 2);
+    const int64_t tiles = (DOWN ? a.K : 2 * a.ffn) / 16, units = choice_most(a.experts, n) * ((tiles + TILES - 1) / TILES);
     // waves that a CU holds, by registers
     const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : (KIND == kE4M3Row ? 16 : 12)) : (PASSES ? 12 : 16));
     const int all = waves + (DOWN ? 1 : 0);
@@ -599,14 +607,19 @@ static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) 
 
 template <int KIND, int MT, int SPW, int POL, bool DOWN>
 static int launch_slices(ExpertArgs a, hipStream_t stream) {
-    const int64_t K = DOWN ? a.ffn : a.K;
+    const int64_t K = DOWN ? a.ffn : a.K, tiles = (DOWN ? a.K : 2 * a.ffn) / 16;
     const int slices = (int)((K + SPW * 64 - 1) / (SPW * 64));
     const int one_pass = MT == 1 ? (DOWN ? 8 : 16) : (DOWN ? 7 : 8);   // waves that stream, as the registers allow
     const int most = slices <= one_pass ? one_pass : (DOWN ? 7 : 8);
     a.passes = (slices + most - 1) / most;
     a.rotate = (K * kind_elem_bytes(KIND)) % 4096 == 0 ? 1 : 0;
     const int waves = (slices + a.passes - 1) / a.passes;
-    return a.passes > 1 ? launch_experts_t<KIND, MT, SPW, true, POL, DOWN>(a, waves, stream) : launch_experts_t<KIND, MT, SPW, false, POL, DOWN>(a, waves, stream);
+    if (a.passes == 1) return launch_experts_t<KIND, MT, SPW, false, POL, DOWN, 2>(a, waves, stream);
+    if constexpr (MT < 4) {
+        // (at least four units of four tiles for each of 256 workgroups, if the tokens' choices differ)
+        if (choice_most(a.experts, (int)(a.M * a.top_k)) * tiles >= 4 * 4 * 256) return launch_experts_t<KIND, MT, SPW, true, POL, DOWN, 4>(a, waves, stream);
+    }
+    return launch_experts_t<KIND, MT, SPW, true, POL, DOWN, 2>(a, waves, stream);
 }
 
 template <int KIND, int POL, bool DOWN>
