@@ -429,9 +429,10 @@ int launch_large_gemm(int kind, const GemmArgs &a, hipStream_t stream) {
     dim3 grid((unsigned)(p.tiles_m * p.tiles_n), (unsigned)c.split);
     p.epi = a.epi;
     if (kind < 0 || kind >= kNumKinds || kind_quantizes(kind)) return kErrArg;
-    if (a.epi.kind == kEpiNone || c.split > 1) launch_tiles_t<kEpiNone>(kind, p, c, grid, stream);
-    else if (a.epi.kind == kEpiFull) launch_tiles_full(kind, p, c, grid, stream);
-    else launch_tiles_gated(kind, p, c, grid, stream);
+    const bool staged = kind == kPlainF16 || kind_is_fp8(kind);
+    if (a.epi.kind == kEpiNone || c.split > 1) (staged ? launch_staged_t<kEpiNone> : launch_nested_t<kEpiNone>)(kind, p, c, grid, stream);
+    else if (a.epi.kind == kEpiFull) (staged ? launch_staged_full : launch_nested_full)(kind, p, c, grid, stream);
+    else (staged ? launch_staged_gated : launch_nested_gated)(kind, p, c, grid, stream);
     if (hipGetLastError() != hipSuccess) return kErrHip;
     if (c.split > 1)
         return launch_splitk_reduce(a.partials, c.split, a.M, a.N, kind_is_fp8(kind) ? a.scales : nullptr,

@@ -190,27 +190,42 @@ struct TileStore {
     static __device__ __forceinline__ void to_lds_epilogue(const LargeParams &p, AccT (&acc)[FNB][FMB], int m0, int n0, int row0, int wn,
                                                            int lane, uint8_t *lds) {
         const int r = lane % MB;
+        // (all that comes from memory is under way at a time: block by block, each waiting for its own, 8192 tokens of (4096, 4096) in FP8 mode took 28 us more
+        // for the residual)
         float s[F];
+        u32x2 add[FNB][NV][F];
+        floatx4 bias[FNB][NV];
 #pragma unroll
         for (int j = 0; j < F; ++j) {
             const int m = m0 + row0 + MB * j + r;
             s[j] = kind_is_fp8(KIND) ? (m < p.M ? p.scales[m] : 0.f) * p.w_scale : 1.0f;
+#pragma unroll
+            for (int i = 0; i < FNB; ++i)
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int n = n0 + wn * WTN + MB * i + acc_col(lane, v);
+                    add[i][v][j] = m < p.M && n < p.N ? residual4<EPI>(p.epi, m, n, p.N) : u32x2{0u, 0u};
+                }
         }
 #pragma unroll
         for (int i = 0; i < FNB; ++i)
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int col = wn * WTN + MB * i + acc_col(lane, v), n = n0 + col;
-                __builtin_amdgcn_sched_barrier(0);     // (loads of one block of rows at a time: of all, they spill registers)
-                if (n >= p.N) continue;
-                const floatx4 bias = bias4(p.epi, n, p.N);
+                const int n = n0 + wn * WTN + MB * i + acc_col(lane, v);
+                bias[i][v] = n < p.N ? bias4(p.epi, n, p.N) : floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+        for (int i = 0; i < FNB; ++i)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int col = wn * WTN + MB * i + acc_col(lane, v);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
                     const int row = row0 + MB * j + r;
-                    if (m0 + row >= p.M) continue;
                     const floatx4 y = epilogue4<EPI>(floatx4{scaled(acc[i][j][4 * v], s[j]), scaled(acc[i][j][4 * v + 1], s[j]),
                                                              scaled(acc[i][j][4 * v + 2], s[j]), scaled(acc[i][j][4 * v + 3], s[j])},
-                                                     bias, p.epi, m0 + row, n, p.N);
+                                                     bias[i][v], add[i][v][j], p.epi.act);
                     uint8_t *const to = lds + row * (TNO * 2);
                     if constexpr (EPI == kEpiGated) {
                         *reinterpret_cast<uint32_t *>(to + (((col >> 4) ^ (row & (OCH - 1))) << 4) + 4 * ((col >> 2) & 3)) = float2_to_half2_bits(y.x, y.y);
@@ -1722,21 +1737,23 @@ static void launch_nested(const LargeParams &p, const LargeConfig &c, dim3 grid,
     }
 }
 
-// The kernels of one epilogue; each is instantiated in a source of its own (they take the compiler a minute each).
+// The kernels of one epilogue: weights through LDS, weights through registers.  With an epilogue, each of the two is instantiated in a source of
+// its own (they take the compiler a minute each).
 template <int EPI>
-static void launch_tiles_t(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
-    switch (kind) {
-        case kPlainF16: launch_large_k<EPI, kPlainF16>(p, c, grid, stream); break;
-        case kNestedF16: launch_nested<EPI, kNestedF16>(p, c, grid, stream); break;
-        case kNestedF16Row: launch_nested<EPI, kNestedF16Row>(p, c, grid, stream); break;
-        case kPlainF16Packed:
-            if constexpr (EPI == kEpiNone) launch_nested<EPI, kPlainF16Packed>(p, c, grid, stream);      // (a baseline: no layer has it)
-            break;
-        case kE4M3: launch_large_k<EPI, kE4M3>(p, c, grid, stream); break;
-        default: launch_large_k<EPI, kE4M3Row>(p, c, grid, stream); break;
-    }
+static void launch_staged_t(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+    if (kind == kPlainF16) launch_large_k<EPI, kPlainF16>(p, c, grid, stream);
+    else if (kind == kE4M3) launch_large_k<EPI, kE4M3>(p, c, grid, stream);
+    else launch_large_k<EPI, kE4M3Row>(p, c, grid, stream);
 }
-void launch_tiles_full(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
-void launch_tiles_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+template <int EPI>
+static void launch_nested_t(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+    if (kind == kNestedF16) launch_nested<EPI, kNestedF16>(p, c, grid, stream);
+    else if (kind == kNestedF16Row) launch_nested<EPI, kNestedF16Row>(p, c, grid, stream);
+    else if constexpr (EPI == kEpiNone) launch_nested<EPI, kPlainF16Packed>(p, c, grid, stream);       // (a baseline: no layer has it)
+}
+void launch_staged_full(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_staged_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_nested_full(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_nested_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
 
 }  // namespace nfp

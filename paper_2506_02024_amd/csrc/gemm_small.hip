@@ -18,6 +18,13 @@ splitk_reduce_kernel(const float *__restrict__ partials, int S, int M, int N, in
     const int64_t idx = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (idx >= total) return;
     const int m = (int)(idx / ldp), n = (int)(idx - (int64_t)m * ldp);
+    // (what is added to the sums is under way while they are loaded)
+    floatx4 bias = {0.f, 0.f, 0.f, 0.f};
+    u32x2 add = {0u, 0u};
+    if constexpr (EPI != kEpiNone) {
+        bias = bias4(epi, n, N);
+        add = residual4<EPI>(epi, m, n, N);
+    }
     floatx4 v = *reinterpret_cast<const floatx4 *>(partials + idx);
     for (int s = 1; s < S; ++s) {
         const floatx4 u = *reinterpret_cast<const floatx4 *>(partials + (int64_t)s * total + idx);
@@ -27,7 +34,7 @@ splitk_reduce_kernel(const float *__restrict__ partials, int S, int M, int N, in
         const float sc = scales[m] * w_scale;
         v.x = scale_f32(v.x, sc); v.y = scale_f32(v.y, sc); v.z = scale_f32(v.z, sc); v.w = scale_f32(v.w, sc);
     }
-    if constexpr (EPI != kEpiNone) v = epilogue4<EPI>(v, bias4(epi, n, N), epi, m, n, N);
+    if constexpr (EPI != kEpiNone) v = epilogue4<EPI>(v, bias, add, epi.act);
     if constexpr (EPI == kEpiGated) {
         uint16_t *to = Y + (int64_t)m * ldy + (n >> 1);
         const uint32_t o = float2_to_half2_bits(v.x, v.y);

@@ -429,7 +429,7 @@ small_gemm_kernel(SmallParams p) {
             float sc = (kind_quantizes(KIND) ? row_scale[m] : p.scales[m]) * p.w_scale;
             sum.x = scale_f32(sum.x, sc); sum.y = scale_f32(sum.y, sc); sum.z = scale_f32(sum.z, sc); sum.w = scale_f32(sum.w, sc);
         }
-        if constexpr (EPI != kEpiNone) sum = epilogue4<EPI>(sum, bias4(p.epi, n, p.N), p.epi, m, n, p.N);
+        if constexpr (EPI != kEpiNone) sum = epilogue4<EPI>(sum, bias4(p.epi, n, p.N), residual4<EPI>(p.epi, m, n, p.N), p.epi.act);
         if constexpr (EPI == kEpiGated) {
             uint16_t *to = p.Y + (int64_t)m * p.ldy + (n >> 1);
             const uint32_t o = float2_to_half2_bits(sum.x, sum.y);

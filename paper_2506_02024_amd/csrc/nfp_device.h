@@ -251,33 +251,41 @@ __device__ __forceinline__ floatx4 four_halves(const uint16_t *src, bool vec, in
     return v;
 }
 
-// The epilogue on the sums of token m and weight rows n .. n + 3 (n a multiple of 4); `bias` are those rows' biases.  The outputs: four, or two gated
-// ones, columns n / 2 and n / 2 + 1, in the first two.
+// What is added to the outputs of token m and weight rows n .. n + 3 (n a multiple of 4), as halves: four, or two of gated ones.  It is loaded ahead of the
+// sums that it is added to.
 template <int EPI>
-__device__ __forceinline__ floatx4 epilogue4(floatx4 z, const floatx4 &bias, const Epilogue &e, int m, int n, int N) {
-    z.x += bias.x;  z.y += bias.y;  z.z += bias.z;  z.w += bias.w;
+__device__ __forceinline__ u32x2 residual4(const Epilogue &e, int64_t m, int n, int N) {
+    u32x2 r = {0u, 0u};
+    if (!e.residual) return r;
+    const uint16_t *src = e.residual + m * e.ldr + (EPI == kEpiGated ? n >> 1 : n);
+    const int count = EPI == kEpiGated ? (N - n) >> 1 : N - n;
     if constexpr (EPI == kEpiGated) {
-        floatx4 y = {activate(z.x, e.act) * z.y, activate(z.z, e.act) * z.w, 0.f, 0.f};
-        if (e.residual) {
-            const uint16_t *r = e.residual + (int64_t)m * e.ldr + (n >> 1);
-            if (e.vec) {
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(r);
-                y.x += half_bits_to_float(w & 0xffffu);
-                y.y += half_bits_to_float(w >> 16);
-            } else {
-                y.x += half_bits_to_float(r[0]);
-                if (n + 2 < N) y.y += half_bits_to_float(r[1]);
-            }
-        }
-        return y;
+        if (e.vec) r.x = *reinterpret_cast<const uint32_t *>(src);
+        else r.x = src[0] | (count > 1 ? (uint32_t)src[1] << 16 : 0u);
     } else {
-        floatx4 y = {activate(z.x, e.act), activate(z.y, e.act), activate(z.z, e.act), activate(z.w, e.act)};
-        if (e.residual) {
-            const floatx4 r = four_halves(e.residual + (int64_t)m * e.ldr + n, e.vec, N - n);
-            y.x += r.x;  y.y += r.y;  y.z += r.z;  y.w += r.w;
+        if (e.vec) r = *reinterpret_cast<const u32x2 *>(src);
+        else {
+            r.x = src[0] | (count > 1 ? (uint32_t)src[1] << 16 : 0u);
+            r.y = (count > 2 ? src[2] : 0u) | (count > 3 ? (uint32_t)src[3] << 16 : 0u);
         }
-        return y;
     }
+    return r;
+}
+
+// The epilogue on the sums of four weight rows; `bias` are those rows' biases.  The outputs: four, or two gated ones in the first two.
+template <int EPI>
+__device__ __forceinline__ floatx4 epilogue4(floatx4 z, const floatx4 &bias, const u32x2 &r, int act) {
+    z.x += bias.x;  z.y += bias.y;  z.z += bias.z;  z.w += bias.w;
+    floatx4 y;
+    if constexpr (EPI == kEpiGated) y = floatx4{activate(z.x, act) * z.y, activate(z.z, act) * z.w, 0.f, 0.f};
+    else y = floatx4{activate(z.x, act), activate(z.y, act), activate(z.z, act), activate(z.w, act)};
+    y.x += half_bits_to_float(r.x & 0xffffu);
+    y.y += half_bits_to_float(r.x >> 16);
+    if constexpr (EPI != kEpiGated) {
+        y.z += half_bits_to_float(r.y & 0xffffu);
+        y.w += half_bits_to_float(r.y >> 16);
+    }
+    return y;
 }
 __device__ __forceinline__ floatx4 bias4(const Epilogue &e, int n, int N) {
     return e.bias ? four_halves(e.bias + n, e.vec, N - n) : floatx4{0.f, 0.f, 0.f, 0.f};

@@ -171,3 +171,46 @@ def test_graph_of_router_and_experts(nfp):
                 dy = dy + dh @ shared_down.double().abs().t().contiguous() + (h - h.half().double()).abs() @ shared_down.double().abs().t().contiguous()
                 ref, tol = ff.moe_ref(x, gate_up, down, got[0], got[1], False, 2, y.half())
                 ff.assert_within(got[2], ref, tol + dy + (y - y.half().double()).abs())
+
+
+@pytest.mark.parametrize("M,E,H,F,top_k", [(3, 2, 160, 2064, 1), (16, 6, 1040, 4112, 2), (20, 2, 96, 2304, 2), (64, 3, 112, 1120, 2), (64, 2, 48, 528, 2)])
+def test_long_products(nfp, M, E, H, F, top_k):
+    """Down products whose rows take one pass and several, for every number of token tiles, an odd number of row tiles among them."""
+    for mode, exception in ((0, False), (1, False), (0, True)):
+        x, gate_up, down, ids, weights, r = make(M, E, H, F, top_k, seed=F, exception=exception)
+        y = nfp.moe(x, nfp.Experts(gate_up, down), ids, weights, mode, residual=r)
+        ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, mode == 1, 2, r)
+        ff.assert_within(y, ref, tol, str((mode, exception)))
+
+
+@pytest.mark.parametrize("M,E,H,F,top_k", [(8, 48, 1552, 2064, 6), (20, 8, 8208, 2064, 4), (16, 32, 4112, 1024, 4)])
+def test_units_of_four_tiles(nfp, M, E, H, F, top_k):
+    """Enough units in several passes: down products of many experts and of long outputs, up products of rows of 4112."""
+    for mode in (0, 1):
+        x, gate_up, down, ids, weights, _ = make(M, E, H, F, top_k, seed=H)
+        y = nfp.moe(x, nfp.Experts(gate_up, down), ids, weights, mode)
+        for rows in (slice(0, 1), slice(M - 1, M)):
+            ref, tol = ff.moe_ref(x[rows], gate_up, down, ids[rows], weights[rows], mode == 1, 2)
+            ff.assert_within(y[rows], ref, tol, str(mode))
+
+
+def test_workspace_for_many_calls(nfp):
+    """One workspace for calls of different shapes and for linears, one after the other: every call leaves the counters cleared."""
+    calls = []
+    for M, E, H, F, k in ((1, 8, 512, 64, 2), (16, 12, 1040, 128, 4), (40, 6, 272, 80, 2), (3, 2, 64, 2064, 1)):
+        x, gate_up, down, ids, weights, r = make(M, E, H, F, k, seed=M)
+        experts = nfp.Experts(gate_up, down)
+        calls.append((x, experts, ids, weights, r, nfp.moe(x, experts, ids, weights, 0, residual=r)))
+    layer, router = nfp.Layer(ff.normal(ff.generator(1), 512, 4096, sigma=0.02)), ff.normal(ff.generator(2), 40, 4096, sigma=0.02)
+    z = ff.normal(ff.generator(3), 5, 4096)
+    need = max([nfp.moe_workspace_size(c[0].shape[0], c[1], c[2].shape[1]) for c in calls] + [nfp.linear_fused_workspace_size(5, layer, 0),
+                                                                                              nfp.moe_route_workspace_size(5, 40, 4096)])
+    ws = nfp.new_workspace(need, "cuda:0")
+    want, chosen = nfp.linear_fused(z, layer, 0, activation=nfp.ACT_GELU), nfp.moe_route(z, router, 3)
+    for _ in range(3):
+        for x, experts, ids, weights, r, y in calls:
+            assert torch.equal(nfp.moe(x, experts, ids, weights, 0, residual=r, workspace=ws), y)
+            assert torch.equal(nfp.linear_fused(z, layer, 0, activation=nfp.ACT_GELU, workspace=ws), want)
+            assert all(torch.equal(a, b) for a, b in zip(nfp.moe_route(z, router, 3, workspace=ws), chosen))
+            torch.cuda.synchronize()
+            assert (ws[:nfp.WORKSPACE_COUNTER_BYTES] == 0).all()
