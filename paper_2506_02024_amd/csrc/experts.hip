@@ -598,7 +598,7 @@ static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) 
     if (lds > 160 * 1024) return kErrShape;
     const int64_t tiles = (DOWN ? a.K : 2 * a.ffn) / 16, units = choice_most(a.experts, n) * ((tiles + TILES - 1) / TILES);
     // waves that a CU holds, by registers
-    const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : (KIND == kE4M3Row ? 16 : 12)) : (PASSES ? 12 : 16));
+    const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : 12) : (PASSES ? 12 : 16));
     const int all = waves + (DOWN ? 1 : 0);
     const int per_cu = std::max(1, std::min(held / all, (int)(160 * 1024 / lds)));
     kern<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(units, 256 * per_cu)), (unsigned)all * 64, lds, stream>>>(a);
