@@ -17,7 +17,8 @@ namespace nfp {
 constexpr int kTerms = 2;
 
 // E4M3 bytes as FP16 words: sign, four bits of exponent and three of mantissa at the same places below FP16's exponent MSB read as the value times
-// 2^-8 (subnormals too), which is the weight that the upper plane stands for (Sec. 4.1).
+// 2^-8 (subnormals too), which is the weight that the upper plane stands for (Sec. 4.1).  (The conversion instruction, two bytes at a time and then a
+// place for each word: up products 90.8 us for 91.5, down products 67.4 for 61.7 with 16 tokens and 64 experts of 1408.)
 __device__ __forceinline__ uint32_t expand2(uint32_t u, uint32_t sel) {
     const uint32_t x = byte_perm(0u, u, sel);          // the bytes in the upper halves of the words
     return (x & 0x80008000u) | ((x >> 1) & 0x3f803f80u);
@@ -262,8 +263,6 @@ experts_kernel(ExpertArgs a) {
     const uint32_t row_bytes = (uint32_t)K * EB;
     const int64_t expert_bytes = tiles * 16 * (int64_t)row_bytes;
     const uint8_t *const w0 = DOWN ? a.down0 : a.up0, *const w1 = DOWN ? a.down1 : a.up1;
-    // (rows of a multiple of 4 KB put the 16 rows of a slice on the same memory channels: the slices are rotated from workgroup to workgroup)
-    const int ks = a.rotate ? (int)((wave + (blockIdx.x >> 3) * 5u) % (unsigned)waves) : wave;
     const Regroup<true> rx(shared, own, lane);
     const Regroup<KIND == kPlainF16> rw(shared, own, lane);
     u32x4 xa[SPW][MT][TERMS], xb[SPW][MT][TERMS];
@@ -273,7 +272,7 @@ experts_kernel(ExpertArgs a) {
     const __amdgpu_buffer_rsrc_t rsx = DOWN ? weight_rsrc(reinterpret_cast<const uint8_t *>(a.H), (uint32_t)n * x_row)
                                             : weight_rsrc(reinterpret_cast<const uint8_t *>(a.X), (uint32_t)(((a.M - 1) * a.ldx + a.K) * 2));
     auto x_at = [&](int which, int l) { return which >= 0 ? (uint32_t)which * x_row + (l & 7) * 16u : kDead; };
-    auto k_of = [&](int pass) { return (pass * waves + ks) * (SPW * KSTEP); };
+    auto k_of = [&](int pass) { return (pass * waves + wave) * (SPW * KSTEP); };
     auto request = [&](int pass) {
         const int k0 = k_of(pass);
 #pragma unroll
@@ -370,7 +369,7 @@ experts_kernel(ExpertArgs a) {
     };
     int region = 0;
     auto consume = [&](WItem (&w)[SPW], int tile, int pass) {
-        floatx4 *const slot = slots + ((region * TILES + tile) * waves + ks) * MT * 64 + lane;
+        floatx4 *const slot = slots + ((region * TILES + tile) * waves + wave) * MT * 64 + lane;
         floatx4 sum[MT];
         regroup_pieces<KIND, SPW>(w, rw);
 #pragma unroll
@@ -612,7 +611,6 @@ static int launch_slices(ExpertArgs a, hipStream_t stream) {
     const int one_pass = MT == 1 ? (DOWN ? 8 : 16) : (DOWN ? 7 : 8);   // waves that stream, as the registers allow
     const int most = slices <= one_pass ? one_pass : (DOWN ? 7 : 8);
     a.passes = (slices + most - 1) / most;
-    a.rotate = (K * kind_elem_bytes(KIND)) % 4096 == 0 ? 1 : 0;
     const int waves = (slices + a.passes - 1) / a.passes;
     if (a.passes == 1) return launch_experts_t<KIND, MT, SPW, false, POL, DOWN, 2>(a, waves, stream);
     if constexpr (MT < 4) {

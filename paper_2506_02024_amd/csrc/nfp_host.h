@@ -298,7 +298,7 @@ struct ExpertArgs {
     uint32_t *counters;                                // one per 32 output rows, zero between calls
     int32_t experts, top_k, act;
     int32_t vec;                                       // 1: residuals are loaded four at a time, 2: outputs are stored so
-    int32_t passes, rotate, gather;
+    int32_t passes, gather;
 };
 size_t experts_workspace_bytes(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);      // behind the counters
 bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);
