@@ -1,8 +1,9 @@
 // The router of a mixture of experts: logits, scores, the chosen experts and their weights.
 //
 // Which experts are the largest must not depend on the order of a sum, so the logits are worked out in binary64: products of FP16 values are exact
-// there, and v_mfma_f64_16x16x4 adds them up.  That is also what bounds the kernel on large batches (the matrix pipe's 64-bit rate, 1 / 32 of
-// the FP16 one); small ones are bound by a chain of latencies.
+// there, and v_mfma_f64_16x16x4 adds them up.  Small batches are bound by a chain of latencies, larger ones by the matrix pipe's 64-bit
+// rate, 1 / 32 of the FP16 one; where there are many logits, they are worked out in binary32 first, and again only those that may be among the
+// largest.
 #include <algorithm>
 #include <type_traits>
 
@@ -11,7 +12,15 @@
 namespace nfp {
 
 typedef double doublex4 __attribute__((ext_vector_type(4)));
-constexpr int kRouteWaves = 8, kMostSlices = 8;
+constexpr int kRouteWaves = 8, kMostSlices = 8, kMostTop = 32;
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+
+// Tokens of a launch: as many tiles as there are counters, and 32 MiB of logits (of 256 experts 16384 tokens, whose products take 0.4 ms).
+static __host__ __device__ int64_t route_tokens(int64_t M, int64_t experts) {
+    const int64_t most = min((int64_t)16 * kMaxCounters, (((int64_t)1 << 22) / experts) & ~(int64_t)31);
+    return min(M, most);
+}
 
 // Orders doubles as unsigned numbers: larger numbers above smaller ones, NaN below all, zero below NaN (for what has been taken or lies outside).
 __device__ __forceinline__ uint64_t sortable(double x) {
@@ -249,11 +258,276 @@ route_kernel(RouteArgs a) {
     }
 }
 
-// Tokens of a launch: as many tiles as there are counters, and 32 MiB of logits (of 256 experts 16384 tokens, whose products take 0.4 ms).
-static int64_t route_tokens(int64_t M, int64_t experts) {
-    const int64_t most = std::min<int64_t>(16 * kMaxCounters, (((int64_t)1 << 22) / experts) & ~(int64_t)31);
-    return std::min(M, most);
+// ---- many logits --------------------------------------------------------------------------------------
+// Two launches: all logits with FP16 matrix instructions and what they may be off by; then, token by token, the experts that may be among the top_k largest by that, their logits
+// again in binary64, and the choice among these.  Where choices differ by more than the sums' error, as nearly always, that is top_k logits of a token, or one more.
+//
+// A sum of n terms whose every addition loses at most a step of the largest magnitude met is off by n 2^-23 sum |x r| <= n 2^-23 |x| |r|; taken twice.  A wave adds up an eighth
+// of the columns, and the eight sums are added up.
+constexpr int kNear = 64;                              // tokens and experts of a workgroup
+__device__ __forceinline__ float near_error(int64_t K) {
+    return 2.0f * (float)((K + 64 * kRouteWaves - 1) / (64 * kRouteWaves) * 64 + kRouteWaves) * 0x1p-23f * 1.01f;         // (1 %: the norms' own rounding)
 }
+static __host__ __device__ __forceinline__ int near_stride(int experts) { return (experts + 3) & ~3; }
+
+__global__ void __launch_bounds__(64 * kRouteWaves)
+route_near_kernel(RouteArgs a) {
+    constexpr int T = kNear / 16;
+    __shared__ floatx4 parts[kRouteWaves][T][64];
+    __shared__ float norms[kRouteWaves][2 * kNear];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r16 = lane & 15;
+    const int tokens = (int)min(route_tokens(a.M, a.experts), a.M - a.token0), m0 = blockIdx.y * kNear, e0 = blockIdx.x * kNear;
+    // (rows behind the last one and columns behind the last one read as zero)
+    auto from = [&](const uint16_t *first, int64_t ld, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(first), 0, (uint32_t)(((int64_t)(rows - 1) * ld + a.K) * 2), 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t rsr = from(a.R + (int64_t)e0 * a.ldr, a.ldr, min(kNear, a.experts - e0));
+    const __amdgpu_buffer_rsrc_t rsx = from(a.X + (a.token0 + m0) * a.ldx, a.ldx, min(kNear, tokens - m0));
+    const uint32_t row_r = (uint32_t)(2 * a.ldr), row_x = (uint32_t)(2 * a.ldx), at_r = r16 * row_r + 16 * g, at_x = r16 * row_x + 16 * g;
+    floatx4 acc[T][T];
+    float rr[T], xx[T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        rr[i] = xx[i] = 0.0f;
+#pragma unroll
+        for (int q = 0; q < T; ++q) acc[i][q] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Step { u32x4 w[T], x[T]; };                 // 32 columns
+    auto load = [&](Step &v, int k0) {
+        const bool in = k0 + 8 * g < a.K;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            v.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rsr, in ? at_r + 16 * t * row_r + 2 * k0 : 0xfffffff0u, 0, 0);
+            v.x[t] = __builtin_amdgcn_raw_buffer_load_b128(rsx, in ? at_x + 16 * t * row_x + 2 * k0 : 0xfffffff0u, 0, 0);
+        }
+    };
+    auto square = [](const u32x4 &v, float s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, v[i]), __builtin_bit_cast(half2v, v[i]), s, false);
+        return s;
+    };
+    auto multiply = [&](const Step &v) {
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int q = 0; q < T; ++q)
+                acc[i][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, v.w[i]), __builtin_bit_cast(half8v, v.x[q]), acc[i][q], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            rr[i] = square(v.w[i], rr[i]);
+            xx[i] = square(v.x[i], xx[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // a wave takes 64 columns at a time, whole lines of 128 bytes; two steps of 32 are under way while two are multiplied
+    constexpr int STRIDE = 64 * kRouteWaves;
+    Step v[4];
+    const int K = (int)a.K;
+    int k0 = 64 * wave;
+    load(v[0], k0);
+    load(v[1], k0 + 32);
+    for (; k0 < K; k0 += 2 * STRIDE) {
+        load(v[2], k0 + STRIDE);
+        load(v[3], k0 + STRIDE + 32);
+        multiply(v[0]);
+        multiply(v[1]);
+        load(v[0], k0 + 2 * STRIDE);
+        load(v[1], k0 + 2 * STRIDE + 32);
+        multiply(v[2]);
+        multiply(v[3]);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        rr[t] += __shfl_xor(rr[t], 16);
+        rr[t] += __shfl_xor(rr[t], 32);
+        xx[t] += __shfl_xor(xx[t], 16);
+        xx[t] += __shfl_xor(xx[t], 32);
+        if (g == 0) {
+            norms[wave][16 * t + r16] = rr[t];
+            norms[wave][kNear + 16 * t + r16] = xx[t];
+        }
+    }
+    float *const logits = reinterpret_cast<float *>(a.logits), *const errors = logits + (int64_t)tokens * near_stride(a.experts);
+    // the waves' sums, 16 experts at a time; rows of a block: expert 4 g + v of lane group g, column: token r16
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        if (i > 0) __syncthreads();
+#pragma unroll
+        for (int q = 0; q < T; ++q) parts[wave][q][lane] = acc[i][q];
+        __syncthreads();
+        if (threadIdx.x < 64 * T) {
+            const int q = threadIdx.x >> 6, e = e0 + 16 * i + 4 * g, m = m0 + 16 * q + r16;
+            floatx4 sum = parts[0][q][lane];
+#pragma unroll
+            for (int w = 1; w < kRouteWaves; ++w) sum += parts[w][q][lane];
+            if (m < tokens && e < a.experts) *reinterpret_cast<floatx4 *>(logits + (int64_t)m * near_stride(a.experts) + e) = sum;
+        }
+    }
+    if (wave == 0) {
+        float r = 0.0f, x = 0.0f;
+        for (int w = 0; w < kRouteWaves; ++w) {
+            r += norms[w][lane];
+            x += norms[w][kNear + lane];
+        }
+        r = __uint_as_float(max_of_wave(__float_as_uint(r) & 0x7fffffffu));        // (of a NaN among them: a NaN)
+        if (m0 + lane < tokens) errors[(int64_t)(m0 + lane) * gridDim.x + blockIdx.x] = near_error(a.K) * sqrtf(r) * sqrtf(x);
+    }
+}
+
+// A wave for each token.
+constexpr int kChoosers = 4;
+template <int VALUES>
+__global__ void __launch_bounds__(64 * kChoosers)
+route_near_choose_kernel(RouteArgs a) {
+    __shared__ uint16_t named[kChoosers][64 * VALUES];
+    __shared__ double exact[kChoosers][64 * VALUES];
+    __shared__ uint64_t keys[kChoosers][64 * VALUES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = (a.experts + kNear - 1) / kNear;
+    const int tokens = (int)min(route_tokens(a.M, a.experts), a.M - a.token0);
+    const int m = blockIdx.x * kChoosers + wave;
+    if (m >= tokens) return;
+    auto ordered = [] { asm volatile("" ::: "memory"); };              // (a wave's LDS accesses stay in order)
+    const float *const logits = reinterpret_cast<const float *>(a.logits), *const errors = logits + (int64_t)tokens * near_stride(a.experts);
+    const float error = __uint_as_float(max_of_wave(lane < tiles ? __float_as_uint(errors[(int64_t)m * tiles + lane]) & 0x7fffffffu : 0u));
+    const bool sure = error < __builtin_inff();
+    // Every expert's choice lies between `least` and `upper`; whose upper bound lies below the top_k-th largest lower bound is not among the top_k.
+    uint32_t least[VALUES];
+    float upper[VALUES];
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        const int e = lane + 64 * v;
+        least[v] = 0;
+        upper[v] = 0.0f;
+        if (e >= a.experts) continue;
+        float c = logits[(int64_t)m * near_stride(a.experts) + e], off = error;
+        if (a.bias) {                                  // (sigmoid: a slope of 1/4 at most; eight roundings)
+            c = 1.0f / (1.0f + __expf(-c)) + a.bias[e];
+            off = __builtin_isinf(c) ? 0.0f : 0.25f * error + 0x1p-20f + 0x1p-22f * fabsf(c);
+        }
+        const float low = sure && c == c ? c - off : -__builtin_inff();
+        upper[v] = !sure ? __builtin_inff() : (c == c ? c + off : -__builtin_inff());
+        const uint32_t b = __float_as_uint(low);
+        least[v] = b ^ ((b >> 31) != 0 ? ~0u : 1u << 31);
+    }
+    uint32_t left = (uint32_t)a.top_k, border = 0, rest[VALUES];
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) rest[v] = least[v];
+    while (left > 0) {                                 // (top_k is no more than the experts: there is one left)
+        uint32_t best = rest[0];
+#pragma unroll
+        for (int v = 1; v < VALUES; ++v) best = max(best, rest[v]);
+        border = max_of_wave(best);
+        bool gone = false;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            const bool it = !gone && rest[v] == border;
+            gone |= it;
+            rest[v] = it ? 0u : rest[v];
+        }
+        left -= min(left, (uint32_t)__popcll(__ballot(gone)));
+    }
+    const float floor_value = __uint_as_float(border ^ ((border >> 31) != 0 ? 1u << 31 : ~0u));
+    int count = 0;
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        const bool in = lane + 64 * v < a.experts && !(upper[v] < floor_value);
+        const uint64_t mask = __ballot(in);
+        if (in) named[wave][count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = (uint16_t)(lane + 64 * v);
+        count += __popcll(mask);
+    }
+    ordered();
+    // their logits: products of FP16 values, exact in binary32, added up in binary64
+    const uint16_t *const x = a.X + (a.token0 + m) * a.ldx;
+    auto dots = [&](auto width, int at) {
+        constexpr int W = decltype(width)::value;
+        const uint16_t *row[W];
+        double sum[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            row[i] = a.R + (int64_t)__builtin_amdgcn_readfirstlane(named[wave][at + i]) * a.ldr;
+            sum[i] = 0.0;
+        }
+        for (int64_t k = 8 * lane; k < a.K; k += 512) {
+            const u32x4 xv = *reinterpret_cast<const u32x4 *>(x + k);
+            u32x4 wv[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) wv[i] = *reinterpret_cast<const u32x4 *>(row[i] + k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xj = half_bits_to_float((xv[j >> 1] >> (16 * (j & 1))) & 0xffffu);
+#pragma unroll
+                for (int i = 0; i < W; ++i) sum[i] += (double)(xj * half_bits_to_float((wv[i][j >> 1] >> (16 * (j & 1))) & 0xffffu));
+            }
+        }
+        // (lanes that differ in the lowest bits take over one sum each)
+        int mine = 0;
+        if constexpr (W == 4) {
+            const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
+            const double s0 = (b0 ? sum[1] : sum[0]) + __shfl_xor(b0 ? sum[0] : sum[1], 1);
+            const double s1 = (b0 ? sum[3] : sum[2]) + __shfl_xor(b0 ? sum[2] : sum[3], 1);
+            sum[0] = (b1 ? s1 : s0) + __shfl_xor(b1 ? s0 : s1, 2);
+            mine = lane & 3;
+        } else {
+            sum[0] += __shfl_xor(sum[0], 1);
+            sum[0] += __shfl_xor(sum[0], 2);
+        }
+#pragma unroll
+        for (int d = 4; d < 64; d <<= 1) sum[0] += __shfl_xor(sum[0], d);
+        if (lane < W) exact[wave][at + mine] = sum[0];
+    };
+    int at = 0;
+    for (; at + 4 <= count; at += 4) dots(std::integral_constant<int, 4>{}, at);
+    for (; at < count; ++at) dots(std::integral_constant<int, 1>{}, at);
+    ordered();
+    auto sigmoid = [](double l) { return 1.0 / (1.0 + exp(-l)); };
+    double most = 0.0;
+    uint32_t strange = 0;
+    uint64_t high = 0;
+    for (int i = lane; i < count; i += 64) {
+        const double l = exact[wave][i];
+        strange |= l != l ? 1u : 0u;
+        const uint64_t key = a.bias ? sortable(sigmoid(l) + (double)a.bias[named[wave][i]]) : sortable(l);
+        keys[wave][i] = key;
+        high = max(high, key);
+    }
+    ordered();
+    if (!a.sigmoid) {
+        const uint32_t up = max_of_wave((uint32_t)(high >> 32)), low = max_of_wave((uint32_t)(high >> 32) == up ? (uint32_t)high : 0u);
+        most = max_of_wave(strange) ? __longlong_as_double(0x7ff8000000000000ll) : unsorted(((uint64_t)up << 32) | low);
+    }
+    // the place of each: how many are larger, or as large and before it
+    double score[VALUES], all = 0.0;
+    int place[VALUES];
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        const int i = lane + 64 * v;
+        place[v] = kMostTop;
+        score[v] = 0.0;
+        if (64 * v >= count) continue;
+        if (i < count) {
+            const uint64_t key = keys[wave][i];
+            int before = 0;
+            for (int q = 0; q < count; ++q) {
+                const uint64_t other = keys[wave][q];
+                before += other > key || (other == key && q < i) ? 1 : 0;
+            }
+            if (before < a.top_k) {
+                place[v] = before;
+                score[v] = a.sigmoid ? sigmoid(exact[wave][i]) : exp(exact[wave][i] - most);
+                all += score[v];
+            }
+        }
+    }
+    if (a.renormalize) all = sum_of_group<64>(all);
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) {
+        if (place[v] >= a.top_k) continue;
+        const int64_t to = (a.token0 + m) * a.top_k + place[v];
+        a.ids[to] = named[wave][lane + 64 * v];
+        a.weights[to] = (float)((a.renormalize ? score[v] / all : score[v]) * (double)a.factor);
+    }
+}
+
 static bool route_pairs(int64_t M, int64_t experts) { return ((M + 31) / 32) * ((experts + 31) / 32) >= 512; }       // two workgroups per CU
 // Slices of K: enough workgroups for the chip, at least a step of every wave's each.
 static int route_slices(int64_t M, int64_t experts, int64_t K) {
@@ -274,6 +548,19 @@ static void launch_route_t(const RouteArgs &a, int64_t tokens, hipStream_t strea
     else route_kernel<GROUP < 32 ? 32 : GROUP, GROUP < 64 ? 16 : 8, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
 }
 
+// Where a choice depends on one logit each, and there are many.
+static bool route_near(const RouteArgs &a, int64_t tokens) {
+    return (a.sigmoid || (a.renormalize && !a.bias)) && a.experts >= 16 && tokens * a.experts >= ((int64_t)1 << 17);
+}
+static void launch_near(const RouteArgs &a, int64_t tokens, hipStream_t stream) {
+    route_near_kernel<<<dim3((unsigned)((a.experts + kNear - 1) / kNear), (unsigned)((tokens + kNear - 1) / kNear)), 64 * kRouteWaves, 0, stream>>>(a);
+    const unsigned groups = (unsigned)((tokens + kChoosers - 1) / kChoosers);
+    if (a.experts <= 64) route_near_choose_kernel<1><<<groups, 64 * kChoosers, 0, stream>>>(a);
+    else if (a.experts <= 128) route_near_choose_kernel<2><<<groups, 64 * kChoosers, 0, stream>>>(a);
+    else if (a.experts <= 256) route_near_choose_kernel<4><<<groups, 64 * kChoosers, 0, stream>>>(a);
+    else route_near_choose_kernel<8><<<groups, 64 * kChoosers, 0, stream>>>(a);
+}
+
 int launch_route(RouteArgs a, hipStream_t stream) {
     const int64_t tokens = route_tokens(a.M, a.experts);
     a.slices = route_slices(tokens, a.experts, a.K);
@@ -281,7 +568,8 @@ int launch_route(RouteArgs a, hipStream_t stream) {
         a.token0 = m;
         const int64_t some = std::min(tokens, a.M - m);
         // (a token per wave, two or four: as many waves as a tile has)
-        if (a.slices == 1 && route_pairs(some, a.experts)) launch_route_t<2, 16>(a, some, stream);
+        if (route_near(a, some)) launch_near(a, some, stream);
+        else if (a.slices == 1 && route_pairs(some, a.experts)) launch_route_t<2, 16>(a, some, stream);
         else if (some <= kRouteWaves) launch_route_t<1, 64>(a, some, stream);
         else launch_route_t<1, 32>(a, some, stream);
         if (hipGetLastError() != hipSuccess) return kErrHip;
