@@ -135,6 +135,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const double (&logit)
     }
 }
 
+// (What each kernel here reads, 35 MB at 4000 tokens and 256 experts of 4096 columns, takes 7 us; the products 107 us at the matrix pipe's 64-bit rate.)
 // Workgroup (x, y, z): 16 T experts, 16 T tokens, one slice of K, which its eight waves share (each holds 8 consecutive columns of a row per lane and step: the sum
 // does not care which four columns a MFMA takes, so its step j takes the j-th of each lane's eight).  The logits go to memory past the caches; the
 // workgroup that takes the token tile's last ticket adds the slices in order and chooses, a token for every GROUP lanes.
@@ -387,7 +388,8 @@ route_near_kernel(RouteArgs a) {
     }
 }
 
-// A wave for each token.
+// A wave for each token: bounds and border 9 of 31 us (4000 tokens, top_k 8 of 256, 4096 columns), the rest rows of experts from the L2 (0.3 GB) and their products, as many with sums
+// in binary32 (28 us).
 constexpr int kChoosers = 4;
 template <int VALUES>
 __global__ void __launch_bounds__(64 * kChoosers)
@@ -457,7 +459,7 @@ route_near_choose_kernel(RouteArgs a) {
         double sum[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            row[i] = a.R + (int64_t)__builtin_amdgcn_readfirstlane(named[wave][at + i]) * a.ldr;
+            row[i] = a.R + (int64_t)__builtin_amdgcn_readfirstlane(named[wave][min(at + i, count - 1)]) * a.ldr;
             sum[i] = 0.0;
         }
         struct Columns { u32x4 x, w[W]; };
@@ -480,24 +482,21 @@ route_near_choose_kernel(RouteArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         }
         // (lanes that differ in the lowest bits take over one sum each)
-        int mine = 0;
-        if constexpr (W == 4) {
-            const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
-            const double s0 = (b0 ? sum[1] : sum[0]) + __shfl_xor(b0 ? sum[0] : sum[1], 1);
-            const double s1 = (b0 ? sum[3] : sum[2]) + __shfl_xor(b0 ? sum[2] : sum[3], 1);
-            sum[0] = (b1 ? s1 : s0) + __shfl_xor(b1 ? s0 : s1, 2);
-            mine = lane & 3;
-        } else {
-            sum[0] += __shfl_xor(sum[0], 1);
-            sum[0] += __shfl_xor(sum[0], 2);
-        }
 #pragma unroll
-        for (int d = 4; d < 64; d <<= 1) sum[0] += __shfl_xor(sum[0], d);
-        if (lane < W) exact[wave][at + mine] = sum[0];
+        for (int d = 1; d < W; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < W / (2 * d); ++i) {
+                const bool odd = (lane & d) != 0;
+                sum[i] = (odd ? sum[2 * i + 1] : sum[2 * i]) + __shfl_xor(odd ? sum[2 * i] : sum[2 * i + 1], d);
+            }
+#pragma unroll
+        for (int d = W; d < 64; d <<= 1) sum[0] += __shfl_xor(sum[0], d);
+        if (lane < W && at + lane < count) exact[wave][at + lane] = sum[0];
     };
+    // (eight rows at a time: level; the rows come from the L2, 8 KB each at 4096 columns, and that is what these take)
     int at = 0;
     for (; at + 4 <= count; at += 4) dots(std::integral_constant<int, 4>{}, at);
-    for (; at < count; ++at) dots(std::integral_constant<int, 1>{}, at);
+    for (; at < count; at += 2) dots(std::integral_constant<int, 2>{}, at);
     ordered();
     auto sigmoid = [](double l) { return 1.0 / (1.0 + exp(-l)); };
     double most = 0.0;
@@ -568,7 +567,9 @@ static void launch_route_t(const RouteArgs &a, int64_t tokens, hipStream_t strea
     else route_kernel<GROUP < 32 ? 32 : GROUP, GROUP < 64 ? 16 : 8, T><<<grid, 64 * kRouteWaves, 0, stream>>>(a);
 }
 
-// Where a choice depends on one logit each, and there are many.
+// Where a choice depends on one logit each, and there are many: us in binary64 and this way, columns 2048 / 7168:
+// 65536 logits (256 tokens, 256 experts) 17.3 and 19.5 / 33.9 and 41.8, 131072 (512, 256) 24.7 and 19.4 / 55.5 and 44.0, (2048, 64) 21.7 and 19.7 / 52.8 and 45.2,
+// 2^20 (4096, 256) 100 and 27 / 283 and 66.  (Scores of a softmax that is not divided out again, or with a bias, need all logits in binary64.)
 static bool route_near(const RouteArgs &a, int64_t tokens) {
     return (a.sigmoid || (a.renormalize && !a.bias)) && a.experts >= 16 && tokens * a.experts >= ((int64_t)1 << 17);
 }
