@@ -121,6 +121,20 @@ def test_many_logits(nfp, M, E, K, top_k, sigmoid, with_bias, renormalize):
     compare(got, ff.route_ref(x, router, top_k, sigmoid, renormalize, bias, 2.5))
 
 
+@pytest.mark.parametrize("places", [(0, 1), (2, 3), (4, 5), (6, 7)])
+def test_many_logits_of_a_few_columns(nfp, places):
+    """Every column counts for what a 32-bit sum may be off by: large sums that cancel, of some of each eight columns alone."""
+    M, E, K, top_k = 1500, 128, 2048, 7
+    g = ff.generator(8)
+    some = torch.zeros(K, dtype=torch.bool, device="cuda:0")
+    for p in places:
+        some[p::8] = True
+    x = torch.where(some, ((12.0 + ff.normal(g, M, K).float()) * 128).round() / 128, 0.0).half()          # multiples of 2^-7
+    base = torch.where(torch.arange(K, device="cuda:0") < K // 2, 0.5, -0.5)
+    router = (base + (ff.normal(g, E, K).float().round() * 2.0 ** -11)).half()                             # multiples of 2^-12: sums are exact in 64 bits
+    compare(nfp.moe_route(x, router, top_k), ff.route_ref(x, router, top_k, False, True, None, 1.0))
+
+
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("kind", ["plain", "outliers", "cancelling"])
 def test_many_logits_that_32_bits_cannot_tell_apart(nfp, sigmoid, kind):
