@@ -186,3 +186,18 @@ def test_another_stream(nfp):
         z = nfp.linear_fused(x, layer, 0, activation=nfp.ACT_SILU, gated=True)
     s.synchronize()
     assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("knobs", TILES, ids=lambda k: "-".join("%s%d" % (n[6:], v) for n, v in k.items()))
+def test_residual_in_place_in_every_tile(nfp, tuned, knobs):
+    """No output is added to twice, where tiles end inside the matrix too."""
+    tuned(small_max_m=0, **knobs)
+    g = ff.generator(13)
+    for rows, split in itertools.product((0, 1), (1, 2)):
+        tuned(large_rows=rows, large_split=split)
+        for mode, gated, N in ((0, False, 517), (0, True, 778), (1, False, 520), (1, True, 780)):
+            x, layer, out = ff.normal(g, 300, 1040), nfp.Layer(ff.normal(g, N, 1040, sigma=0.02)), N // 2 if gated else N
+            r = ff.normal(g, 300, out)
+            apart = nfp.linear_fused(x, layer, mode, activation=nfp.ACT_SILU, gated=gated, residual=r)
+            nfp.linear_fused(x, layer, mode, activation=nfp.ACT_SILU, gated=gated, residual=r, out=r)
+            assert torch.equal(r, apart), (rows, split, mode, gated)

@@ -214,3 +214,39 @@ def test_workspace_for_many_calls(nfp):
             assert all(torch.equal(a, b) for a, b in zip(nfp.moe_route(z, router, 3, workspace=ws), chosen))
             torch.cuda.synchronize()
             assert (ws[:nfp.WORKSPACE_COUNTER_BYTES] == 0).all()
+
+
+def test_two_streams_at_once(nfp):
+    """Routers (few and many tokens), experts and linears with an epilogue on two streams, each with a workspace of its own, give what they give alone."""
+    g = ff.generator(21)
+    experts = nfp.Experts(ff.normal(g, 24, 2 * 272, 1040, sigma=0.03), ff.normal(g, 24, 1040, 272, sigma=0.03))
+    router, layer = ff.normal(g, 24, 1040, sigma=0.03), nfp.Layer(ff.normal(g, 2 * 528, 1040, sigma=0.03))
+    wide = ff.normal(g, 128, 1040, sigma=0.03)
+    few = [ff.normal(g, m, 1040) for m in (33, 48)]
+    many = [ff.normal(g, m, 1040) for m in (1300, 2048)]
+    need = max(nfp.moe_route_workspace_size(2048, 128, 1040), nfp.moe_workspace_size(48, experts, 4), nfp.linear_fused_workspace_size(2048, layer, nfp.MODE_FP8),
+               nfp.linear_fused_workspace_size(2048, layer, nfp.MODE_FP16))
+
+    def everything(i, mode, ws):
+        ids, weights = nfp.moe_route(few[i], router, 4, workspace=ws)
+        y = nfp.moe(few[i], experts, ids, weights, mode, residual=few[i], workspace=ws)
+        more = nfp.moe_route(many[i], wide, 6, scoring="sigmoid", workspace=ws)
+        z = nfp.linear_fused(many[i], layer, mode, activation=nfp.ACT_SILU, gated=True, workspace=ws)
+        return (ids, weights, y, *more, z, nfp.linear_fused(few[i], layer, mode, activation=nfp.ACT_GELU, gated=True, workspace=ws))
+
+    rooms = [nfp.new_workspace(need, "cuda:0") for _ in range(2)]
+    alone = [everything(i, i, rooms[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(everything(i, i, rooms[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for run in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(run, alone[i]))
+        assert (rooms[i][:nfp.WORKSPACE_COUNTER_BYTES] == 0).all()
