@@ -242,7 +242,7 @@ __device__ __forceinline__ void lds_barrier() {
 // (with many sums those of one unit are all that the LDS has room for: a second barrier)
 constexpr int sum_regions(int MT, int TILES) { return MT * TILES > 4 ? 1 : 2; }
 template <int KIND, int MT, int SPW, bool PASSES, int POL, bool DOWN, int TILES>
-__global__ void __launch_bounds__(MT == 1 && !PASSES ? (DOWN ? 576 : 1024) : 512)
+__global__ void __launch_bounds__(MT == 1 && !PASSES ? (DOWN && SPW > 2 ? 576 : 1024) : 512)
 experts_kernel(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     constexpr int KSTEP = 64, EB = kind_elem_bytes(KIND), PIECES = row_pieces<KIND == kPlainF16 ? kPlainF16 : kNestedF16Row, SPW>();
@@ -597,7 +597,7 @@ static int launch_experts_t(const ExpertArgs &a, int waves, hipStream_t stream) 
     if (lds > 160 * 1024) return kErrShape;
     const int64_t tiles = (DOWN ? a.K : 2 * a.ffn) / 16, units = choice_most(a.experts, n) * ((tiles + TILES - 1) / TILES);
     // waves that a CU holds, by registers
-    const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : 12) : (PASSES ? 12 : 16));
+    const int held = MT > 1 ? 8 : (DOWN ? (PASSES ? 8 : (SPW == 2 ? 16 : 12)) : (PASSES ? 12 : 16));
     const int all = waves + (DOWN ? 1 : 0);
     const int per_cu = std::max(1, std::min(held / all, (int)(160 * 1024 / lds)));
     kern<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(units, 256 * per_cu)), (unsigned)all * 64, lds, stream>>>(a);
@@ -608,7 +608,7 @@ template <int KIND, int MT, int SPW, int POL, bool DOWN>
 static int launch_slices(ExpertArgs a, hipStream_t stream) {
     const int64_t K = DOWN ? a.ffn : a.K, tiles = (DOWN ? a.K : 2 * a.ffn) / 16;
     const int slices = (int)((K + SPW * 64 - 1) / (SPW * 64));
-    const int one_pass = MT == 1 ? (DOWN ? 8 : 16) : (DOWN ? 7 : 8);   // waves that stream, as the registers allow
+    const int one_pass = MT == 1 ? (DOWN ? (SPW == 2 ? 15 : 8) : 16) : (DOWN ? 7 : 8);         // waves that stream, as the registers allow
     const int most = slices <= one_pass ? one_pass : (DOWN ? 7 : 8);
     a.passes = (slices + most - 1) / most;
     const int waves = (slices + a.passes - 1) / a.passes;
@@ -623,7 +623,13 @@ static int launch_slices(ExpertArgs a, hipStream_t stream) {
 template <int KIND, int POL, bool DOWN>
 static int launch_columns(const ExpertArgs &a, hipStream_t stream) {
     // both launches alike: the chunks of an expert's choices are counted once
-    if (a.M <= 16 || 2 * a.M * a.top_k <= 16 * a.experts) return launch_slices<KIND, 1, 4, POL, DOWN>(a, stream);
+    if (a.M <= 16 || 2 * a.M * a.top_k <= 16 * a.experts) {
+        // Twice as many waves on half as long slices where there are few units, that is little more than one unit's latency (1 token, hidden 1040, 2 experts of 528: up 7.4 -> 7.2 us,
+        // down 7.0 -> 6.2; 4 tokens, 16 experts of 768 x 2048: up 22.1 -> 19.6, down 14.6 and 15.1; but 16 tokens, 50 experts of 1408 x 4096: down 62 -> 66)
+        const int64_t K = DOWN ? a.ffn : a.K, tiles = (DOWN ? a.K : 2 * a.ffn) / 16;
+        if (K <= (DOWN ? 15 : 16) * 128 && choice_most(a.experts, (int)(a.M * a.top_k)) * tiles <= 8 * 256) return launch_slices<KIND, 1, 2, POL, DOWN>(a, stream);
+        return launch_slices<KIND, 1, 4, POL, DOWN>(a, stream);
+    }
     return a.M <= 32 || a.M * a.top_k <= 16 * a.experts ? launch_slices<KIND, 2, 4, POL, DOWN>(a, stream) : launch_slices<KIND, 4, 2, POL, DOWN>(a, stream);
 }
 

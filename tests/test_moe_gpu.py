@@ -250,3 +250,13 @@ def test_two_streams_at_once(nfp):
         for run in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(run, alone[i]))
         assert (rooms[i][:nfp.WORKSPACE_COUNTER_BYTES] == 0).all()
+
+
+@pytest.mark.parametrize("M,E,H,F,top_k", [(16, 24, 1600, 800, 4), (7, 40, 2048, 528, 6), (1, 32, 1920, 1920, 32), (1, 3, 2064, 2064, 2), (33, 30, 1552, 1040, 5)])
+def test_many_units_and_few(nfp, M, E, H, F, top_k):
+    """Both lengths of a wave's slice, on either side of what chooses them."""
+    for mode, exception in ((0, False), (1, False), (0, True)):
+        x, gate_up, down, ids, weights, r = make(M, E, H, F, top_k, seed=F, exception=exception)
+        y = nfp.moe(x, nfp.Experts(gate_up, down), ids, weights, mode, residual=r)
+        ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, mode == 1 and not exception, 2, r)
+        ff.assert_within(y, ref, tol, str((mode, exception)))
