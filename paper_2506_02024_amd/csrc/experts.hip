@@ -1,5 +1,5 @@
-// A mixture of experts on a few tokens (1 ... 64), in two launches of one kernel: gate and up products with the activation, down products with the
-// weighted sum.  Bound by the bytes of the experts that the tokens have chosen; everything here is arranged around streaming
+// A mixture of experts on a few tokens (1 ... 64), in two launches of one kernel, gate and up products with the activation and down products, and the weighted sum, of few choices in the second
+// launch, of more in a third.  Bound by the bytes of the experts that the tokens have chosen; everything here is arranged around streaming
 // those once.  Which experts these are the first launch finds out itself from the tokens' choices, which lie in device memory.
 //
 // As in the streaming linears, weight rows are the MFMA's first operand (row-major, fetched in pieces of 16 rows x 128 bytes and
@@ -222,6 +222,60 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("" ::: "memory");
 }
 
+// ---- the sum over a token's choices -------------------------------------------------------------------
+constexpr int kThrough = 1 | 16;                       // sc0 | sc1: every XCD has an L2 of its own
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t products_rsrc(const ExpertArgs &a) {
+    return weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)(a.M * a.top_k * a.K * 4));
+}
+// Four outputs of token m, its choices in their order.
+__device__ __forceinline__ void join_four(const ExpertArgs &a, const Choices &c, __amdgpu_buffer_rsrc_t rsp, int m, int col) {
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {          // (eight loads under way at a time)
+        u32x4 v[8];
+        float share[8];
+        uint32_t used[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = m * a.top_k + min(j0 + j, a.top_k - 1);
+            v[j] = __builtin_amdgcn_raw_buffer_load_b128(rsp, j0 + j < a.top_k ? (uint32_t)(((int64_t)r * a.K + col) * 4) : 0xfffffff0u, 0, kThrough);
+            used[j] = c.used[r >> 5] >> (r & 31) & 1u;
+            share[j] = c.share[r];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {                  // (what nobody has written, or repeats an earlier choice, is not added, whatever it holds)
+            const bool in = j0 + j < a.top_k && used[j] != 0;
+            share[j] = in ? share[j] : 0.0f;
+            v[j] = in ? v[j] : u32x4{0u, 0u, 0u, 0u};
+            sum.x = __builtin_fmaf(share[j], __uint_as_float(v[j].x), sum.x);
+            sum.y = __builtin_fmaf(share[j], __uint_as_float(v[j].y), sum.y);
+            sum.z = __builtin_fmaf(share[j], __uint_as_float(v[j].z), sum.z);
+            sum.w = __builtin_fmaf(share[j], __uint_as_float(v[j].w), sum.w);
+        }
+    }
+    if (a.residual) {
+        const floatx4 v = four_halves(a.residual + (int64_t)m * a.ldr + col, a.vec & 1, 4);
+        sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
+    }
+    u32x2 o;
+    o.x = float2_to_half2_bits(sum.x, sum.y);
+    o.y = float2_to_half2_bits(sum.z, sum.w);
+    uint16_t *const dst = a.Y + (int64_t)m * a.ldy + col;
+    if (a.vec & 2) *reinterpret_cast<u32x2 *>(dst) = o;
+    else
+#pragma unroll
+        for (int p = 0; p < 4; ++p) dst[p] = (uint16_t)((p < 2 ? o.x : o.y) >> (16 * (p & 1)));
+}
+
+// Many choices are joined by a launch of their own: joined by the wave with a block's last unit, they keep that wave's workgroup waiting.  us of the down products that join, and without
+// plus this launch (4.6): 48 tokens, top_k 6, 5120 outputs 311 and 259; 16, 6, 4096 62 and 56; 8, 8, 2048 26.5 and 17.6; 12, 4, 2048 27.5 and 19.8; 8, 4, 4096 35.4 and 31.3; 4, 6, 4096 28.5 and
+// 27.0; 1, 8, 2048 10.4 and 7.7.
+__global__ void __launch_bounds__(256)
+join_choices_kernel(ExpertArgs a) {
+    const Choices c = choices_at(a.choices, a.experts, (int)a.M * a.top_k);
+    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x, across = a.K >> 2;
+    if (item < a.M * across) join_four(a, c, products_rsrc(a), (int)(item / across), (int)(item % across) * 4);
+}
+
 // ---- the kernel ---------------------------------------------------------------------------------------
 // Rows of weights: gate and up rows in turn (first launch, !DOWN), so that a lane's four sums of a 16-row tile are two gated pairs; rows of the output (DOWN).
 // A unit of work is two (or four) such tiles of one expert for up to 16 MT of its choices.  All units stand in one row, expert by expert, and every
@@ -230,9 +284,9 @@ __device__ __forceinline__ void lds_barrier() {
 // across units and experts; sums meet in LDS, one barrier per unit.
 // Columns are the choices of the expert, loaded anew with every expert, so that 48 tokens over many experts take the time of a few; in the first launch up
 // to 16 tokens stand in the columns as they are (`gather` 0) and are loaded once.
-// The second launch leaves the product of every choice in memory, 32 bits each.  A wave of every workgroup that streams nothing adds up its units' sums,
-// stores them past the caches and counts the units per block of output rows a unit later, when they have arrived; where it has the last of them, it adds up the rows'
-// choices, token by token in their order, so that the result does not depend on timing.  (Counted by the workgroup at its end, the last workgroups
+// The second launch leaves the product of every choice in memory, 32 bits each.  A wave of every workgroup that streams nothing adds up its units' sums and
+// stores them past the caches.  Of few choices (`join`) it counts the units per block of output rows a unit later, when they have arrived; where it has the last of them, it adds up the rows'
+// choices, token by token in their order, so that the result does not depend on timing.  More are added up by a third launch, in the same order.  (Counted by the workgroup at its end, the last workgroups
 // to end had all their rows to add up, 10 to 17 us.)
 // (Tried for the second launch: a workgroup for 16 output rows that walks over all experts and needs no memory in between.  Each of its waves has to fetch
 // the products of every expert anew for 16 rows of weights: 16 tokens, 64 experts of 1408, FP8 mode 80 us; 48 tokens, 96 experts of 1520, FP16 mode 478 us.)
@@ -410,46 +464,14 @@ experts_kernel(ExpertArgs a) {
     if constexpr (DOWN) {
         if (wave == waves) {
             // products of the choices: written through, read back past the caches (every XCD has an L2 of its own)
-            constexpr int kThrough = 1 | 16;           // sc0 | sc1
-            const __amdgpu_buffer_rsrc_t rsp = weight_rsrc(reinterpret_cast<const uint8_t *>(a.products), (uint32_t)((int64_t)n * a.K * 4));
+            const __amdgpu_buffer_rsrc_t rsp = products_rsrc(a);
             auto join = [&](int f) {
                 for (int i = lane; i < a.M * (4 * TILES); i += 64) {
                     const int m = i / (4 * TILES), col = 16 * TILES * f + 4 * (i % (4 * TILES));
-                    if (col >= a.K) continue;
-                    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-                    for (int j0 = 0; j0 < a.top_k; j0 += 8) {          // (eight loads under way at a time)
-                        u32x4 v[8];
-                        float share[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int r = m * a.top_k + j0 + j;
-                            const bool in = j0 + j < a.top_k && (c.used[r >> 5] >> (r & 31) & 1u) != 0;
-                            share[j] = in ? c.share[r] : 0.0f;
-                            v[j] = __builtin_amdgcn_raw_buffer_load_b128(rsp, in ? (uint32_t)(((int64_t)r * a.K + col) * 4) : 0xfffffff0u, 0, kThrough);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            sum.x = __builtin_fmaf(share[j], __uint_as_float(v[j].x), sum.x);
-                            sum.y = __builtin_fmaf(share[j], __uint_as_float(v[j].y), sum.y);
-                            sum.z = __builtin_fmaf(share[j], __uint_as_float(v[j].z), sum.z);
-                            sum.w = __builtin_fmaf(share[j], __uint_as_float(v[j].w), sum.w);
-                        }
-                    }
-                    if (a.residual) {
-                        const floatx4 v = four_halves(a.residual + (int64_t)m * a.ldr + col, a.vec & 1, 4);
-                        sum.x += v.x;  sum.y += v.y;  sum.z += v.z;  sum.w += v.w;
-                    }
-                    u32x2 o;
-                    o.x = float2_to_half2_bits(sum.x, sum.y);
-                    o.y = float2_to_half2_bits(sum.z, sum.w);
-                    uint16_t *const dst = a.Y + (int64_t)m * a.ldy + col;
-                    if (a.vec & 2) *reinterpret_cast<u32x2 *>(dst) = o;
-                    else
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) dst[p] = (uint16_t)((p < 2 ? o.x : o.y) >> (16 * (p & 1)));
+                    if (col < a.K) join_four(a, c, rsp, m, col);
                 }
             };
-            if (total == 0)                            // nobody has chosen anything: the rows are shared out
+            if (total == 0 && a.join)                  // nobody has chosen anything: the rows are shared out
                 for (int f = blockIdx.x; f < per_expert; f += gridDim.x) join(f);
             if (first >= end) return;
             auto count_unit = [&](int f) {             // (behind a wait for the unit's products)
@@ -467,7 +489,7 @@ experts_kernel(ExpertArgs a) {
             for (uint32_t u = first; u < end; ++u) {
                 lds_barrier();
                 uint32_t before = 0;
-                if (f_before >= 0) {
+                if (f_before >= 0 && a.join) {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the products of the unit before
                     before = count_unit(f_before);
                 }
@@ -478,7 +500,7 @@ experts_kernel(ExpertArgs a) {
                     for (int i = 0; i < MT; ++i) sum[t][i] = add_up(t, i);
                 if constexpr (REGIONS == 2) region ^= 1;
                 else lds_barrier();
-                if (f_before >= 0) finish(f_before, before);
+                if (f_before >= 0 && a.join) finish(f_before, before);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -494,6 +516,7 @@ experts_kernel(ExpertArgs a) {
                 if (u + 1 < end && (next.r != at.r || next.chunk != at.chunk)) columns(next);
                 at = next;
             }
+            if (!a.join) return;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             finish(f_before, count_unit(f_before));
             return;
@@ -642,8 +665,11 @@ static int launch_lines(const ExpertArgs &a, hipStream_t stream) {
 
 template <int KIND>
 static int launch_both(const ExpertArgs &a, hipStream_t stream) {
-    const int st = launch_lines<KIND, false>(a, stream);
-    return st != kOk ? st : launch_lines<KIND, true>(a, stream);
+    int st = launch_lines<KIND, false>(a, stream);
+    if (st == kOk) st = launch_lines<KIND, true>(a, stream);
+    if (st != kOk || a.join) return st;
+    join_choices_kernel<<<(unsigned)((a.M * (a.K >> 2) + 255) / 256), 256, 0, stream>>>(a);
+    return hip_ok(hipGetLastError());
 }
 
 int launch_experts_layer(int kind, ExpertArgs a, uint8_t *room, hipStream_t stream) {
@@ -651,6 +677,7 @@ int launch_experts_layer(int kind, ExpertArgs a, uint8_t *room, hipStream_t stre
     a.H = reinterpret_cast<uint16_t *>(room + choices_bytes(a.experts, a.M * a.top_k));
     a.products = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.H) + activated_bytes(a.M * a.top_k, a.ffn));
     a.gather = a.M > 16 ? 1 : 0;
+    a.join = a.M * a.top_k <= 32 ? 1 : 0;
     return kind == kPlainF16 ? launch_both<kPlainF16>(a, stream) : (kind == kE4M3Row ? launch_both<kE4M3Row>(a, stream) : launch_both<kNestedF16Row>(a, stream));
 }
 

@@ -299,6 +299,7 @@ struct ExpertArgs {
     int32_t experts, top_k, act;
     int32_t vec;                                       // 1: residuals are loaded four at a time, 2: outputs are stored so
     int32_t passes, gather;
+    int32_t join;                                      // the down products' launch adds up the tokens' choices
 };
 size_t experts_workspace_bytes(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);      // behind the counters
 bool experts_supported(int64_t experts, int64_t hidden, int64_t ffn, int64_t M, int64_t top_k);
