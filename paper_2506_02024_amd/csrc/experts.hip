@@ -647,10 +647,11 @@ template <int KIND, int POL, bool DOWN>
 static int launch_columns(const ExpertArgs &a, hipStream_t stream) {
     // both launches alike: the chunks of an expert's choices are counted once
     if (a.M <= 16 || 2 * a.M * a.top_k <= 16 * a.experts) {
-        // Twice as many waves on half as long slices where there are few units, that is little more than one unit's latency (1 token, hidden 1040, 2 experts of 528: up 7.4 -> 7.2 us,
-        // down 7.0 -> 6.2; 4 tokens, 16 experts of 768 x 2048: up 22.1 -> 19.6, down 14.6 and 15.1; but 16 tokens, 50 experts of 1408 x 4096: down 62 -> 66)
-        const int64_t K = DOWN ? a.ffn : a.K, tiles = (DOWN ? a.K : 2 * a.ffn) / 16;
-        if (K <= (DOWN ? 15 : 16) * 128 && choice_most(a.experts, (int)(a.M * a.top_k)) * tiles <= 8 * 256) return launch_slices<KIND, 1, 2, POL, DOWN>(a, stream);
+        // Twice as many waves on half as long slices: for gate and up where there are few units, that is little more than one unit's latency (1 token, hidden 1040, 2 experts of 528:
+        // 7.4 -> 7.2 us; 4 tokens, 16 experts of 768 x 2048: 22.1 -> 19.6; but 16 tokens, 52 of these, FP8 mode: 32.1 and 34.1), for down wherever one pass takes all of K
+        // (1 token, 528: 7.0 -> 6.2 us; 16 tokens, 50 experts of 1408 x 4096, FP8 mode: 57 -> 52; 48 tokens, 92 of 1520 x 5120: 259 and 257; 16 tokens, 52 of 768 x 2048: 29.4 and 30.0).
+        const int64_t K = DOWN ? a.ffn : a.K, tiles = 2 * a.ffn / 16;
+        if (DOWN ? K <= 15 * 128 : K <= 16 * 128 && choice_most(a.experts, (int)(a.M * a.top_k)) * tiles <= 8 * 256) return launch_slices<KIND, 1, 2, POL, DOWN>(a, stream);
         return launch_slices<KIND, 1, 4, POL, DOWN>(a, stream);
     }
     return a.M <= 32 || a.M * a.top_k <= 16 * a.experts ? launch_slices<KIND, 2, 4, POL, DOWN>(a, stream) : launch_slices<KIND, 4, 2, POL, DOWN>(a, stream);
