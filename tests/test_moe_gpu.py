@@ -260,3 +260,30 @@ def test_many_units_and_few(nfp, M, E, H, F, top_k):
         y = nfp.moe(x, nfp.Experts(gate_up, down), ids, weights, mode, residual=r)
         ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, mode == 1 and not exception, 2, r)
         ff.assert_within(y, ref, tol, str((mode, exception)))
+
+
+@pytest.mark.parametrize("M,top_k", [(1, 8), (8, 4), (9, 4), (33, 2), (64, 6)])
+def test_replays_on_a_workspace_that_holds_anything(nfp, M, top_k):
+    """Few choices, which the down products' launch adds up, and more, which a launch of their own does: replayed with new choices, some of them outside the experts and some named twice,
+    in place, with NaN in the workspace behind its counters."""
+    E, H, F = 10, 208, 144
+    x, gate_up, down, ids, weights, r = make(M, E, H, F, top_k, seed=M)
+    experts, g = nfp.Experts(gate_up, down), ff.generator(M + 1)
+    ws = nfp.new_workspace(nfp.moe_workspace_size(M, experts, top_k), "cuda:0")
+    y = r.clone()
+    call = lambda: nfp.moe(x, experts, ids, weights, 0, residual=y, out=y, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for turn in range(5):
+        ids.copy_(torch.randint(-2, E + 2, ids.shape, generator=g, device="cuda:0") if turn < 4 else torch.full_like(ids, -1))
+        x.normal_(generator=g)
+        y.copy_(r)
+        ws[nfp.WORKSPACE_COUNTER_BYTES:] = 0xff
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, tol = ff.moe_ref(x, gate_up, down, ids, weights, False, 2, r)
+        ff.assert_within(y, ref, tol, str(turn))
+        assert (ws[:nfp.WORKSPACE_COUNTER_BYTES] == 0).all()
