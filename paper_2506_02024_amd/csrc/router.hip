@@ -555,9 +555,14 @@ static int route_slices(int64_t M, int64_t experts, int64_t K) {
     const int64_t tiles = ((experts + 15) / 16) * ((M + 15) / 16), steps = (K + 31) / 32;
     return (int)std::max<int64_t>(1, std::min<int64_t>({kMostSlices, 256 / tiles, steps / kRouteWaves}));
 }
+// Room for M tokens and for any fewer, whose logits can take more of it in more slices (256 experts of 2048 columns: 32 tokens 8 slices and 512 KiB, 33 tokens 5 and 330 KiB): a
+// program shares the workspace of its largest batch.
 size_t route_logit_bytes(int64_t M, int64_t experts, int64_t K) {
-    const int64_t tokens = route_tokens(M, experts);
-    return (size_t)route_slices(tokens, experts, K) * (size_t)tokens * (size_t)experts * 8;
+    const int64_t tokens = route_tokens(M, experts), across = (experts + 15) / 16;
+    int64_t rows = tokens;                             // slices * tokens, at most
+    for (int64_t s = 2; s <= std::min<int64_t>(kMostSlices, (K + 31) / 32 / kRouteWaves); ++s)
+        rows = std::max(rows, s * std::min(tokens, 256 / (s * across) * 16));          // (the most tokens that take s slices)
+    return (size_t)rows * (size_t)experts * 8;
 }
 
 template <int T, int GROUP>
