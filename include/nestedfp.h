@@ -356,7 +356,8 @@ int nestedfp_moe_route(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, con
  *   ids (int32) and weights (float) are dense [M,top_k], 1 <= top_k <= 32, and may come from anywhere: an id outside 0 ... experts - 1 adds nothing (experts of other
  *     GPUs, tokens that are padding), one that a token names twice counts with the sum of its weights.
  *   residual (FP16, row stride ldr, or NULL) and X may be Y.  Strides of X are multiples of 8, X and the weights 16-byte aligned.
- * Sums are binary32.  The activated products lie in the workspace as two FP16 terms (2^-22 of each; above 65504 they are infinite, as a linear's outputs).
+ * Sums are binary32.  The activated products lie in the workspace as two FP16 terms, off by 2^-22 of each product, by 2^-36 of one below 2^-14; above 65504 they are infinite, as a
+ * linear's outputs.  (Down weights that are infinite themselves, which only an exception can hold, give NaN.)
  * The results do not depend on timing.  The workspace follows the rules above (WORKSPACE).
  */
 typedef struct {

@@ -12,9 +12,12 @@
 
 namespace nfp {
 
-// The activated products between the two launches are kept as two FP16 terms, h = high + low: rounded to one, their error is as large as the
-// output's own rounding.
+// The activated products between the two launches are kept as two FP16 terms, h = high + 2^-11 low: rounded to one, their error is as large as the
+// output's own rounding.  The second term is the rest, at most half a step of the first, times 2^11, and so no larger than the first and a normal number wherever 2^-22 of h matters:
+// together they are off by 2^-22 of h, by 2^-36 below 2^-14 (where the first term is subnormal).  Unscaled, the rest was subnormal from h = 1/4 down: off by 2^-25, of products of 1e-4 2^-12.5.
+// Its products have a sum of their own, multiplied back once.
 constexpr int kTerms = 2;
+constexpr float kLowScale = 0x1p11f;
 
 // E4M3 bytes as FP16 words: sign, four bits of exponent and three of mantissa at the same places below FP16's exponent MSB read as the value times
 // 2^-8 (subnormals too), which is the weight that the upper plane stands for (Sec. 4.1).  (The conversion instruction, two bytes at a time and then a
@@ -424,10 +427,13 @@ experts_kernel(ExpertArgs a) {
     int region = 0;
     auto consume = [&](WItem (&w)[SPW], int tile, int pass) {
         floatx4 *const slot = slots + ((region * TILES + tile) * waves + wave) * MT * 64 + lane;
-        floatx4 sum[MT];
+        floatx4 sum[MT][TERMS];
         regroup_pieces<KIND, SPW>(w, rw);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sum[i] = PASSES && pass > 0 ? slot[i * 64] : floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < MT; ++i) {
+            sum[i][0] = PASSES && pass > 0 ? slot[i * 64] : floatx4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (TERMS == 2) sum[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll
         for (int s = 0; s < SPW; ++s) {
             u32x4 w_lo, w_hi;
@@ -436,12 +442,21 @@ experts_kernel(ExpertArgs a) {
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int t = TERMS - 1; t >= 0; --t) {
-                    sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_lo), as_half8(xa[s][i][t]), sum[i], 0, 0, 0);
-                    sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_hi), as_half8(xb[s][i][t]), sum[i], 0, 0, 0);
+                    sum[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_lo), as_half8(xa[s][i][t]), sum[i][t], 0, 0, 0);
+                    sum[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(w_hi), as_half8(xb[s][i][t]), sum[i][t], 0, 0, 0);
                 }
         }
 #pragma unroll
-        for (int i = 0; i < MT; ++i) slot[i * 64] = sum[i];
+        for (int i = 0; i < MT; ++i) {
+            floatx4 all = sum[i][0];
+            if constexpr (TERMS == 2) {
+                all.x = __builtin_fmaf(sum[i][1].x, 1.0f / kLowScale, all.x);
+                all.y = __builtin_fmaf(sum[i][1].y, 1.0f / kLowScale, all.y);
+                all.z = __builtin_fmaf(sum[i][1].z, 1.0f / kLowScale, all.z);
+                all.w = __builtin_fmaf(sum[i][1].w, 1.0f / kLowScale, all.w);
+            }
+            slot[i * 64] = all;
+        }
     };
     auto add_up = [&](int t, int i) {
         floatx4 sum = slots[(((region * TILES + t) * waves) * MT + i) * 64 + lane];
@@ -570,7 +585,7 @@ experts_kernel(ExpertArgs a) {
                     *reinterpret_cast<uint32_t *>(dst) = high;
                     if constexpr (kTerms == 2) {
                         // (an infinite first term has no rest)
-                        const float l0 = h0 - half_bits_to_float(high & 0xffffu), l1 = h1 - half_bits_to_float(high >> 16);
+                        const float l0 = kLowScale * (h0 - half_bits_to_float(high & 0xffffu)), l1 = kLowScale * (h1 - half_bits_to_float(high >> 16));
                         *reinterpret_cast<uint32_t *>(dst + a.ffn) =
                             float2_to_half2_bits((high & 0x7fffu) == 0x7c00u ? 0.0f : l0, (high & 0x7fff0000u) == 0x7c000000u ? 0.0f : l1);
                     }
