@@ -526,13 +526,13 @@ def linear_fused(X, layer, mode, bias=None, activation=ACT_NONE, gated=False, re
     """A linear with an epilogue, rounded once: act(X @ W^T + bias) + residual for a Layer in the given mode or, gated, the products of the
     activated gate rows and the up rows (+ residual), for a layer whose rows are gate and up rows in turn (interleave_gate_up).
 
-    X: float16 [M,K], or E4M3 codes (uint8 [M,K], contiguous) with their scales (float32 [M]), for which the mode is FP8.  bias: float16
+    X: float16 [M,K], or E4M3 codes (uint8 [M,K], contiguous) with their scales (float32 [M]), for which the mode has to be FP8 and act_scale None.  bias: float16
     [N]; residual: float16 [M, N or N / 2], may be out.  Exception layers run in FP16 and take no codes."""
     N = layer._dims[0]
     if out is None:
         out = torch.empty((X.shape[0], N // 2 if gated else N), dtype=torch.float16, device=X.device)
     if workspace is None:
-        workspace = _workspace(lib().nestedfp_linear_workspace_size(X.shape[0], layer._ref, MODE_FP8 if scales is not None else int(mode)), X.device)
+        workspace = _workspace(linear_fused_workspace_size(X.shape[0], layer, mode), X.device)
     st = (_marshal or _marshalled()).linear_fused(X, scales, layer._at, mode, act_scale, bias, activation, gated, residual, out, workspace, _stream())
     if st:
         raise NestedFPError(st, "nestedfp_linear_fused")

@@ -170,6 +170,8 @@ PyObject *linear_fused(PyObject *, PyObject *const *a, Py_ssize_t n) {
         e.activation = (int32_t)whole(a[6]);
         e.gated = PyObject_IsTrue(a[7]) == 1;
         const bool codes = a[1] != Py_None;
+        if (codes && whole(a[3]) != NESTEDFP_MODE_FP8) refuse("mode", "FP8 mode where X is codes");
+        if (codes && a[4] != Py_None) refuse("act_scale", "None where X is codes, which have scales");
         const char *what = codes ? "contiguous uint8 [M,K] codes, K as the layer's" : "float16 [M,K] with unit inner stride, K as the layer's";
         const Rows x = rows_of(a[0], "X", codes ? at::kByte : at::kHalf, what);
         if (x.cols != layer->K || (codes && x.ld != x.cols)) refuse("X", what);
