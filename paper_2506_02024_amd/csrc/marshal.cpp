@@ -35,6 +35,7 @@ const at::Tensor &tensor(PyObject *o, const char *name) {
 struct Rows {
     int64_t rows = 0, cols = 0, ld = 0;
     void *at = nullptr;
+    bool dense() const { return rows < 2 || ld == cols; }      // (one row is, whatever its stride, as for torch)
 };
 Rows rows_of(PyObject *o, const char *name, at::ScalarType type, const char *what) {
     const at::Tensor &t = tensor(o, name);
@@ -108,7 +109,7 @@ PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         void *q = nullptr, *scales = nullptr;
         if (a[6] != Py_None) {
             const Rows codes = rows_of(a[6], "Xq", at::kByte, "a contiguous uint8 [M,K] tensor");
-            if (codes.rows != x.rows || codes.cols != x.cols || codes.ld != x.cols) refuse("Xq", "a contiguous uint8 [M,K] tensor");
+            if (codes.rows != x.rows || codes.cols != x.cols || !codes.dense()) refuse("Xq", "a contiguous uint8 [M,K] tensor");
             q = codes.at;
             scales = dense(a[7], "scales", at::kFloat, x.rows, "a contiguous float32 [M] tensor");
         }
@@ -132,7 +133,7 @@ PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
             const char *what = "a contiguous float32 [positions, rotary_dim / 2] tensor";
             cos = rows_of(a[6], "cos", at::kFloat, what);
             sin = rows_of(a[7], "sin", at::kFloat, what);
-            if (cos.ld != cos.cols || sin.ld != sin.cols) refuse("cos and sin", "contiguous");
+            if (!cos.dense() || !sin.dense()) refuse("cos and sin", "contiguous");
             if (sin.rows != cos.rows || sin.cols != cos.cols) refuse("sin", "of the shape of cos");
             positions = dense(a[3], "positions", at::kInt, q.rows, "a contiguous int32 tensor, one for every token");
         }
@@ -174,7 +175,7 @@ PyObject *linear_fused(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (codes && a[4] != Py_None) refuse("act_scale", "None where X is codes, which have scales");
         const char *what = codes ? "contiguous uint8 [M,K] codes, K as the layer's" : "float16 [M,K] with unit inner stride, K as the layer's";
         const Rows x = rows_of(a[0], "X", codes ? at::kByte : at::kHalf, what);
-        if (x.cols != layer->K || (codes && x.ld != x.cols)) refuse("X", what);
+        if (x.cols != layer->K || (codes && !x.dense())) refuse("X", what);
         if (e.gated && layer->N % 2 != 0) refuse("a gated layer's rows", "gate and up rows in turn");
         Rows shape;
         shape.rows = x.rows;
@@ -221,7 +222,7 @@ PyObject *moe(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (x.cols != experts->hidden) refuse("X", "float16 [M, hidden] of the experts");
         const char *what = "contiguous [M,top_k] tensors, ids int32 and weights float32";
         const Rows ids = rows_of(a[3], "ids", at::kInt, what), weights = rows_of(a[4], "weights", at::kFloat, what);
-        if (ids.rows != x.rows || weights.rows != x.rows || ids.cols != weights.cols || ids.ld != ids.cols || weights.ld != weights.cols)
+        if (ids.rows != x.rows || weights.rows != x.rows || ids.cols != weights.cols || !ids.dense() || !weights.dense())
             refuse("ids and weights", what);
         const Rows residual = like(a[5], "residual", x), out = like(a[6], "out", x);
         const at::Tensor &workspace = tensor(a[7], "workspace");
