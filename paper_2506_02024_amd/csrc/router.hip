@@ -452,9 +452,24 @@ route_near_choose_kernel(RouteArgs a) {
         if (in) named[wave][count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = (uint16_t)(lane + 64 * v);
         count += __popcll(mask);
     }
+    const uint16_t *const x = a.X + (a.token0 + m) * a.ldx;
+    // A row of zeros (padding) among finite experts: all logits are zero.  Without a bias they all tie and would all be summed again, 540 us in place of 53 for 4000 such tokens
+    // (256 experts, 4096 columns); the first top_k are the choice (34 us).  (A bound of zero alone is not enough: squares of the smallest numbers may be lost on the way to it.)
+    bool zeros = error == 0.0f && !a.bias;
+    if (zeros) {
+        u32x4 any = {0u, 0u, 0u, 0u};
+        for (int64_t k = 8 * lane; k < a.K; k += 512) any |= *reinterpret_cast<const u32x4 *>(x + k);
+        zeros = __ballot(((any.x | any.y | any.z | any.w) & 0x7fff7fffu) != 0) == 0;
+        if (zeros) {
+            if (lane < a.top_k) {
+                named[wave][lane] = (uint16_t)lane;
+                exact[wave][lane] = 0.0;
+            }
+            count = a.top_k;
+        }
+    }
     ordered();
     // their logits: products of FP16 values, exact in binary32, added up in binary64
-    const uint16_t *const x = a.X + (a.token0 + m) * a.ldx;
     auto dots = [&](auto width, int at) {
         constexpr int W = decltype(width)::value;
         const uint16_t *row[W];
@@ -496,7 +511,7 @@ route_near_choose_kernel(RouteArgs a) {
         if (lane < W && at + lane < count) exact[wave][at + lane] = sum[0];
     };
     // (eight rows at a time: level; the rows come from the L2, 8 KB each at 4096 columns, and that is what these take)
-    int at = 0;
+    int at = zeros ? count : 0;
     for (; at + 4 <= count; at += 4) dots(std::integral_constant<int, 4>{}, at);
     for (; at < count; at += 2) dots(std::integral_constant<int, 2>{}, at);
     ordered();
