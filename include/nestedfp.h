@@ -304,7 +304,7 @@ typedef enum {
     NESTEDFP_ACT_NONE = 0,
     NESTEDFP_ACT_RELU = 1,
     NESTEDFP_ACT_SILU = 2,
-    NESTEDFP_ACT_GELU = 3       /* the form with a tangent */
+    NESTEDFP_ACT_GELU = 3       /* the form with a hyperbolic tangent */
 } nestedfp_activation;
 
 typedef struct {
@@ -333,7 +333,7 @@ int nestedfp_linear_fused_prequantized(const uint8_t *Xq, const float *scales, i
  *   weights[m] score of each (/ their sum if renormalize) * factor, float [M,top_k], rounded once
  * A NaN is chosen after all numbers; the ids of a token are different experts whatever its activations hold.  1 <= top_k <= 32, top_k <= experts
  * <= 512; K is a multiple of 16, strides are multiples of 8 and at most 2^21, X and R 16-byte aligned.  The workspace follows the rules above
- * (WORKSPACE): it holds logits, 32 MiB and 16 KiB at most.
+ * (WORKSPACE): it holds logits, 32 MiB and 16 KiB at most, and one for M tokens takes any fewer.
  */
 typedef enum {
     NESTEDFP_SCORE_SOFTMAX = 0,
@@ -347,7 +347,7 @@ int nestedfp_moe_route(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, con
 
 /*
  * moe: Y[m] = fp16(residual[m] + sum_j weights[m,j] * down_e (act(gate_e x_m) * up_e x_m)),  e = ids[m,j],  for M tokens, 1 ... 64 (more are
- * NESTEDFP_ERR_SHAPE: their experts' products are large enough for linears of their own).
+ * NESTEDFP_ERR_SHAPE: each call reads the experts that its tokens have chosen once).
  *   experts: a description in HOST memory.  `up` is the stacked matrix [experts * 2 ffn, hidden], an expert's gate and up rows in turn (gate row f
  *     at 2 f, up row f at 2 f + 1), `down` [experts * hidden, ffn]; either as the row-major planes that nestedfp_decompose writes of it
  *     or, with is_exception, as dense FP16.  hidden and ffn are multiples of 16, experts <= 512, an expert's FP16 matrices below 2 GiB.
@@ -358,7 +358,7 @@ int nestedfp_moe_route(const uint16_t *X, int64_t M, int64_t K, int64_t ldx, con
  *   residual (FP16, row stride ldr, or NULL) and X may be Y.  Strides of X are multiples of 8, X and the weights 16-byte aligned.
  * Sums are binary32.  The activated products lie in the workspace as two FP16 terms, off by 2^-22 of each product, by 2^-36 of one below 2^-14; above 65504 they are infinite, as a
  * linear's outputs.  (Down weights that are infinite themselves, which only an exception can hold, give NaN.)
- * The results do not depend on timing.  The workspace follows the rules above (WORKSPACE).
+ * The results do not depend on timing.  The workspace follows the rules above (WORKSPACE); one for M tokens takes any fewer.
  */
 typedef struct {
     int64_t experts, hidden, ffn;

@@ -509,7 +509,7 @@ def linear(X, layer, mode, act_scale=None, out=None, workspace=None):
     return out
 
 
-ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)         # ACT_GELU: the form with a tangent
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)         # ACT_GELU: the form with a hyperbolic tangent
 
 
 def interleave_gate_up(w):
@@ -547,7 +547,8 @@ class _ExpertsStruct(ctypes.Structure):
 
 class Experts:
     """The experts of a layer as the library describes them: row-major planes of gate and up ([experts, 2 ffn, hidden], gate rows first; laid out
-    anew here) and of down ([experts, hidden, ffn]), or the FP16 weights themselves if any |w| > 1.75.  Keeps the device buffers alive."""
+    anew here) and of down ([experts, hidden, ffn]), or, if any |w| > 1.75 in any
+    expert, the FP16 weights of all of them (is_exception), which both modes multiply then.  Keeps the device buffers alive."""
 
     def __init__(self, gate_up, down, activation=ACT_SILU):
         if gate_up.dim() != 3 or down.dim() != 3 or gate_up.dtype != torch.float16 or down.dtype != torch.float16:

@@ -225,7 +225,7 @@ __device__ __forceinline__ uint32_t float2_to_half2_bits(float a, float b) {
 }
 
 // ---- Epilogue of a linear (see Epilogue) -------------------------------------------------
-// SiLU is z sigma(z) and the GELU with a tangent z sigma(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi), since 1 + tanh u = 2 sigma(2 u):
+// SiLU is z sigma(z) and the GELU with a hyperbolic tangent z sigma(2 c (z + 0.044715 z^3)), c = sqrt(2 / pi), since 1 + tanh u = 2 sigma(2 u):
 // both are z / (1 + 2^u) with u = z (k1 + k3 z^2).  2^u overflows to infinity for large negative z, whose reciprocal is the
 // zero that is wanted.  Exponential and reciprocal are the hardware's, 1 ulp each; the rounding of u adds up to |u| 2^-24
 // to the relative error of 2^u, of which 2^-17 is left where the result is still a normal FP16 number (|u| < 2^7).

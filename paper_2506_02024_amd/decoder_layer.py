@@ -42,8 +42,8 @@ class DecoderLayer:
     float16.  mixture: a Mixture, which is added to what gate_up and down (a shared expert, fused) give, or is all there is if they are None.
 
     Calls that may overlap in time need workspaces of their own, and a captured graph needs one that stays: a program that captures calls
-    or issues them on several streams makes one for each graph and stream, of workspace_size for its largest call, and passes it (all layers of a
-    model can share it).  A call that is given none takes the layer's own, of which there is one for every stream, and while a graph is
+    or issues them on several streams makes one for each graph and stream, of the largest workspace_size among its calls (a smaller batch can need more
+    than a larger one, where it splits K or a sequence into more parts), and passes it (all layers of a model can share it).  A call that is given none takes the layer's own, of which there is one for every stream, and while a graph is
     captured one from that graph's memory, which the graph clears in every replay (3 us a layer)."""
 
     def __init__(self, qkv, o, gate_up, down, norm1, norm2, heads, kv_heads, eps=1e-5, packed=False, fused=False, mixture=None):
