@@ -399,7 +399,7 @@ int launch_large_gemm(int kind, const GemmArgs &a, hipStream_t stream) {
     const size_t slice_bytes = (size_t)a.M * (size_t)partial_ld(a.N) * sizeof(float);
     const size_t room = a.partials != nullptr ? a.partial_bytes / slice_bytes : 0;
     if ((size_t)c.split > room) c.split = room > 1 ? (int)room : 1;
-    LargeParams p;
+    FusedLargeParams p;
     p.X = static_cast<const uint8_t *>(a.X);
     p.x_row_bytes = kind_is_fp8(kind) ? a.ldx : 2 * a.ldx;
     p.scales = a.scales;

@@ -49,8 +49,9 @@ struct LargeParams {
     int rows_anywhere;      // output rows need not start on 16 bytes (N or ldy no multiple of 8, or Y not 16-byte aligned)
     int xcd_map;            // group the token tiles of a weight tile on one XCD (see tile_of_block)
     int xcd_group;          // token tiles per group of an XCD's part; 0: another order
-    Epilogue epi;
 };
+struct FusedLargeParams : LargeParams { Epilogue epi; };       // (see FusedSmallParams)
+template <int EPI> using LargeParamsOf = std::conditional_t<EPI == kEpiNone, LargeParams, FusedLargeParams>;
 
 // Which tile a workgroup takes.  The hardware deals consecutive workgroups to the 8 XCDs in turn,
 // and every XCD has an L2 of its own.  In launch order "token tile fastest" the token tiles of one weight tile land on
@@ -155,7 +156,7 @@ struct TileStore {
 
     // row0: the wave's first token row within the tile, F: its token blocks
     template <int F>
-    static __device__ __forceinline__ void to_lds(const LargeParams &p, AccT (&acc)[FNB][FMB], int m0, int n0, int row0, int wn, int lane,
+    static __device__ __forceinline__ void to_lds(const LargeParamsOf<EPI> &p, AccT (&acc)[FNB][FMB], int m0, int n0, int row0, int wn, int lane,
                                                   uint8_t *lds) {
         const int r = lane % MB;
         if constexpr (EPI != kEpiNone) {
@@ -187,7 +188,7 @@ struct TileStore {
     // per lane (the residual in pieces of 32 bytes per token, whose neighbours the next block of rows asks for).  Through LDS as
     // sums the tile would not fit, and added to the rounded outputs on their way out the residual would cost a second rounding.
     template <int F>
-    static __device__ __forceinline__ void to_lds_epilogue(const LargeParams &p, AccT (&acc)[FNB][FMB], int m0, int n0, int row0, int wn,
+    static __device__ __forceinline__ void to_lds_epilogue(const LargeParamsOf<EPI> &p, AccT (&acc)[FNB][FMB], int m0, int n0, int row0, int wn,
                                                            int lane, uint8_t *lds) {
         const int r = lane % MB;
         // (all that comes from memory is under way at a time: block by block, each waiting for its own, 8192 tokens of (4096, 4096) in FP8 mode took 28 us more
@@ -238,7 +239,7 @@ struct TileStore {
                 }
             }
     }
-    static __device__ __forceinline__ void epilogue_lds(const LargeParams &p, AccT (&acc)[FNB][FMB], int m0, int n0,
+    static __device__ __forceinline__ void epilogue_lds(const LargeParamsOf<EPI> &p, AccT (&acc)[FNB][FMB], int m0, int n0,
                                                         int row0, int wn, int lane, int wave, uint8_t *lds) {
         to_lds<FMB>(p, acc, m0, n0, row0, wn, lane, lds);
         __syncthreads();
@@ -600,7 +601,7 @@ struct LargeKernel {
         }
     }
 
-    static __device__ __forceinline__ void run(const LargeParams &p, uint8_t *lds, lds_byte *lds3) {
+    static __device__ __forceinline__ void run(const LargeParamsOf<EPI> &p, uint8_t *lds, lds_byte *lds3) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wm = UNEVEN ? wave / WAVES_N : wave % WAVES_M, wn = UNEVEN ? wave % WAVES_N : wave / WAVES_M;
@@ -673,7 +674,7 @@ struct LargeKernel {
 
 template <int KIND, int TM, int TN, int WAVES_M, int WAVES_N, int NST, int NSTW, int EPI>
 __global__ void __launch_bounds__(64 * WAVES_M * WAVES_N)
-large_gemm_kernel(LargeParams p) {
+large_gemm_kernel(LargeParamsOf<EPI> p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
     typedef LargeKernel<EPI, KIND, TM, TN, WAVES_M, WAVES_N, NST, NSTW> Kern;
     Kern::run(p, lds_raw, (typename Kern::lds_byte *)lds_raw);
@@ -922,7 +923,7 @@ struct BypassKernel {
         }
     }
 
-    static __device__ __forceinline__ void run(const LargeParams &p, uint8_t *lds, lds_byte *lds3) {
+    static __device__ __forceinline__ void run(const LargeParamsOf<EPI> &p, uint8_t *lds, lds_byte *lds3) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         int tm, tn;
@@ -1027,7 +1028,7 @@ struct BypassKernel {
 
 template <int TM, int TN, int WK, bool DEEP, bool NT, bool PAIRS, int EPI>
 __global__ void __launch_bounds__(512)
-nested_bypass_kernel(LargeParams p) {
+nested_bypass_kernel(LargeParamsOf<EPI> p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
     typedef BypassKernel<EPI, TM, TN, WK, DEEP, NT, PAIRS> Kern;
     Kern::run(p, lds_raw, (typename Kern::lds_byte *)lds_raw);
@@ -1228,7 +1229,7 @@ struct RowsKernel {
         }
     }
 
-    static __device__ __forceinline__ void run(const LargeParams &p, uint8_t *lds, lds_byte *lds3) {
+    static __device__ __forceinline__ void run(const LargeParamsOf<EPI> &p, uint8_t *lds, lds_byte *lds3) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         int tm, tn;
@@ -1326,7 +1327,7 @@ struct RowsKernel {
 
 template <int TM, int TN, bool NT, int EPI>
 __global__ void __launch_bounds__(512)
-nested_rows_kernel(LargeParams p) {
+nested_rows_kernel(LargeParamsOf<EPI> p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
     typedef RowsKernel<EPI, TM, TN, NT> Kern;
     Kern::run(p, lds_raw, (typename Kern::lds_byte *)lds_raw);
@@ -1487,7 +1488,7 @@ struct E4m3BypassKernel {
         }
     }
 
-    static __device__ __forceinline__ void run(const LargeParams &p, uint8_t *lds, lds_byte *lds3) {
+    static __device__ __forceinline__ void run(const LargeParamsOf<EPI> &p, uint8_t *lds, lds_byte *lds3) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         int tm, tn;
@@ -1569,7 +1570,7 @@ struct E4m3BypassKernel {
 
 template <int TM, int TN, bool ROWMAJOR, bool NT, int EPI>
 __global__ void __launch_bounds__(512)
-e4m3_bypass_kernel(LargeParams p) {
+e4m3_bypass_kernel(LargeParamsOf<EPI> p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
     typedef E4m3BypassKernel<EPI, TM, TN, ROWMAJOR, NT> Kern;
     Kern::run(p, lds_raw, (typename Kern::lds_byte *)lds_raw);
@@ -1578,7 +1579,7 @@ e4m3_bypass_kernel(LargeParams p) {
 struct LargeConfig { int tm, tn, split, deep; double cost; int height; };     // height of the token tiles: tm or less (see cuts_tiles)
 
 template <int EPI, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, int NST = 2, int NSTW = NST>
-static void launch_large_t(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_large_t(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     auto kern = large_gemm_kernel<KIND, TM, TN, WAVES_M, WAVES_N, NST, NSTW, EPI>;
     constexpr int lds = LargeKernel<EPI, KIND, TM, TN, WAVES_M, WAVES_N, NST, NSTW>::LDS_BYTES;
     static std::atomic<bool> attr_set{false};
@@ -1608,7 +1609,7 @@ static inline bool streams_tiles64(const LargeParams &p, bool fp8) {
 }
 
 template <int EPI, int TM, int TN, int WK, bool DEEP = false, bool NT = false, bool PAIRS = false>
-static void launch_bypass(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_bypass(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     auto kern = nested_bypass_kernel<TM, TN, WK, DEEP, NT, PAIRS, EPI>;
     constexpr int lds = BypassKernel<EPI, TM, TN, WK, DEEP, NT, PAIRS>::LDS_BYTES;
     static std::atomic<bool> attr_set{false};
@@ -1620,7 +1621,7 @@ static void launch_bypass(const LargeParams &p, dim3 grid, hipStream_t stream) {
 }
 
 template <int EPI, int TM, int TN, bool NT = false>
-static void launch_rows(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_rows(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     auto kern = nested_rows_kernel<TM, TN, NT, EPI>;
     constexpr int lds = RowsKernel<EPI, TM, TN, NT>::LDS_BYTES;
     static std::atomic<bool> attr_set{false};
@@ -1632,7 +1633,7 @@ static void launch_rows(const LargeParams &p, dim3 grid, hipStream_t stream) {
 }
 
 template <int EPI, int TM, int TN, bool ROWMAJOR, bool NT = false>
-static void launch_e4m3_bypass(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_e4m3_bypass(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     if constexpr (!NT) {
         if (ROWMAJOR ? streams_rows(p) : streams_tiles64(p, true)) {
             launch_e4m3_bypass<EPI, TM, TN, ROWMAJOR, true>(p, grid, stream);
@@ -1651,7 +1652,7 @@ static void launch_e4m3_bypass(const LargeParams &p, dim3 grid, hipStream_t stre
 
 // weights through LDS: plain row-major FP16, E4M3 in either storage order
 template <int EPI, int KIND>
-static void launch_large_k(const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_large_k(const LargeParamsOf<EPI> &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     if (c.height == 224) { launch_large_t<EPI, KIND, 224, 256, 2, 4, 2, 3>(p, grid, stream);  return; }
     if (c.height == 192) { launch_large_t<EPI, KIND, 192, 256, 2, 4, 2, 3>(p, grid, stream);  return; }
     if (c.height == 160) { launch_large_t<EPI, KIND, 160, 256, 2, 4, 3>(p, grid, stream);  return; }
@@ -1672,7 +1673,7 @@ static void launch_large_k(const LargeParams &p, const LargeConfig &c, dim3 grid
 }
 
 template <int EPI, int TM, bool DEEP>
-static void launch_rows_by_pairs(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_rows_by_pairs(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     const bool nt = streams_rows(p) && (TM == 64 || (int64_t)p.N * p.K >= ((int64_t)100 << 20));
     if (!rows_by_pairs(TM, p.M, p.N, p.K, p.w_row_bytes, (int)grid.y)) launch_bypass<EPI, TM, 128, kNestedF16Row, DEEP>(p, grid, stream);
     else if (nt) launch_bypass<EPI, TM, 128, kNestedF16Row, DEEP, true, true>(p, grid, stream);
@@ -1680,7 +1681,7 @@ static void launch_rows_by_pairs(const LargeParams &p, dim3 grid, hipStream_t st
 }
 
 template <int EPI, int TM, int TN>
-static void launch_rows_tile(const LargeParams &p, dim3 grid, hipStream_t stream) {
+static void launch_rows_tile(const LargeParamsOf<EPI> &p, dim3 grid, hipStream_t stream) {
     const int64_t knob = tuning().large_rows;
     const bool lds = knob >= 0 ? knob != 0 : rows_through_lds(TM > 128 ? 256 : 128, TN, p.M, p.K, p.w_row_bytes, (int)grid.y);
     if (!lds) {
@@ -1695,7 +1696,7 @@ static void launch_rows_tile(const LargeParams &p, dim3 grid, hipStream_t stream
 
 // weights through registers: NestedFP16 in either storage order, packed FP16.  TM: the height of the token tiles
 template <int EPI, int WK, int TM>
-static void launch_nested_tm(const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_nested_tm(const LargeParamsOf<EPI> &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     if constexpr (WK == kNestedF16Row) {
         if (c.tn == 128) launch_rows_tile<EPI, TM, 128>(p, grid, stream);
         else launch_rows_tile<EPI, TM, 256>(p, grid, stream);
@@ -1706,7 +1707,7 @@ static void launch_nested_tm(const LargeParams &p, const LargeConfig &c, dim3 gr
 }
 
 template <int EPI, int WK>
-static void launch_nested(const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_nested(const LargeParamsOf<EPI> &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     if (c.height == 256) { launch_nested_tm<EPI, WK, 256>(p, c, grid, stream);  return; }
     if (c.height == 224) { launch_nested_tm<EPI, WK, 224>(p, c, grid, stream);  return; }
     if (c.height == 192) { launch_nested_tm<EPI, WK, 192>(p, c, grid, stream);  return; }
@@ -1746,20 +1747,20 @@ static void launch_nested(const LargeParams &p, const LargeConfig &c, dim3 grid,
 // The kernels of one epilogue: weights through LDS, weights through registers.  With an epilogue, each of the two is instantiated in a source of
 // its own (they take the compiler a minute each).
 template <int EPI>
-static void launch_staged_t(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_staged_t(int kind, const LargeParamsOf<EPI> &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     if (kind == kPlainF16) launch_large_k<EPI, kPlainF16>(p, c, grid, stream);
     else if (kind == kE4M3) launch_large_k<EPI, kE4M3>(p, c, grid, stream);
     else launch_large_k<EPI, kE4M3Row>(p, c, grid, stream);
 }
 template <int EPI>
-static void launch_nested_t(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_nested_t(int kind, const LargeParamsOf<EPI> &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     if (kind == kNestedF16) launch_nested<EPI, kNestedF16>(p, c, grid, stream);
     else if (kind == kNestedF16Row) launch_nested<EPI, kNestedF16Row>(p, c, grid, stream);
     else if constexpr (EPI == kEpiNone) launch_nested<EPI, kPlainF16Packed>(p, c, grid, stream);       // (a baseline: no layer has it)
 }
-void launch_staged_full(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
-void launch_staged_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
-void launch_nested_full(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
-void launch_nested_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_staged_full(int kind, const FusedLargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_staged_gated(int kind, const FusedLargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_nested_full(int kind, const FusedLargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
+void launch_nested_gated(int kind, const FusedLargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream);
 
 }  // namespace nfp

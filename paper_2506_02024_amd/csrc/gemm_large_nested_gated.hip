@@ -3,7 +3,7 @@
 
 namespace nfp {
 
-void launch_nested_gated(int kind, const LargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
+void launch_nested_gated(int kind, const FusedLargeParams &p, const LargeConfig &c, dim3 grid, hipStream_t stream) {
     launch_nested_t<kEpiGated>(kind, p, c, grid, stream);
 }
 

@@ -7,13 +7,16 @@
 
 namespace nfp {
 
+struct NoEpilogue {};
+template <int EPI> using ReducedEpilogue = std::conditional_t<EPI == kEpiNone, NoEpilogue, Epilogue>;
+
 // Sums the S split-K partials (rows of ldp floats) in slice order, four columns per lane, applies the
 // FP8-mode scale, writes fp16.  VEC: 8-byte stores (N % 4 == 0 and 8-byte aligned output rows; gated: 4-byte
 // stores).
 template <int EPI, bool VEC>
 __global__ void __launch_bounds__(256)
 splitk_reduce_kernel(const float *__restrict__ partials, int S, int M, int N, int ldp, const float *scales,
-                     float w_scale, uint16_t *Y, int64_t ldy, Epilogue epi) {
+                     float w_scale, uint16_t *Y, int64_t ldy, ReducedEpilogue<EPI> epi) {
     const int64_t total = (int64_t)M * ldp;
     const int64_t idx = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (idx >= total) return;
@@ -64,7 +67,7 @@ splitk_reduce_kernel(const float *__restrict__ partials, int S, int M, int N, in
 
 template <int EPI>
 static void launch_reduce_t(const float *partials, int S, int64_t M, int64_t N, const float *scales, float w_scale, uint16_t *Y, int64_t ldy,
-                            const Epilogue &epi, hipStream_t stream) {
+                            const ReducedEpilogue<EPI> &epi, hipStream_t stream) {
     const int64_t ldp = partial_ld(N), total = M * ldp;
     const int64_t piece = EPI == kEpiGated ? 2 : 4;            // outputs of a lane
     const bool vec = (N & 3) == 0 && ldy % piece == 0 && (reinterpret_cast<uintptr_t>(Y) & (2 * piece - 1)) == 0;
@@ -75,7 +78,7 @@ static void launch_reduce_t(const float *partials, int S, int64_t M, int64_t N, 
 
 int launch_splitk_reduce(const float *partials, int S, int64_t M, int64_t N, const float *scales,
                          float w_scale, uint16_t *Y, int64_t ldy, const Epilogue &epi, hipStream_t stream) {
-    if (epi.kind == kEpiNone) launch_reduce_t<kEpiNone>(partials, S, M, N, scales, w_scale, Y, ldy, epi, stream);
+    if (epi.kind == kEpiNone) launch_reduce_t<kEpiNone>(partials, S, M, N, scales, w_scale, Y, ldy, NoEpilogue(), stream);
     else if (epi.kind == kEpiFull) launch_reduce_t<kEpiFull>(partials, S, M, N, scales, w_scale, Y, ldy, epi, stream);
     else launch_reduce_t<kEpiGated>(partials, S, M, N, scales, w_scale, Y, ldy, epi, stream);
     return hip_ok(hipGetLastError());
@@ -232,7 +235,7 @@ bool small_gemm_fuses_quant(int64_t M, int64_t N, int64_t K) {
 
 int launch_small_gemm(int kind, const GemmArgs &a, hipStream_t stream) {
     SmallConfig c = choose_small(kind, a.M, a.N, a.K);
-    SmallParams p;
+    FusedSmallParams p;
     p.X = static_cast<const uint8_t *>(a.X);
     p.x_row_bytes = (kind == kE4M3 || kind == kE4M3Row) ? a.ldx : 2 * a.ldx;
     p.scales = a.scales;

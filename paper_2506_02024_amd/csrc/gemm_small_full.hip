@@ -3,7 +3,7 @@
 
 namespace nfp {
 
-void launch_stream_full(int kind, const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
+void launch_stream_full(int kind, const FusedSmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
     launch_stream_t<kEpiFull>(kind, p, c, grid, stream);
 }
 

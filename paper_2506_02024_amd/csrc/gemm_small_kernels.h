@@ -51,8 +51,11 @@ struct SmallParams {
     int tile_stride;        // distance between a workgroup's consecutive tiles (1 or gridDim.x)
     int rotate;             // 1: the waves' K-slices are rotated from workgroup to workgroup
     int vec_store;          // 1: 8-byte fp16 stores allowed (gated: 4-byte ones)
-    Epilogue epi;
 };
+// (Arguments that a kernel does not use cost it time all the same: the epilogue's 40 bytes in the bare kernels' arguments made each launch 0.2 to 0.3 us longer, 1.0 to 2.7 % of a decode step's
+// linears of 16 tokens.)
+struct FusedSmallParams : SmallParams { Epilogue epi; };
+template <int EPI> using SmallParamsOf = std::conditional_t<EPI == kEpiNone, SmallParams, FusedSmallParams>;
 
 template <int KIND> struct StepK { static constexpr int value = kind_is_fp8(KIND) ? 128 : 64; };
 
@@ -224,7 +227,7 @@ struct FetchTile<KIND, SPW, POL, SPW> {
 //   across the waves once, at the end, in fixed wave order.
 template <int KIND, int MT, int SPW, bool MULTIPASS, int POL, int EPI>
 __global__ void __launch_bounds__((MT == 4 || SPW == 8) ? 512 : 1024)
-small_gemm_kernel(SmallParams p) {
+small_gemm_kernel(SmallParamsOf<EPI> p) {
     extern __shared__ float lds[];                    // [tile][wave][MT][64] x float4, then 2 KB per wave
     const int lane = threadIdx.x & 63;
     const int wave = threadIdx.x >> 6;
@@ -548,7 +551,7 @@ static inline size_t small_lds(const SmallConfig &c) {
 constexpr int kQuantLds = 158 * 1024;                            // (the row maxima and scales are static)
 
 template <int EPI, int KIND, int MT, int SPW, int POL = kStream>
-static void launch_small_t(const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_small_t(const SmallParamsOf<EPI> &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
     if constexpr (!kind_is_packed(KIND) && POL == kStream) {      // rows that do not start on lines (see kStream)
         if ((p.w_row_bytes & 127) != 0 || (reinterpret_cast<uintptr_t>(p.W0) & 127) != 0 ||
             (reinterpret_cast<uintptr_t>(p.W1) & 127) != 0) {
@@ -573,7 +576,7 @@ static void launch_small_t(const SmallParams &p, const SmallConfig &c, dim3 grid
 }
 
 template <int EPI, int KIND>
-static void launch_small_k(const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_small_k(const SmallParamsOf<EPI> &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
     if constexpr (KIND == kPlainF16 || KIND == kNestedF16Row) {
         if (c.mt == 1 && c.spw == 8) { launch_small_t<EPI, KIND, 1, 8>(p, c, grid, stream);  return; }
     }
@@ -592,7 +595,7 @@ static void launch_small_k(const SmallParams &p, const SmallConfig &c, dim3 grid
 
 // The kernels of one epilogue; each is instantiated in a source of its own.
 template <int EPI>
-static void launch_stream_t(int kind, const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
+static void launch_stream_t(int kind, const SmallParamsOf<EPI> &p, const SmallConfig &c, dim3 grid, hipStream_t stream) {
     switch (kind) {
         case kPlainF16: launch_small_k<EPI, kPlainF16>(p, c, grid, stream); break;
         case kPlainF16Packed:
@@ -606,7 +609,7 @@ static void launch_stream_t(int kind, const SmallParams &p, const SmallConfig &c
         default: launch_small_k<EPI, kE4M3>(p, c, grid, stream); break;
     }
 }
-void launch_stream_full(int kind, const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream);
-void launch_stream_gated(int kind, const SmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream);
+void launch_stream_full(int kind, const FusedSmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream);
+void launch_stream_gated(int kind, const FusedSmallParams &p, const SmallConfig &c, dim3 grid, hipStream_t stream);
 
 }  // namespace nfp
